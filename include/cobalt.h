@@ -333,6 +333,98 @@ int cobalt_forward_rows(const void* dedup_send, const int32_t* fwd_src_row, cons
                         int64_t P, int32_t H, void* recv, int64_t src_rows, int64_t dst_rows,
                         cobalt_stream_t stream);
 
+/* ==== the layer around the routed rows ==========================================================
+ * The training step that the routing serves (Section 1: gating, assignment, dispatch, expert FFN,
+ * combine) has operators on both sides of the four stages.  These are they, for the same conventions
+ * (device pointers, 16-byte alignment, caller's workspace, one stream, no synchronisation).
+ *   x -> cobalt_layer_norm -> (logits = n Wr^T, a plain product) -> cobalt_gate_topk -> route
+ *     -> cobalt_permute -> cobalt_expert_ffn -> cobalt_combine -> cobalt_dropout_add with x
+ * and the *_backward calls in the opposite order, around cobalt_combine_backward and
+ * cobalt_permute_backward.  All sums are fp32; bf16 results are rounded once, to nearest even. */
+
+/* element types of the dense operators */
+#define COBALT_BF16 0
+#define COBALT_F32 1
+
+/* ---- layer norm -----------------------------------------------------------------------------
+ * Over the H columns of each of T rows, z = (x - mean) * rstd, rstd = 1 / sqrt(variance + eps):
+ *   y = z * gamma + beta
+ *   grad_x = rstd * (g - mean(g) - z * mean(g * z)) with g = grad_y * gamma
+ *   grad_gamma = sum_t grad_y * z      grad_beta = sum_t grad_y       (overwritten)
+ * x, y, grad_y, grad_x: [T, H] of `dtype` (COBALT_BF16 or COBALT_F32).  gamma, beta, their gradients
+ * fp32 [H]; mean, rstd fp32 [T], written by the forward call and read by the backward call.
+ * H a multiple of 8, at most 16384; T < 2^31; T = 0 is allowed (the gradients are then 0).  eps >= 0.
+ * y may be x, grad_x may be grad_y.  Results do not vary from run to run. */
+int cobalt_layer_norm(const void* x, const float* gamma, const float* beta, int64_t T, int32_t H,
+                      int32_t dtype, float eps, void* y, float* mean, float* rstd,
+                      cobalt_stream_t stream);
+size_t cobalt_layer_norm_workspace_bytes(int64_t T, int32_t H);
+int cobalt_layer_norm_backward(const void* grad_y, const void* x, const float* gamma, const float* mean,
+                               const float* rstd, int64_t T, int32_t H, int32_t dtype, void* grad_x,
+                               float* grad_gamma, float* grad_beta, void* workspace,
+                               size_t workspace_bytes, cobalt_stream_t stream);
+
+/* ---- gate: the routing path's topk_ids and gate_w, and where its grad_gate_w goes -----------------
+ * logits [T, E] of `dtype`.  topk_ids int32 [T, K]: the K largest logits of a token, descending, equal
+ * ones by ascending id; distinct within a token whatever the logits hold (a NaN orders above +inf, as
+ * if largest; masked experts are -inf or the type's lowest value).  gate_w fp32 [T, K]:
+ *   default               softmax over the K chosen logits
+ *   COBALT_GATE_SIGMOID   sigmoid of the chosen logits, divided by their sum
+ * A token whose chosen logits are all -inf gets weights 0; NaN and +inf give NaN weights where exp does.
+ * Backward: grad_logits [T, E] of `dtype`, w_k (g_k - sum_j g_j w_j) at the chosen ids (times 1 - sigmoid
+ * with COBALT_GATE_SIGMOID, which reads `logits`; NULL is accepted otherwise) and 0 elsewhere.  An id
+ * outside [0, E) sets COBALT_DEVERR_BAD_EXPERT_ID and is skipped.  E <= 1024, K <= min(E, 16). */
+#define COBALT_GATE_SIGMOID 0x1u
+int cobalt_gate_topk(const void* logits, int64_t T, int32_t E, int32_t K, int32_t dtype,
+                     int32_t* topk_ids, float* gate_w, uint32_t flags, cobalt_stream_t stream);
+int cobalt_gate_topk_backward(const float* grad_gate_w, const void* logits, const int32_t* topk_ids,
+                              const float* gate_w, int64_t T, int32_t E, int32_t K, int32_t dtype,
+                              void* grad_logits, uint32_t flags, cobalt_stream_t stream);
+
+/* ---- expert feed-forward over the dispatched rows ---------------------------------------------------
+ * rows bf16 [P, H] in the order of `send`: rows dest_offsets[d] .. dest_offsets[d+1] belong to slot d,
+ * whose expert is slot_expert[d] (device int32 [D]; -1 = empty).  With e that expert, w_gate_up bf16
+ * [E, 2F, H] (F gate rows, then F up rows) and w_down bf16 [E, H, F]:
+ *   pre = x w_gate_up[e]^T = (g, u)     act = g * sigmoid(g) * u     out = act w_down[e]^T
+ * act bf16 [P, F] is scratch for inference and an input of the backward call; pre bf16 [P, 2F] is only
+ * needed by the backward call (NULL for inference).
+ * Backward: grad_pre bf16 [P, 2F] is scratch (it may be `pre` itself, which is then overwritten);
+ *   d_act = grad_out w_down[e]     d_u = d_act g s     d_g = d_act u s (1 + g (1 - s)),  s = sigmoid(g)
+ *   grad_rows = (d_g, d_u) w_gate_up[e]      grad_w_gate_up[e] = sum (d_g, d_u)^T x
+ *   grad_w_down[e] = sum grad_out^T act      sums over the rows of ALL slots that hold e
+ * Weight gradients are bf16 in the weights' layout and overwritten (0 for an expert without rows);
+ * any of the three results may be NULL, but not all.  act and the pre-activations are rounded to bf16
+ * once each, products accumulate in fp32.  Rows outside [dest_offsets[0], dest_offsets[D]) are neither
+ * read nor written.  dest_offsets must not decrease or pass P (clamped), and a slot with rows must hold an
+ * expert in [0, E): otherwise COBALT_DEVERR_BAD_SLOT is set and its rows are skipped.
+ * H and F multiples of 8, at most COBALT_FFN_MAX_WIDTH; D <= 4096, E <= 1024, P < 2^31. */
+#define COBALT_FFN_MAX_WIDTH 65536
+size_t cobalt_expert_ffn_workspace_bytes(int64_t P, int32_t D, int32_t E, int32_t H, int32_t F);
+int cobalt_expert_ffn(const void* rows, const uint32_t* dest_offsets, const int32_t* slot_expert,
+                      int64_t P, int32_t D, int32_t E, int32_t H, int32_t F, const void* w_gate_up,
+                      const void* w_down, void* act, void* pre, void* out, void* workspace,
+                      size_t workspace_bytes, cobalt_stream_t stream);
+int cobalt_expert_ffn_backward(const void* grad_out, const void* rows, const uint32_t* dest_offsets,
+                               const int32_t* slot_expert, int64_t P, int32_t D, int32_t E, int32_t H,
+                               int32_t F, const void* w_gate_up, const void* w_down, const void* pre,
+                               const void* act, void* grad_pre, void* grad_rows, void* grad_w_gate_up,
+                               void* grad_w_down, void* workspace, size_t workspace_bytes,
+                               cobalt_stream_t stream);
+
+/* ---- dropout, added to the residual stream ----------------------------------------------------------
+ * out[i] = residual[i] + (keep(i) ? x[i] * scale : 0), n elements of `dtype`; residual NULL = 0.
+ * keep(i) is drawn anew from (seed, i) by every call, so no mask is stored: Philox-4x32-10 with the
+ * counter (b mod 2^32, b / 2^32, 0, 0), b = i / 8, and the key (seed mod 2^32, seed / 2^32); element i is
+ * kept when half-word i % 8 (low half of word 0, high half of word 0, low half of word 1, ...) is >=
+ * round(p * 2^16), and scale = 2^16 / (2^16 - round(p * 2^16)), 0 if all are dropped.  0 <= p <= 1.
+ * Backward: grad_x[i] = keep(i) ? grad_out[i] * scale : 0; the residual's gradient is grad_out itself.
+ * A dropped element is 0 whatever x holds.  out may be x or residual, grad_x may be grad_out.
+ * flags: COBALT_SEED_ON_DEVICE, as for cobalt_assign. */
+int cobalt_dropout_add(const void* x, const void* residual, int64_t n, int32_t dtype, double p,
+                       uint64_t seed, void* out, uint32_t flags, cobalt_stream_t stream);
+int cobalt_dropout_add_backward(const void* grad_out, int64_t n, int32_t dtype, double p, uint64_t seed,
+                                void* grad_x, uint32_t flags, cobalt_stream_t stream);
+
 /* ---- device error word -------------------------------------------------------------------
  * Waits for `stream`, copies the COBALT_DEVERR_* bits set by kernels on the current device
  * since the last call into *out_bits_host and clears them. */

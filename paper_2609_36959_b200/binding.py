@@ -39,6 +39,8 @@ STATS_TILE16 = 0x10
 STATS_TILE32 = 0x20
 ROUTE_SEPARATE_KERNELS = 0x40
 EMA_INITIALISE = 0x1
+GATE_SIGMOID = 0x1
+BF16, F32 = 0, 1
 IMPL_VECTOR = 0x100
 IMPL_BULK = 0x200
 
@@ -55,6 +57,10 @@ EXPORTS = (
     "cobalt_ema_update", "cobalt_ochiai", "cobalt_rebalance_intra_node",
     "cobalt_dedup_workspace_bytes", "cobalt_dedup_index", "cobalt_forward_rows",
     "cobalt_combine", "cobalt_read_and_clear_device_error",
+    "cobalt_layer_norm", "cobalt_layer_norm_workspace_bytes", "cobalt_layer_norm_backward",
+    "cobalt_gate_topk", "cobalt_gate_topk_backward",
+    "cobalt_expert_ffn_workspace_bytes", "cobalt_expert_ffn", "cobalt_expert_ffn_backward",
+    "cobalt_dropout_add", "cobalt_dropout_add_backward",
 )
 
 
@@ -102,6 +108,17 @@ def _load() -> C.CDLL:
         "cobalt_forward_rows": (C.c_int, [vp, vp, vp, i64, i32, vp, i64, i64, vp]),
         "cobalt_permute_rows_block": (C.c_int, [vp, vp, i64, i32, i32, vp, i64, u32, vp]),
         "cobalt_combine_block": (C.c_int, [vp, vp, vp, i64, i32, i32, vp, i64, u32, vp]),
+        "cobalt_layer_norm": (C.c_int, [vp, vp, vp, i64, i32, i32, C.c_float, vp, vp, vp, vp]),
+        "cobalt_layer_norm_workspace_bytes": (sz, [i64, i32]),
+        "cobalt_layer_norm_backward": (C.c_int, [vp, vp, vp, vp, vp, i64, i32, i32, vp, vp, vp, vp, sz, vp]),
+        "cobalt_gate_topk": (C.c_int, [vp, i64, i32, i32, i32, vp, vp, u32, vp]),
+        "cobalt_gate_topk_backward": (C.c_int, [vp, vp, vp, vp, i64, i32, i32, i32, vp, u32, vp]),
+        "cobalt_expert_ffn_workspace_bytes": (sz, [i64, i32, i32, i32, i32]),
+        "cobalt_expert_ffn": (C.c_int, [vp, vp, vp, i64, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]),
+        "cobalt_expert_ffn_backward": (C.c_int, [vp, vp, vp, vp, i64, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp,
+                                                 sz, vp]),
+        "cobalt_dropout_add": (C.c_int, [vp, vp, i64, i32, C.c_double, u64, vp, u32, vp]),
+        "cobalt_dropout_add_backward": (C.c_int, [vp, i64, i32, C.c_double, u64, vp, u32, vp]),
         "cobalt_read_and_clear_device_error": (C.c_int, [C.POINTER(u32), vp]),
     }
     for name, (res, args) in sig.items():
@@ -529,6 +546,158 @@ def forward_rows(dedup_send: torch.Tensor, fwd_src_row: torch.Tensor, row_of_pai
                                     _ptr(row_of_pair, torch.int32, "row_of_pair"), P, H,
                                     _ptr(recv, torch.bfloat16, "recv"), dedup_send.shape[0], recv.shape[0], _stream()),
            "cobalt_forward_rows")
+
+
+# ---- the layer around the routed rows ------------------------------------------------------
+
+_DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
+
+
+def _dtype_code(t: torch.Tensor, what: str) -> int:
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{what} must be bfloat16 or float32, got {t.dtype}")
+    return code
+
+
+def layer_norm(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, eps: float, y: torch.Tensor,
+               mean: torch.Tensor, rstd: torch.Tensor) -> None:
+    """y = (x - mean) * rstd * gamma + beta over the rows of x [T, H] (bfloat16 or float32; gamma, beta float32 [H]).
+    mean and rstd (float32 [T]) are kept for layer_norm_backward."""
+    T, H = x.shape
+    code = _dtype_code(x, "x")
+    if gamma.numel() != H or beta.numel() != H or y.shape != x.shape or mean.numel() != T or rstd.numel() != T:
+        raise CobaltError(ERR_INVALID_ARG, "layer_norm (sizes)")
+    _check(_lib.cobalt_layer_norm(_ptr(x, None, "x"), _ptr(gamma, torch.float32, "gamma"), _ptr(beta, torch.float32, "beta"),
+                                  T, H, code, eps, _ptr(y, x.dtype, "y"), _ptr(mean, torch.float32, "mean"),
+                                  _ptr(rstd, torch.float32, "rstd"), _stream()), "cobalt_layer_norm")
+
+
+def layer_norm_workspace_bytes(T: int, H: int) -> int:
+    return _lib.cobalt_layer_norm_workspace_bytes(T, H)
+
+
+def layer_norm_backward(grad_y: torch.Tensor, x: torch.Tensor, gamma: torch.Tensor, mean: torch.Tensor,
+                        rstd: torch.Tensor, grad_x: torch.Tensor, grad_gamma: torch.Tensor, grad_beta: torch.Tensor,
+                        workspace: torch.Tensor) -> None:
+    """Gradients of layer_norm: grad_x like x, grad_gamma and grad_beta float32 [H] (overwritten)."""
+    T, H = x.shape
+    code = _dtype_code(x, "x")
+    if (grad_y.shape != x.shape or grad_x.shape != x.shape or gamma.numel() != H or mean.numel() != T or
+            rstd.numel() != T or grad_gamma.numel() != H or grad_beta.numel() != H):
+        raise CobaltError(ERR_INVALID_ARG, "layer_norm_backward (sizes)")
+    _check(_lib.cobalt_layer_norm_backward(_ptr(grad_y, x.dtype, "grad_y"), _ptr(x, None, "x"),
+                                           _ptr(gamma, torch.float32, "gamma"), _ptr(mean, torch.float32, "mean"),
+                                           _ptr(rstd, torch.float32, "rstd"), T, H, code, _ptr(grad_x, x.dtype, "grad_x"),
+                                           _ptr(grad_gamma, torch.float32, "grad_gamma"),
+                                           _ptr(grad_beta, torch.float32, "grad_beta"), _ptr(workspace),
+                                           _ws_bytes(workspace), _stream()), "cobalt_layer_norm_backward")
+
+
+def gate_topk(logits: torch.Tensor, topk_ids: torch.Tensor, gate_w: torch.Tensor, *, flags: int = 0) -> None:
+    """The K largest logits of each token (descending, ties to the lowest id) and their weights: softmax over the
+    chosen, or with flags=GATE_SIGMOID their sigmoids divided by the sum.  logits [T, E] bfloat16 or float32;
+    topk_ids int32 [T, K] and gate_w float32 [T, K] are the gating output that the routing stages take."""
+    T, E = logits.shape
+    code = _dtype_code(logits, "logits")
+    if topk_ids.dim() != 2 or topk_ids.shape[0] != T or gate_w.shape != topk_ids.shape:
+        raise CobaltError(ERR_INVALID_ARG, "gate_topk (output sizes)")
+    _check(_lib.cobalt_gate_topk(_ptr(logits, None, "logits"), T, E, topk_ids.shape[1], code,
+                                 _ptr(topk_ids, torch.int32, "topk_ids"), _ptr(gate_w, torch.float32, "gate_w"), flags,
+                                 _stream()), "cobalt_gate_topk")
+
+
+def gate_topk_backward(grad_gate_w: torch.Tensor, logits: torch.Tensor, topk_ids: torch.Tensor, gate_w: torch.Tensor,
+                       grad_logits: torch.Tensor, *, flags: int = 0) -> None:
+    """grad_logits [T, E] (like logits) from grad_gate_w [T, K], e.g. that of combine_backward."""
+    T, E = logits.shape
+    code = _dtype_code(logits, "logits")
+    if (topk_ids.dim() != 2 or topk_ids.shape[0] != T or gate_w.shape != topk_ids.shape or
+            grad_gate_w.shape != topk_ids.shape or grad_logits.shape != logits.shape):
+        raise CobaltError(ERR_INVALID_ARG, "gate_topk_backward (sizes)")
+    _check(_lib.cobalt_gate_topk_backward(_ptr(grad_gate_w, torch.float32, "grad_gate_w"), _ptr(logits, None, "logits"),
+                                          _ptr(topk_ids, torch.int32, "topk_ids"), _ptr(gate_w, torch.float32, "gate_w"),
+                                          T, E, topk_ids.shape[1], code, _ptr(grad_logits, logits.dtype, "grad_logits"),
+                                          flags, _stream()), "cobalt_gate_topk_backward")
+
+
+def expert_ffn_workspace_bytes(P: int, D: int, E: int, H: int, F: int) -> int:
+    return _lib.cobalt_expert_ffn_workspace_bytes(P, D, E, H, F)
+
+
+def _ffn_sizes(rows, dest_offsets, slot_expert, w_gate_up, w_down, what):
+    P, H = rows.shape
+    if w_down.dim() != 3 or w_gate_up.dim() != 3:
+        raise CobaltError(ERR_INVALID_ARG, f"{what} (weights must be [E, 2F, H] and [E, H, F])")
+    E, F = w_down.shape[0], w_down.shape[2]
+    D = slot_expert.numel()
+    if tuple(w_gate_up.shape) != (E, 2 * F, H) or w_down.shape[1] != H or dest_offsets.numel() != D + 1:
+        raise CobaltError(ERR_INVALID_ARG, f"{what} (sizes)")
+    return P, H, E, F, D
+
+
+def _ffn_buffer(t: Optional[torch.Tensor], shape, what: str) -> Optional[int]:
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise CobaltError(ERR_INVALID_ARG, f"{what} (size)")
+    return _ptr(t, torch.bfloat16, what)
+
+
+def expert_ffn(rows: torch.Tensor, dest_offsets: torch.Tensor, slot_expert: torch.Tensor, w_gate_up: torch.Tensor,
+               w_down: torch.Tensor, act: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor, *,
+               pre: Optional[torch.Tensor] = None) -> None:
+    """out = (silu(x Wg^T) * (x Wu^T)) Wd^T for the rows of every slot, with the weights of the slot's expert.
+
+    rows, out bfloat16 [P, H] in the order of the send buffer; dest_offsets int32 [D+1] and slot_expert int32 [D] on
+    the device; w_gate_up [E, 2F, H] (gate rows first), w_down [E, H, F].  act [P, F] and, if a backward pass follows,
+    pre [P, 2F] are written and kept for expert_ffn_backward."""
+    P, H, E, F, D = _ffn_sizes(rows, dest_offsets, slot_expert, w_gate_up, w_down, "expert_ffn")
+    _check(_lib.cobalt_expert_ffn(_ptr(rows, torch.bfloat16, "rows"), _ptr(dest_offsets, torch.int32, "dest_offsets"),
+                                  _ptr(slot_expert, torch.int32, "slot_expert"), P, D, E, H, F,
+                                  _ptr(w_gate_up, torch.bfloat16, "w_gate_up"), _ptr(w_down, torch.bfloat16, "w_down"),
+                                  _ffn_buffer(act, (P, F), "act"), _ffn_buffer(pre, (P, 2 * F), "pre"),
+                                  _ffn_buffer(out, (P, H), "out"), _ptr(workspace), _ws_bytes(workspace), _stream()),
+           "cobalt_expert_ffn")
+
+
+def expert_ffn_backward(grad_out: torch.Tensor, rows: torch.Tensor, dest_offsets: torch.Tensor, slot_expert: torch.Tensor,
+                        w_gate_up: torch.Tensor, w_down: torch.Tensor, pre: torch.Tensor, act: torch.Tensor,
+                        grad_pre: torch.Tensor, workspace: torch.Tensor, *, grad_rows: Optional[torch.Tensor] = None,
+                        grad_w_gate_up: Optional[torch.Tensor] = None,
+                        grad_w_down: Optional[torch.Tensor] = None) -> None:
+    """Gradients of expert_ffn from grad_out [P, H] and the act and pre of the forward call.  grad_pre [P, 2F] is
+    scratch and may be `pre`.  Each of the three results may be left out; weight gradients are overwritten."""
+    P, H, E, F, D = _ffn_sizes(rows, dest_offsets, slot_expert, w_gate_up, w_down, "expert_ffn_backward")
+    _check(_lib.cobalt_expert_ffn_backward(
+        _ffn_buffer(grad_out, (P, H), "grad_out"), _ptr(rows, torch.bfloat16, "rows"),
+        _ptr(dest_offsets, torch.int32, "dest_offsets"), _ptr(slot_expert, torch.int32, "slot_expert"), P, D, E, H, F,
+        _ptr(w_gate_up, torch.bfloat16, "w_gate_up"), _ptr(w_down, torch.bfloat16, "w_down"),
+        _ffn_buffer(pre, (P, 2 * F), "pre"), _ffn_buffer(act, (P, F), "act"), _ffn_buffer(grad_pre, (P, 2 * F), "grad_pre"),
+        _ffn_buffer(grad_rows, (P, H), "grad_rows"), _ffn_buffer(grad_w_gate_up, (E, 2 * F, H), "grad_w_gate_up"),
+        _ffn_buffer(grad_w_down, (E, H, F), "grad_w_down"), _ptr(workspace), _ws_bytes(workspace), _stream()),
+        "cobalt_expert_ffn_backward")
+
+
+def dropout_add(x: torch.Tensor, residual: Optional[torch.Tensor], p: float, seed, out: torch.Tensor) -> None:
+    """out = residual + dropout(x) (residual None: dropout alone), bfloat16 or float32.  The mask is a function of
+    (seed, element index) and is drawn again by dropout_add_backward; seed as in assign: an int, or a one-element
+    int64 CUDA tensor read when the kernel runs."""
+    code = _dtype_code(x, "x")
+    if out.shape != x.shape or (residual is not None and residual.shape != x.shape):
+        raise CobaltError(ERR_INVALID_ARG, "dropout_add (sizes)")
+    seed, flags = _seed_arg(seed, 0)
+    _check(_lib.cobalt_dropout_add(_ptr(x, None, "x"), _ptr(residual, x.dtype, "residual"), x.numel(), code, p, seed,
+                                   _ptr(out, x.dtype, "out"), flags, _stream()), "cobalt_dropout_add")
+
+
+def dropout_add_backward(grad_out: torch.Tensor, p: float, seed, grad_x: torch.Tensor) -> None:
+    """grad_x = grad_out * scale where dropout_add with this p and seed kept the element, 0 elsewhere."""
+    code = _dtype_code(grad_out, "grad_out")
+    if grad_x.shape != grad_out.shape:
+        raise CobaltError(ERR_INVALID_ARG, "dropout_add_backward (sizes)")
+    seed, flags = _seed_arg(seed, 0)
+    _check(_lib.cobalt_dropout_add_backward(_ptr(grad_out, None, "grad_out"), grad_out.numel(), code, p, seed,
+                                            _ptr(grad_x, grad_out.dtype, "grad_x"), flags, _stream()),
+           "cobalt_dropout_add_backward")
 
 
 def read_and_clear_device_error() -> int:
