@@ -5,142 +5,705 @@
 //   da = Wd^T dy    du = da g s    dg = da u s (1 + g (1 - s))    dx = Wg^T dg + Wu^T du
 //   dWg = sum dg x^T    dWu = sum du x^T    dWd = sum dy a^T     over the rows of all slots that hold e
 //
-// First form: plain shared-memory tiles on the fp32 units, right for every size.
+// Every step is a product on the tensor cores (tcgen05, bf16 operands, fp32 accumulators in tensor memory) with the
+// elementwise part in its epilogue.  One kernel template serves the five products:
+//
+//   - A CTA pair computes a tile of 256 features (M: 128 a CTA) by up to 256 rows of one slot (N).  The weights are
+//     the M side, so that a slot's ragged row count is the N extent of the instruction, a multiple of 32 chosen for
+//     every tile: a slot of 40 rows costs 64, not 128 or 256, and a single token streams the weights once.
+//     The weight gradients have features on both sides and the rows as the summed extent.
+//   - Warp 0 of each CTA feeds a ring of 64-deep blocks by tensor-map loads, warp 1 of the leading CTA issues the
+//     products, warps 2 to 5 run the epilogue.  Two accumulators (2 x 256 of 512 columns) let the epilogue of a tile
+//     run under the products of the next one.
+//   - CTAs are persistent, a pair for every two SMs, and deal the tiles of all slots round robin; the tile list is
+//     built on the device from dest_offsets (no copy to the host).
+//
+// Every wait is bounded: when one runs out the kernel sets COBALT_DEVERR_WAIT_TIMEOUT, drains its copies, frees its
+// tensor memory and returns.
 #include "numeric.cuh"
+#include "tcgen05.cuh"
 
 namespace cobalt {
 
 typedef __nv_bfloat16 bf16;
 
-constexpr int kTile = 64, kTileK = 16;
+// ---- tile lists ------------------------------------------------------------------------------------------------
 
-// Rows of slot d, clamped so that no bad offset leads out of the buffers.
-__device__ __forceinline__ void slot_rows(const uint32_t* offsets, int d, int64_t P, int64_t* first, int64_t* last)
+constexpr int kTileM = 256;              // features of a pair
+constexpr int kTileN = 256;              // most rows (or, for weight gradients, columns) of a tile
+constexpr int kBlockK = 64;              // depth of one ring slot: 128 bytes, one swizzle row
+
+// Workspace: header, row tiles, experts' segment lists.
+struct PlanView {
+    int32_t* row_tiles;                  // [1] number of row tiles
+    int4* tile;                          // {first row, rows | slot's tiles << 9, expert, slot's first tile}
+    int32_t* seg_start;                  // [E + 1] into segs
+    int32_t* expert_blocks;              // [E] 64-row blocks of the expert's rows
+    int2* segs;                          // [D] {first row, rows}, slots in ascending order
+};
+
+__host__ __device__ inline int64_t max_row_tiles(int64_t P, int D) { return P / kTileN + D; }
+
+static size_t plan_bytes(int64_t P, int D, int E)
 {
-    const int64_t a = offsets[d], b = offsets[d + 1];
-    *first = a < P ? a : P;
-    *last = b < P ? b : P;
-    if (*last < *first) *last = *first;
+    return 256 + round_up(16 * static_cast<size_t>(max_row_tiles(P, D)), 256) + round_up(4 * static_cast<size_t>(E + 1), 256) +
+           round_up(4 * static_cast<size_t>(E), 256) + round_up(8 * static_cast<size_t>(D), 256);
 }
 
-// acc[i][j] += sum_k A[m0 + 4 ty + i][k] * B[n0 + 4 tx + j][k] for k in [k0, k1); element strides given.
-__device__ __forceinline__ void tile_product(const bf16* A, int64_t am, int64_t ak, int64_t m0, int64_t m1, const bf16* B,
-                                             int64_t bn, int64_t bk, int64_t n0, int64_t n1, int64_t k0, int64_t k1,
-                                             float (*sa)[kTile + 1], float (*sb)[kTile + 1], float (&acc)[4][4])
+static PlanView plan_view(void* workspace, int64_t P, int D, int E)
 {
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    for (int64_t k = k0; k < k1; k += kTileK) {
-        for (int i = threadIdx.x; i < kTile * kTileK; i += 256) {
-            const int kk = ak == 1 ? i % kTileK : i / kTile, m = ak == 1 ? i / kTileK : i % kTile;
-            sa[kk][m] = (m0 + m < m1 && k + kk < k1) ? __bfloat162float(A[(m0 + m) * am + (k + kk) * ak]) : 0.0f;
-        }
-        for (int i = threadIdx.x; i < kTile * kTileK; i += 256) {
-            const int kk = bk == 1 ? i % kTileK : i / kTile, n = bk == 1 ? i / kTileK : i % kTile;
-            sb[kk][n] = (n0 + n < n1 && k + kk < k1) ? __bfloat162float(B[(n0 + n) * bn + (k + kk) * bk]) : 0.0f;
-        }
-        __syncthreads();
+    PlanView v;
+    char* p = static_cast<char*>(workspace);
+    v.row_tiles = reinterpret_cast<int32_t*>(p);
+    p += 256;
+    v.tile = reinterpret_cast<int4*>(p);
+    p += round_up(16 * static_cast<size_t>(max_row_tiles(P, D)), 256);
+    v.seg_start = reinterpret_cast<int32_t*>(p);
+    p += round_up(4 * static_cast<size_t>(E + 1), 256);
+    v.expert_blocks = reinterpret_cast<int32_t*>(p);
+    p += round_up(4 * static_cast<size_t>(E), 256);
+    v.segs = reinterpret_cast<int2*>(p);
+    return v;
+}
+
+constexpr int kPlanThreads = 1024;
+
+// Exclusive prefix of v over the CTA; *total gets the sum.  `scratch`: 32 ints.
+__device__ __forceinline__ int block_prefix(int v, int* scratch, int* total)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int s = v;
 #pragma unroll
-        for (int kk = 0; kk < kTileK; ++kk)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(sa[kk][4 * ty + i], sb[kk][4 * tx + j], acc[i][j]);
-        __syncthreads();
+    for (int off = 1; off < 32; off <<= 1) {
+        const int o = __shfl_up_sync(0xFFFFFFFFu, s, off);
+        if (lane >= off) s += o;
     }
+    __syncthreads();                     // scratch of the previous call has been read
+    if (lane == 31) scratch[warp] = s;
+    __syncthreads();
+    if (warp == 0) {
+        int w = scratch[lane];
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const int o = __shfl_up_sync(0xFFFFFFFFu, w, off);
+            if (lane >= off) w += o;
+        }
+        scratch[lane] = w;
+    }
+    __syncthreads();
+    *total = scratch[31];
+    return s - v + (warp > 0 ? scratch[warp - 1] : 0);
 }
 
-enum { kUp, kDown, kDownBackward, kUpBackward };
+// One CTA.  Offsets that decrease or pass P are clamped, rows of a slot without a valid expert skipped, both flagged.
+__global__ void __launch_bounds__(kPlanThreads)
+ffn_plan_kernel(const uint32_t* __restrict__ offsets, const int32_t* __restrict__ slot_expert, int64_t P, int D, int E, PlanView out,
+                bool with_experts, uint32_t* __restrict__ err_word)
+{
+    __shared__ int scratch[32];
+    extern __shared__ int per_slot[];            // [4][D]
+    int *s_first = per_slot, *s_rows = per_slot + D, *s_tile = per_slot + 2 * D, *s_expert = per_slot + 3 * D;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int tiles_before = 0;
+    for (int base = 0; base < D; base += kPlanThreads) {
+        const int d = base + threadIdx.x;
+        int rows = 0, tiles = 0;
+        if (d < D) {
+            const int64_t a = offsets[d], b = offsets[d + 1];
+            const int64_t lo = a < P ? a : P, hi = b < P ? b : P;
+            const int e = slot_expert[d];
+            bool bad = b < a || b > P;
+            rows = hi > lo ? static_cast<int>(hi - lo) : 0;
+            if (rows > 0 && (e < 0 || e >= E)) {
+                bad = true;
+                rows = 0;
+            }
+            if (bad) flag_error(err_word, COBALT_DEVERR_BAD_SLOT);
+            s_first[d] = static_cast<int>(lo);
+            s_rows[d] = rows;
+            s_expert[d] = rows > 0 ? e : -1;
+            tiles = (rows + kTileN - 1) / kTileN;
+        }
+        int total;
+        const int at = block_prefix(tiles, scratch, &total);
+        if (d < D) s_tile[d] = tiles_before + at;
+        tiles_before += total;
+    }
+    if (threadIdx.x == 0) *out.row_tiles = tiles_before;
+    __syncthreads();
+    for (int d = warp; d < D; d += kPlanThreads / 32) {
+        const int rows = s_rows[d], n = (rows + kTileN - 1) / kTileN;
+        if (n == 0) continue;
+        // the slot's rows in equal tiles of a multiple of 32 rows: all but the last are full
+        const int step = ((rows + n - 1) / n + 31) / 32 * 32;
+        for (int i = lane; i < n; i += 32) {
+            const int left = rows - i * step;
+            out.tile[s_tile[d] + i] = make_int4(s_first[d] + i * step, (left < step ? left : step) | (n << 9), s_expert[d], s_tile[d]);
+        }
+    }
+    if (!with_experts) return;
+    // segments of every expert in ascending slot order (E <= 1024: an expert a thread)
+    const int e = threadIdx.x;
+    int count = 0, blocks = 0;
+    if (e < E)
+        for (int d = 0; d < D; ++d)
+            if (s_expert[d] == e) {
+                count += 1;
+                blocks += (s_rows[d] + kBlockK - 1) / kBlockK;
+            }
+    int total;
+    int at = block_prefix(count, scratch, &total);
+    if (e < E) {
+        out.seg_start[e] = at;
+        out.expert_blocks[e] = blocks;
+        if (count > 0)
+            for (int d = 0; d < D; ++d)
+                if (s_expert[d] == e) out.segs[at++] = make_int2(s_first[d], s_rows[d]);
+    }
+    if (threadIdx.x == 0) out.seg_start[E] = total;
+}
 
-struct FfnArgs {
-    const bf16 *rows, *w_gate_up, *w_down, *grad_out, *pre_in, *act_in;
-    bf16 *act, *pre, *out, *grad_pre, *grad_rows;
-    const uint32_t* offsets;
-    const int32_t* slot_expert;
-    int64_t P;
-    int D, E, H, F;
+// ---- the product kernel ------------------------------------------------------------------------------------------
+
+enum Stage {
+    kUp,             // act, pre   = rows     x w_gate_up^T   (gate and up features interleaved by eight along M)
+    kDown,           // out        = act      x w_down^T
+    kDownBackward,   // grad_pre   from grad_out x w_down
+    kUpBackward,     // grad_rows  = grad_pre x w_gate_up
+    kWeights         // a weight gradient: (M side)^T x (N side) over the rows
+};
+
+struct ProductArgs {
+    PlanView plan;
+    int E, M, N;             // features of the M side; columns of the N side (kWeights)
+    int K;                   // summed extent (row stages)
+    int F;                   // kUp, kDownBackward: columns of act
+    bf16* out;               // kUp: act; kDown, kUpBackward, kWeights: the result; kDownBackward: grad_pre
+    bf16* pre;               // kUp: pre or null
+    const bf16* pre_in;      // kDownBackward (may be out)
     uint32_t* err_word;
 };
 
+constexpr int kProductThreads = 192;
+constexpr int kHalfBytes = 128 * kBlockK * 2;      // one operand of one CTA in a ring slot: 128 x 64 bf16
+constexpr int kSlotBytes = 2 * kHalfBytes;
+constexpr int kBoxBytes = 64 * kBlockK * 2;        // MN-major box: 64 values of M or N x 64 of k
+
 template <int kStage>
-__global__ void __launch_bounds__(256) ffn_rows_kernel(FfnArgs p)
+struct Shape {
+    static constexpr bool kWeightsStage = kStage == kWeights;
+    static constexpr bool kAMn = kStage == kDownBackward || kStage == kUpBackward || kStage == kWeights;
+    static constexpr int kRing = 6;
+    // epilogue staging, pitches an odd number of 16-byte units: the eight rows of a matrix fall into different banks
+    static constexpr int kPitch = kStage == kUp ? 144 : kStage == kDownBackward ? 528 : kStage == kWeights ? 144 : 272;
+    static constexpr int kPlanes = kStage == kUp ? 3 : 1;                     // act, gate, up
+    static constexpr int kBuffers = kStage == kUp || kStage == kDown || kStage == kUpBackward ? 2 : 1;
+    static constexpr int kStaging = kStage == kWeights ? 4 * 32 * kPitch : kBuffers * kPlanes * 32 * kPitch;
+    static constexpr int kBarriers = 256;
+    static constexpr int kSmem = kRing * kSlotBytes + kStaging + kBarriers;
+};
+
+struct Tile {
+    int expert, m0, n0, n;       // n: extent of the instruction's N (multiple of 32)
+    int row0, rows;              // row stages
+    int blocks;                  // 64-deep blocks of k
+};
+
+template <int kStage>
+__device__ __forceinline__ int count_tiles(const ProductArgs& p)
 {
-    __shared__ float sa[kTileK][kTile + 1], sb[kTileK][kTile + 1];
-    const int d = blockIdx.y, e = p.slot_expert[d];
-    int64_t first, last;
-    slot_rows(p.offsets, d, p.P, &first, &last);
-    if (blockIdx.x == 0 && threadIdx.x == 0 && (p.offsets[d + 1] < p.offsets[d] || p.offsets[d + 1] > p.P))
-        flag_error(p.err_word, COBALT_DEVERR_BAD_SLOT);
-    if (first == last) return;
-    if (e < 0 || e >= p.E) {
-        if (threadIdx.x == 0) flag_error(p.err_word, COBALT_DEVERR_BAD_SLOT);
-        return;
-    }
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    const int64_t H = p.H, F = p.F, n0 = static_cast<int64_t>(blockIdx.x) * kTile;
-    const bf16* wgu = p.w_gate_up + static_cast<int64_t>(e) * 2 * F * H;
-    const bf16* wd = p.w_down + static_cast<int64_t>(e) * H * F;
-    for (int64_t m0 = first; m0 < last; m0 += kTile) {
-        float acc[4][4] = {}, acc2[4][4] = {};
-        if (kStage == kUp) {
-            tile_product(p.rows, H, 1, m0, last, wgu, H, 1, n0, F, 0, H, sa, sb, acc);
-            tile_product(p.rows, H, 1, m0, last, wgu + F * H, H, 1, n0, F, 0, H, sa, sb, acc2);
-        } else if (kStage == kDown) {
-            tile_product(p.act_in, F, 1, m0, last, wd, F, 1, n0, H, 0, F, sa, sb, acc);
-        } else if (kStage == kDownBackward) {
-            tile_product(p.grad_out, H, 1, m0, last, wd, 1, F, n0, F, 0, H, sa, sb, acc);
-        } else {
-            tile_product(p.grad_pre, 2 * F, 1, m0, last, wgu, 1, H, n0, H, 0, 2 * F, sa, sb, acc);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int64_t r = m0 + 4 * ty + i, c = n0 + 4 * tx + j;
-                if (r >= last) continue;
-                if (kStage == kUp && c < F) {
-                    const float g = acc[i][j], u = acc2[i][j];
-                    p.act[r * F + c] = __float2bfloat16_rn(g / (1.0f + expf(-g)) * u);
-                    if (p.pre) {
-                        p.pre[r * 2 * F + c] = __float2bfloat16_rn(g);
-                        p.pre[r * 2 * F + F + c] = __float2bfloat16_rn(u);
-                    }
-                } else if (kStage == kDown && c < H) {
-                    p.out[r * H + c] = __float2bfloat16_rn(acc[i][j]);
-                } else if (kStage == kDownBackward && c < F) {
-                    const float g = __bfloat162float(p.pre_in[r * 2 * F + c]), u = __bfloat162float(p.pre_in[r * 2 * F + F + c]);
-                    const float s = 1.0f / (1.0f + expf(-g)), da = acc[i][j];
-                    p.grad_pre[r * 2 * F + c] = __float2bfloat16_rn(da * u * s * (1.0f + g * (1.0f - s)));
-                    p.grad_pre[r * 2 * F + F + c] = __float2bfloat16_rn(da * g * s);
-                } else if (kStage == kUpBackward && c < H) {
-                    p.grad_rows[r * H + c] = __float2bfloat16_rn(acc[i][j]);
-                }
-            }
-    }
+    const int mt = (p.M + kTileM - 1) / kTileM;
+    if (kStage == kWeights) return p.E * mt * ((p.N + kTileN - 1) / kTileN);
+    return *p.plan.row_tiles * mt;
 }
 
-// grad_w[e][m][n] = sum over the rows of e's slots of a[row][m] * b[row][n]
-__global__ void __launch_bounds__(256)
-ffn_weights_kernel(const bf16* a, int64_t M, const bf16* b, int64_t N, const uint32_t* offsets, const int32_t* slot_expert,
-                   int64_t P, int D, bf16* grad_w)
+template <int kStage>
+__device__ __forceinline__ Tile get_tile(const ProductArgs& p, int t)
 {
-    __shared__ float sa[kTileK][kTile + 1], sb[kTileK][kTile + 1];
-    const int e = blockIdx.z;
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    const int64_t m0 = static_cast<int64_t>(blockIdx.y) * kTile, n0 = static_cast<int64_t>(blockIdx.x) * kTile;
-    float acc[4][4] = {};
-    for (int d = 0; d < D; ++d) {
-        if (slot_expert[d] != e) continue;
-        int64_t first, last;
-        slot_rows(offsets, d, P, &first, &last);
-        tile_product(a, 1, M, m0, M, b, 1, N, n0, N, first, last, sa, sb, acc);
+    Tile r;
+    const int mt = (p.M + kTileM - 1) / kTileM;
+    if (kStage == kWeights) {
+        const int nt = (p.N + kTileN - 1) / kTileN;
+        r.expert = t / (mt * nt);
+        const int in = t - r.expert * mt * nt;
+        r.m0 = in / nt * kTileM;
+        r.n0 = in % nt * kTileN;
+        r.n = min(kTileN, (p.N - r.n0 + 31) / 32 * 32);
+        r.row0 = r.rows = 0;
+        r.blocks = p.plan.expert_blocks[r.expert];
+    } else {
+        // tiles of a slot lie together, its row tiles innermost: what runs at one time shares weights and rows in L2.
+        // All entries between a slot's first and last tile carry its first tile and count.
+        const int4 any = p.plan.tile[t / mt];
+        const int count = static_cast<int>(static_cast<uint32_t>(any.y) >> 9), in = t - any.w * mt;
+        const int4 own = p.plan.tile[any.w + in % count];
+        r.expert = own.z;
+        r.m0 = in / count * kTileM;
+        r.n0 = 0;
+        r.row0 = own.x;
+        r.rows = own.y & 511;
+        r.n = (r.rows + 31) / 32 * 32;
+        r.blocks = (p.K + kBlockK - 1) / kBlockK;
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (m0 + 4 * ty + i < M && n0 + 4 * tx + j < N)
-                grad_w[(static_cast<int64_t>(e) * M + m0 + 4 * ty + i) * N + n0 + 4 * tx + j] = __float2bfloat16_rn(acc[i][j]);
+    return r;
 }
+
+// Position in the ring: slot and the parity of its present use.
+struct Ring {
+    int slot = 0;
+    uint32_t phase = 0;
+    template <int kRing>
+    __device__ __forceinline__ void next()
+    {
+        if (++slot == kRing) {
+            slot = 0;
+            phase ^= 1;
+        }
+    }
+};
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi)
+{
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+__device__ __forceinline__ float low_half(uint32_t v) { return __uint_as_float(v << 16); }
+__device__ __forceinline__ float high_half(uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); }
+
+// 1 / (1 + exp(-g)): the fast exponential and division are good to a few units of fp32, far below the bf16 results
+__device__ __forceinline__ float sigmoid(float g) { return __fdividef(1.0f, 1.0f + __expf(-g)); }
+
+// Clears k rows valid .. 63 of this CTA's boxes in a ring slot (the loads brought rows of the next slot there).
+__device__ __forceinline__ void clear_tail(uint32_t slot_addr, int boxes_b, int valid, int lane)
+{
+    const int vectors = (kBlockK - valid) * 8;               // 16-byte vectors of a box
+    for (int b = 0; b < 2 + boxes_b; ++b) {
+        const uint32_t at = slot_addr + (b < 2 ? b * kBoxBytes : kHalfBytes + (b - 2) * kBoxBytes) + valid * 128;
+        for (int i = lane; i < vectors; i += 32) store_shared16(at + i * 16, make_uint4(0, 0, 0, 0));
+    }
+    fence_async_shared();
+    __syncwarp();
+}
+
+template <int kStage>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
+ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                   const __grid_constant__ CUtensorMap map_b_part, const __grid_constant__ ProductArgs p)
+{
+    typedef Shape<kStage> S;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const uint32_t base = smem_u32(smem);
+    const uint32_t staging = base + S::kRing * kSlotBytes;
+    const uint32_t bars = staging + S::kStaging;
+    const uint32_t full = bars, empty = bars + 8 * S::kRing, relay = bars + 16 * S::kRing;
+    const uint32_t acc_full = bars + 24 * S::kRing, acc_empty = acc_full + 16, drain = acc_full + 32, tmem_slot = acc_full + 40;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S::kRing; ++i) {
+            barrier_init(full + 8 * i, 1);       // this CTA's loads
+            barrier_init(empty + 8 * i, 1);      // the products that read the slot are done
+            barrier_init(relay + 8 * i, 1);      // leading CTA: the other CTA's loads
+        }
+        for (int i = 0; i < 2; ++i) {
+            barrier_init(acc_full + 8 * i, 1);
+            barrier_init(acc_empty + 8 * i, 8);  // leading CTA: four epilogue warps of each CTA
+        }
+        barrier_init(drain, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        prefetch_map(&map_a);
+        prefetch_map(&map_b);
+    }
+    if (warp == 1) tmem_alloc_pair(tmem_slot, 512);
+    tmem_fence_before();
+    cluster_sync();
+    tmem_fence_after();
+    uint32_t tmem;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot) : "memory");
+
+    const int tiles = count_tiles<kStage>(p);
+    const int first = blockIdx.x >> 1, step = gridDim.x >> 1;
+    bool ok = (base & 1023u) == 0;               // the swizzle counts from 1024-byte boundaries
+
+    if (warp == 0) {
+        // ---- loads of this CTA's halves --------------------------------------------------------------------
+        if (lane == 0) {
+            Ring ring;
+            int64_t issued = 0;
+            for (int t = first; t < tiles && ok; t += step) {
+                const Tile w = get_tile<kStage>(p, t);
+                const int half = w.n / 2, m0 = w.m0 + static_cast<int>(rank) * 128;
+                if (kStage == kWeights) {
+                    const int boxes_b = (half + 63) / 64, n0 = w.n0 + static_cast<int>(rank) * half;
+                    for (int s = p.plan.seg_start[w.expert], z = p.plan.seg_start[w.expert + 1]; s < z && ok; ++s) {
+                        const int2 seg = p.plan.segs[s];
+                        for (int r = 0; r < seg.y; r += kBlockK) {
+                            if (!(ok = barrier_wait(empty + 8 * ring.slot, ring.phase ^ 1))) break;
+                            const uint32_t bar = full + 8 * ring.slot, a = base + ring.slot * kSlotBytes;
+                            barrier_expect(bar, (2 + boxes_b) * kBoxBytes);
+                            for (int i = 0; i < 2; ++i) tma_load_2d(a + i * kBoxBytes, &map_a, bar, m0 + 64 * i, seg.x + r);
+                            for (int i = 0; i < boxes_b; ++i)
+                                tma_load_2d(a + kHalfBytes + i * kBoxBytes, &map_b, bar, n0 + 64 * i, seg.x + r);
+                            ring.next<S::kRing>();
+                            ++issued;
+                        }
+                    }
+                } else {
+                    const int row0 = w.row0 + static_cast<int>(rank) * half;
+                    for (int k = 0; k < w.blocks; ++k) {
+                        if (!(ok = barrier_wait(empty + 8 * ring.slot, ring.phase ^ 1))) break;
+                        const uint32_t bar = full + 8 * ring.slot, a = base + ring.slot * kSlotBytes, b = a + kHalfBytes;
+                        barrier_expect(bar, kHalfBytes + half * kBlockK * 2);
+                        if (kStage == kUp) tma_load_5d(a, &map_a, bar, k * kBlockK, 0, 0, m0 / 16, w.expert);
+                        if (kStage == kDown) tma_load_3d(a, &map_a, bar, k * kBlockK, m0, w.expert);
+                        if (S::kAMn)
+                            for (int i = 0; i < 2; ++i) tma_load_3d(a + i * kBoxBytes, &map_a, bar, m0 + 64 * i, k * kBlockK, w.expert);
+                        if (half == 128)
+                            tma_load_2d(b, &map_b, bar, k * kBlockK, row0);
+                        else
+                            for (int i = 0; i < half; i += 16) tma_load_2d(b + i * 128, &map_b_part, bar, k * kBlockK, row0 + i);
+                        ring.next<S::kRing>();
+                        ++issued;
+                    }
+                }
+            }
+            if (!ok) {
+                // the copies in flight have to land before this CTA's shared memory is given back
+                flag_error(p.err_word, COBALT_DEVERR_WAIT_TIMEOUT);
+                for (int64_t i = issued > S::kRing ? issued - S::kRing : 0; i < issued; ++i)
+                    (void)barrier_wait(full + 8 * static_cast<int>(i % S::kRing), static_cast<uint32_t>(i / S::kRing) & 1);
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        // ---- products (leading CTA); the other CTA passes on that its loads have landed -------------------------
+        Ring ring;
+        int turn = 0;                            // accumulators used so far
+        for (int t = first; t < tiles && ok; t += step) {
+            const Tile w = get_tile<kStage>(p, t);
+            if (w.blocks == 0) continue;
+            const int half = w.n / 2;
+            const uint32_t acc = turn & 1, d = tmem + acc * 256;
+            const uint32_t idesc = instruction_descriptor(w.n, S::kAMn, S::kWeightsStage);
+            if (rank == 0) {
+                if (!(ok = barrier_wait(acc_empty + 8 * acc, ((turn >> 1) & 1) ^ 1))) break;
+                tmem_fence_after();
+            }
+            int s = 0, z = 0, left = 0;
+            if (kStage == kWeights) {
+                s = p.plan.seg_start[w.expert];
+                z = p.plan.seg_start[w.expert + 1];
+                left = p.plan.segs[s].y;
+            }
+            for (int k = 0; k < w.blocks; ++k) {
+                if (!(ok = barrier_wait(full + 8 * ring.slot, ring.phase))) break;
+                const uint32_t a = base + ring.slot * kSlotBytes;
+                if (kStage == kWeights) {
+                    if (left < kBlockK) clear_tail(a, (half + 63) / 64, left, lane);
+                    left -= kBlockK;
+                    if (left <= 0 && ++s < z) left = p.plan.segs[s].y;
+                }
+                if (rank != 0) {
+                    if (lane == 0) barrier_arrive_cluster(peer_address(relay + 8 * ring.slot, 0));
+                } else {
+                    if (!(ok = barrier_wait(relay + 8 * ring.slot, ring.phase))) break;
+                    tmem_fence_after();
+                    if (lane == 0) {
+#pragma unroll
+                        for (int i = 0; i < kBlockK / 16; ++i) {
+                            // K-major: 16 values of k are 32 bytes further in the swizzled row; MN-major: two 8-row groups
+                            const uint64_t da = S::kAMn ? matrix_descriptor(a + i * 2048, kBoxBytes, 1024) : matrix_descriptor(a + i * 32, 16, 1024);
+                            const uint64_t db = S::kWeightsStage ? matrix_descriptor(a + kHalfBytes + i * 2048, kBoxBytes, 1024)
+                                                                 : matrix_descriptor(a + kHalfBytes + i * 32, 16, 1024);
+                            mma_pair(d, da, db, idesc, k > 0 || i > 0);
+                        }
+                        mma_commit_pair(empty + 8 * ring.slot);
+                    }
+                    __syncwarp();
+                }
+                ring.next<S::kRing>();
+            }
+            if (rank == 0 && ok && lane == 0) mma_commit_pair(acc_full + 8 * acc);
+            ++turn;
+        }
+        if (!ok && lane == 0) {
+            flag_error(p.err_word, COBALT_DEVERR_WAIT_TIMEOUT);
+            if (rank == 0) {                     // products in flight end before the tensor memory is freed
+                mma_commit_pair(drain);
+                (void)barrier_wait(drain, 0);
+            }
+        }
+        __syncwarp();
+    } else {
+        // ---- epilogue: quarter of the tensor memory lanes by warp, 32 accumulator columns at a time ---------------
+        const int quarter = warp & 3, tid = threadIdx.x - 64;
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(32 * quarter) << 16);
+        int turn = 0, chunk_turn = 0;
+        for (int t = first; t < tiles && ok; t += step) {
+            const Tile w = get_tile<kStage>(p, t);
+            const uint32_t acc = turn & 1;
+            if (w.blocks > 0) {
+                // one verdict for the four warps: none is left alone at the barriers below
+                ok = named_barrier_and(1, 128, barrier_wait(acc_full + 8 * acc, (turn >> 1) & 1));
+                if (!ok) break;
+                tmem_fence_after();
+            }
+            const int64_t F = p.F;
+            if (kStage == kUp) {
+                // TMEM lane 16 i + 8 j + l: gate (j = 0) or up (j = 1) feature 8 i + l, so both are in one thread
+                const int f0 = w.m0 / 2 + static_cast<int>(rank) * 64;
+                for (int c = 0; c < w.n; c += 32, ++chunk_turn) {
+                    const uint32_t buf = staging + (chunk_turn & 1) * (S::kPlanes * 32 * S::kPitch);
+#pragma unroll
+                    for (int hl = 0; hl < 2; ++hl) {
+                        uint32_t r[16], a[4], g[4], u[4];
+                        tmem_load_16x32(lanes + (static_cast<uint32_t>(16 * hl) << 16) + acc * 256 + c, r);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float g0 = __uint_as_float(r[4 * i]), g1 = __uint_as_float(r[4 * i + 1]);
+                            const float u0 = __uint_as_float(r[4 * i + 2]), u1 = __uint_as_float(r[4 * i + 3]);
+                            a[i] = pack2(g0 * sigmoid(g0) * u0, g1 * sigmoid(g1) * u1);
+                            g[i] = pack2(g0, g1);
+                            u[i] = pack2(u0, u1);
+                        }
+                        const uint32_t at = buf + lane * S::kPitch + (16 * quarter + 8 * hl) * 2;
+                        stmatrix_x4_trans(at, a[0], a[1], a[2], a[3]);
+                        if (p.pre) {
+                            stmatrix_x4_trans(at + 32 * S::kPitch, g[0], g[1], g[2], g[3]);
+                            stmatrix_x4_trans(at + 64 * S::kPitch, u[0], u[1], u[2], u[3]);
+                        }
+                    }
+                    named_barrier(1, 128);
+                    const int v = tid & 7, f = f0 + 8 * v;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int tok = i * 16 + (tid >> 3);
+                        if (c + tok < w.rows && f < F) {
+                            const int64_t row = w.row0 + c + tok;
+                            const uint32_t at = buf + tok * S::kPitch + v * 16;
+                            *reinterpret_cast<uint4*>(p.out + row * F + f) = load_shared16(at);
+                            if (p.pre) {
+                                *reinterpret_cast<uint4*>(p.pre + row * 2 * F + f) = load_shared16(at + 32 * S::kPitch);
+                                *reinterpret_cast<uint4*>(p.pre + row * 2 * F + F + f) = load_shared16(at + 64 * S::kPitch);
+                            }
+                        }
+                    }
+                }
+            } else if (kStage == kDown || kStage == kUpBackward) {
+                const int m0 = w.m0 + static_cast<int>(rank) * 128;
+                for (int c = 0; c < w.n; c += 32, ++chunk_turn) {
+                    const uint32_t buf = staging + (chunk_turn & 1) * (32 * S::kPitch);
+#pragma unroll
+                    for (int hl = 0; hl < 2; ++hl) {
+                        uint32_t r[16];
+                        tmem_load_16x32(lanes + (static_cast<uint32_t>(16 * hl) << 16) + acc * 256 + c, r);
+#pragma unroll
+                        for (int o = 0; o < 2; ++o) {
+                            uint32_t v[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                v[i] = pack2(__uint_as_float(r[4 * i + 2 * o]), __uint_as_float(r[4 * i + 2 * o + 1]));
+                            stmatrix_x4_trans(buf + lane * S::kPitch + (32 * quarter + 16 * hl + 8 * o) * 2, v[0], v[1], v[2], v[3]);
+                        }
+                    }
+                    named_barrier(1, 128);
+                    const int v = tid & 15, m = m0 + 8 * v;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int tok = i * 8 + (tid >> 4);
+                        if (c + tok < w.rows && m < p.M)
+                            *reinterpret_cast<uint4*>(p.out + static_cast<int64_t>(w.row0 + c + tok) * p.M + m) =
+                                load_shared16(buf + tok * S::kPitch + v * 16);
+                    }
+                }
+            } else if (kStage == kDownBackward) {
+                const int f0 = w.m0 + static_cast<int>(rank) * 128;
+                const int v = tid & 31, f = f0 + 8 * (v & 15);
+                const int64_t col = (v < 16 ? 0 : F) + f;
+                for (int c = 0; c < w.n; c += 32) {
+                    // gate and up of the chunk come in by rows; each thread reads and later overwrites the same vectors
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int tok = i * 4 + (tid >> 5);
+                        uint4 x = make_uint4(0, 0, 0, 0);
+                        if (c + tok < w.rows && f < F) x = ld_once16(p.pre_in + static_cast<int64_t>(w.row0 + c + tok) * 2 * F + col);
+                        store_shared16(staging + tok * S::kPitch + v * 16, x);
+                    }
+                    named_barrier(1, 128);
+#pragma unroll
+                    for (int hl = 0; hl < 2; ++hl) {
+                        uint32_t r[16];
+                        tmem_load_16x32(lanes + (static_cast<uint32_t>(16 * hl) << 16) + acc * 256 + c, r);
+#pragma unroll
+                        for (int o = 0; o < 2; ++o) {
+                            const uint32_t at = staging + lane * S::kPitch + (32 * quarter + 16 * hl + 8 * o) * 2;
+                            uint32_t gv[4], uv[4];
+                            ldmatrix_x4_trans(at, gv);
+                            ldmatrix_x4_trans(at + 256, uv);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float g0 = low_half(gv[i]), g1 = high_half(gv[i]), u0 = low_half(uv[i]), u1 = high_half(uv[i]);
+                                const float d0 = __uint_as_float(r[4 * i + 2 * o]), d1 = __uint_as_float(r[4 * i + 2 * o + 1]);
+                                const float s0 = sigmoid(g0), s1 = sigmoid(g1);
+                                gv[i] = pack2(d0 * u0 * s0 * (1.0f + g0 * (1.0f - s0)), d1 * u1 * s1 * (1.0f + g1 * (1.0f - s1)));
+                                uv[i] = pack2(d0 * g0 * s0, d1 * g1 * s1);
+                            }
+                            stmatrix_x4_trans(at, gv[0], gv[1], gv[2], gv[3]);
+                            stmatrix_x4_trans(at + 256, uv[0], uv[1], uv[2], uv[3]);
+                        }
+                    }
+                    named_barrier(1, 128);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int tok = i * 4 + (tid >> 5);
+                        if (c + tok < w.rows && f < F)
+                            st_stream16(p.out + static_cast<int64_t>(w.row0 + c + tok) * 2 * F + col,
+                                        load_shared16(staging + tok * S::kPitch + v * 16));
+                    }
+                }
+            } else {
+                // weight gradients: TMEM lanes are rows of the result, columns its columns; a warp is on its own
+                const int m0 = w.m0 + static_cast<int>(rank) * 128 + 32 * quarter;
+                const uint32_t buf = staging + quarter * 32 * S::kPitch;
+                bf16* out = p.out + static_cast<int64_t>(w.expert) * p.M * p.N;
+                for (int c = 0; c < w.n; c += 64) {
+                    const int parts = min(2, (w.n - c) / 32);
+#pragma unroll
+                    for (int hl = 0; hl < 2; ++hl)
+                        for (int q = 0; q < parts; ++q) {
+                            uint32_t r[16] = {};
+                            if (w.blocks > 0) {
+                                tmem_load_16x32(lanes + (static_cast<uint32_t>(16 * hl) << 16) + acc * 256 + c + 32 * q, r);
+                                    }
+#pragma unroll
+                            for (int o = 0; o < 2; ++o) {
+                                uint32_t v[4];
+#pragma unroll
+                                for (int i = 0; i < 4; ++i)
+                                    v[i] = pack2(__uint_as_float(r[4 * i + 2 * o]), __uint_as_float(r[4 * i + 2 * o + 1]));
+                                stmatrix_x4(buf + (16 * hl + 8 * o + (lane & 7)) * S::kPitch + (32 * q + 8 * (lane >> 3)) * 2, v[0], v[1], v[2],
+                                            v[3]);
+                            }
+                        }
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int m = i * 4 + (lane >> 3), n = w.n0 + c + 8 * (lane & 7);
+                        if (m0 + m < p.M && n < p.N && 8 * (lane & 7) < 32 * parts)
+                            st_stream16(out + static_cast<int64_t>(m0 + m) * p.N + n, load_shared16(buf + m * S::kPitch + (lane & 7) * 16));
+                    }
+                    __syncwarp();
+                }
+            }
+            if (w.blocks > 0) {
+                tmem_fence_before();
+                __syncwarp();
+                if (lane == 0) barrier_arrive_cluster(peer_address(acc_empty + 8 * acc, 0));
+                ++turn;
+            }
+        }
+        if (!ok && lane == 0) flag_error(p.err_word, COBALT_DEVERR_WAIT_TIMEOUT);
+        __syncwarp();
+    }
+    tmem_fence_before();
+    cluster_sync();                              // no CTA leaves while the other may still reach its barriers
+    tmem_fence_after();
+    if (warp == 1) tmem_free_pair(tmem, 512);
+}
+
+// ---- host side ----------------------------------------------------------------------------------------------------
+
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+static int encode_function(EncodeTiled* out)
+{
+    static EncodeTiled cached = nullptr;         // the same for every device; a race writes the same value
+    if (!cached) {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        COBALT_CUDA_TRY(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found));
+        if (found != cudaDriverEntryPointSuccess || !f) return COBALT_ERR_UNSUPPORTED;
+        cached = reinterpret_cast<EncodeTiled>(f);
+    }
+    *out = cached;
+    return COBALT_OK;
+}
+
+// A bf16 tensor of up to five dimensions, the first one contiguous; strides of the others in elements.
+static int make_map(CUtensorMap* map, const void* ptr, int rank, const uint64_t (&dim)[5], const uint64_t (&stride)[5], const uint32_t (&box)[5])
+{
+    EncodeTiled encode;
+    const int rc = encode_function(&encode);
+    if (rc != COBALT_OK) return rc;
+    cuuint64_t dims[5], bytes[4];
+    cuuint32_t boxes[5], ones[5] = {1, 1, 1, 1, 1};
+    for (int i = 0; i < rank; ++i) {
+        dims[i] = dim[i];
+        boxes[i] = box[i];
+        if (i > 0) bytes[i - 1] = stride[i] * 2;
+    }
+    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(ptr), dims, bytes, boxes, ones,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? COBALT_OK : record_cuda_error(cudaErrorInvalidValue);
+}
+
+static int rows_map(CUtensorMap* map, const void* ptr, int64_t rows, int64_t columns, uint32_t box_rows)
+{
+    const uint64_t dim[5] = {static_cast<uint64_t>(columns), static_cast<uint64_t>(rows)}, stride[5] = {1, static_cast<uint64_t>(columns)};
+    const uint32_t box[5] = {kBlockK, box_rows};
+    return make_map(map, ptr, 2, dim, stride, box);
+}
+
+static int weights_map(CUtensorMap* map, const void* ptr, int64_t E, int64_t rows, int64_t columns, uint32_t box_rows)
+{
+    const uint64_t dim[5] = {static_cast<uint64_t>(columns), static_cast<uint64_t>(rows), static_cast<uint64_t>(E)};
+    const uint64_t stride[5] = {1, static_cast<uint64_t>(columns), static_cast<uint64_t>(rows * columns)};
+    const uint32_t box[5] = {kBlockK, box_rows, 1};
+    return make_map(map, ptr, 3, dim, stride, box);
+}
+
+// w_gate_up [E][2][F][H] read so that a box of 128 rows is eight gate rows, eight up rows, the next eight gate rows ...
+static int gate_up_map(CUtensorMap* map, const void* ptr, int64_t E, int64_t F, int64_t H)
+{
+    const uint64_t h = H, f = F;
+    const uint64_t dim[5] = {h, 8, 2, f / 8, static_cast<uint64_t>(E)}, stride[5] = {1, h, f * h, 8 * h, 2 * f * h};
+    const uint32_t box[5] = {kBlockK, 8, 2, 8, 1};
+    return make_map(map, ptr, 5, dim, stride, box);
+}
+
+template <int kStage>
+static int launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& b_part, const ProductArgs& p, int64_t max_tiles,
+                          cudaStream_t s)
+{
+    const void* kernel = reinterpret_cast<const void*>(ffn_product_kernel<kStage>);
+    int rc = ensure_kernel_attributes(kernel, Shape<kStage>::kSmem, false);
+    if (rc != COBALT_OK) return rc;
+    int sms = 0;
+    rc = sm_count(&sms);
+    if (rc != COBALT_OK) return rc;
+    const int64_t pairs = max_tiles < sms / 2 ? max_tiles : sms / 2;
+    ffn_product_kernel<kStage><<<static_cast<unsigned>(2 * (pairs < 1 ? 1 : pairs)), kProductThreads, Shape<kStage>::kSmem, s>>>(a, b, b_part, p);
+    COBALT_CUDA_TRY(cudaGetLastError());
+    return COBALT_OK;
+}
+
+static int launch_plan(const uint32_t* offsets, const int32_t* slot_expert, int64_t P, int D, const ProductArgs& p, bool with_experts,
+                       cudaStream_t s)
+{
+    const size_t bytes = 16 * static_cast<size_t>(D);
+    // the attribute is set to the most that any call needs, so that concurrent calls agree on it
+    const int rc = ensure_kernel_attributes(reinterpret_cast<const void*>(ffn_plan_kernel), 16 * COBALT_MAX_DESTS, false);
+    if (rc != COBALT_OK) return rc;
+    ffn_plan_kernel<<<1, kPlanThreads, bytes, s>>>(offsets, slot_expert, P, D, p.E, p.plan, with_experts, p.err_word);
+    COBALT_CUDA_TRY(cudaGetLastError());
+    return COBALT_OK;
+}
+
+static int64_t m_tiles(int64_t features) { return (features + kTileM - 1) / kTileM; }
 
 static int check_ffn(int64_t P, int32_t D, int32_t E, int32_t H, int32_t F)
 {
@@ -151,7 +714,11 @@ static int check_ffn(int64_t P, int32_t D, int32_t E, int32_t H, int32_t F)
     return COBALT_OK;
 }
 
-static unsigned tiles(int64_t n) { return static_cast<unsigned>((n + kTile - 1) / kTile); }
+#define COBALT_TRY(expr)                       \
+    do {                                       \
+        const int cobalt_rc__ = (expr);        \
+        if (cobalt_rc__ != COBALT_OK) return cobalt_rc__; \
+    } while (0)
 
 }  // namespace cobalt
 
@@ -162,42 +729,55 @@ extern "C" {
 size_t cobalt_expert_ffn_workspace_bytes(int64_t P, int32_t D, int32_t E, int32_t H, int32_t F)
 {
     if (check_ffn(P, D, E, H, F) != COBALT_OK) return 0;
-    return 256;
+    return plan_bytes(P, D, E);
 }
 
-int cobalt_expert_ffn(const void* rows, const uint32_t* dest_offsets, const int32_t* slot_expert, int64_t P, int32_t D,
-                      int32_t E, int32_t H, int32_t F, const void* w_gate_up, const void* w_down, void* act, void* pre,
-                      void* out, void* workspace, size_t workspace_bytes, cobalt_stream_t stream)
+int cobalt_expert_ffn(const void* rows, const uint32_t* dest_offsets, const int32_t* slot_expert, int64_t P, int32_t D, int32_t E,
+                      int32_t H, int32_t F, const void* w_gate_up, const void* w_down, void* act, void* pre, void* out, void* workspace,
+                      size_t workspace_bytes, cobalt_stream_t stream)
 {
-    int rc = check_ffn(P, D, E, H, F);
-    if (rc != COBALT_OK) return rc;
+    COBALT_TRY(check_ffn(P, D, E, H, F));
     if (P == 0) return COBALT_OK;
     if (!rows || !dest_offsets || !slot_expert || !w_gate_up || !w_down || !act || !out) return COBALT_ERR_INVALID_ARG;
     if (!aligned16(rows) || !aligned16(dest_offsets) || !aligned16(slot_expert) || !aligned16(w_gate_up) || !aligned16(w_down) ||
         !aligned16(act) || !aligned16(pre) || !aligned16(out) || !aligned16(workspace))
         return COBALT_ERR_INVALID_ARG;
-    if (!workspace || workspace_bytes < cobalt_expert_ffn_workspace_bytes(P, D, E, H, F)) return COBALT_ERR_WORKSPACE_TOO_SMALL;
-    FfnArgs p = {};
-    rc = device_error_word(&p.err_word);
-    if (rc != COBALT_OK) return rc;
-    p.rows = static_cast<const bf16*>(rows); p.w_gate_up = static_cast<const bf16*>(w_gate_up);
-    p.w_down = static_cast<const bf16*>(w_down); p.act = static_cast<bf16*>(act); p.act_in = p.act;
-    p.pre = static_cast<bf16*>(pre); p.out = static_cast<bf16*>(out);
-    p.offsets = dest_offsets; p.slot_expert = slot_expert; p.P = P; p.D = D; p.E = E; p.H = H; p.F = F;
+    if (!workspace || workspace_bytes < plan_bytes(P, D, E)) return COBALT_ERR_WORKSPACE_TOO_SMALL;
+    ProductArgs p = {};
+    COBALT_TRY(device_error_word(&p.err_word));
+    p.plan = plan_view(workspace, P, D, E);
+    p.E = E;
+    p.F = F;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    ffn_rows_kernel<kUp><<<dim3(tiles(F), D), 256, 0, s>>>(p);
-    ffn_rows_kernel<kDown><<<dim3(tiles(H), D), 256, 0, s>>>(p);
-    COBALT_CUDA_TRY(cudaGetLastError());
-    return COBALT_OK;
+    const int64_t row_tiles = max_row_tiles(P, static_cast<int>(P < D ? P : D));
+
+    CUtensorMap a, b, part;
+    COBALT_TRY(gate_up_map(&a, w_gate_up, E, F, H));
+    COBALT_TRY(rows_map(&b, rows, P, H, 128));
+    COBALT_TRY(rows_map(&part, rows, P, H, 16));
+    CUtensorMap a2, b2, part2;
+    COBALT_TRY(weights_map(&a2, w_down, E, H, F, 128));
+    COBALT_TRY(rows_map(&b2, act, P, F, 128));
+    COBALT_TRY(rows_map(&part2, act, P, F, 16));
+
+    COBALT_TRY(launch_plan(dest_offsets, slot_expert, P, D, p, false, s));
+    p.M = 2 * F;
+    p.K = H;
+    p.out = static_cast<bf16*>(act);
+    p.pre = static_cast<bf16*>(pre);
+    COBALT_TRY(launch_product<kUp>(a, b, part, p, row_tiles * m_tiles(p.M), s));
+    p.M = H;
+    p.K = F;
+    p.out = static_cast<bf16*>(out);
+    return launch_product<kDown>(a2, b2, part2, p, row_tiles * m_tiles(p.M), s);
 }
 
-int cobalt_expert_ffn_backward(const void* grad_out, const void* rows, const uint32_t* dest_offsets, const int32_t* slot_expert,
-                               int64_t P, int32_t D, int32_t E, int32_t H, int32_t F, const void* w_gate_up, const void* w_down,
-                               const void* pre, const void* act, void* grad_pre, void* grad_rows, void* grad_w_gate_up,
-                               void* grad_w_down, void* workspace, size_t workspace_bytes, cobalt_stream_t stream)
+int cobalt_expert_ffn_backward(const void* grad_out, const void* rows, const uint32_t* dest_offsets, const int32_t* slot_expert, int64_t P,
+                               int32_t D, int32_t E, int32_t H, int32_t F, const void* w_gate_up, const void* w_down, const void* pre,
+                               const void* act, void* grad_pre, void* grad_rows, void* grad_w_gate_up, void* grad_w_down, void* workspace,
+                               size_t workspace_bytes, cobalt_stream_t stream)
 {
-    int rc = check_ffn(P, D, E, H, F);
-    if (rc != COBALT_OK) return rc;
+    COBALT_TRY(check_ffn(P, D, E, H, F));
     if (!dest_offsets || !slot_expert) return COBALT_ERR_INVALID_ARG;
     if (!grad_rows && !grad_w_gate_up && !grad_w_down) return COBALT_ERR_INVALID_ARG;
     if (P > 0 && (!grad_out || !rows || !w_gate_up || !w_down || !pre || !act || !grad_pre)) return COBALT_ERR_INVALID_ARG;
@@ -205,27 +785,58 @@ int cobalt_expert_ffn_backward(const void* grad_out, const void* rows, const uin
         !aligned16(w_down) || !aligned16(pre) || !aligned16(act) || !aligned16(grad_pre) || !aligned16(grad_rows) ||
         !aligned16(grad_w_gate_up) || !aligned16(grad_w_down) || !aligned16(workspace))
         return COBALT_ERR_INVALID_ARG;
-    if (!workspace || workspace_bytes < cobalt_expert_ffn_workspace_bytes(P, D, E, H, F)) return COBALT_ERR_WORKSPACE_TOO_SMALL;
-    FfnArgs p = {};
-    rc = device_error_word(&p.err_word);
-    if (rc != COBALT_OK) return rc;
-    p.rows = static_cast<const bf16*>(rows); p.w_gate_up = static_cast<const bf16*>(w_gate_up);
-    p.w_down = static_cast<const bf16*>(w_down); p.grad_out = static_cast<const bf16*>(grad_out);
-    p.pre_in = static_cast<const bf16*>(pre); p.act_in = static_cast<const bf16*>(act);
-    p.grad_pre = static_cast<bf16*>(grad_pre); p.grad_rows = static_cast<bf16*>(grad_rows);
-    p.offsets = dest_offsets; p.slot_expert = slot_expert; p.P = P; p.D = D; p.E = E; p.H = H; p.F = F;
+    if (!workspace || workspace_bytes < plan_bytes(P, D, E)) return COBALT_ERR_WORKSPACE_TOO_SMALL;
+    ProductArgs p = {};
+    COBALT_TRY(device_error_word(&p.err_word));
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (P > 0 && (grad_rows || grad_w_gate_up)) {
-        ffn_rows_kernel<kDownBackward><<<dim3(tiles(F), D), 256, 0, s>>>(p);
-        if (grad_rows) ffn_rows_kernel<kUpBackward><<<dim3(tiles(H), D), 256, 0, s>>>(p);
+    if (P == 0) {                                // no rows: the weights' gradients are 0
+        const size_t bytes = static_cast<size_t>(E) * H * F * sizeof(bf16);
+        if (grad_w_gate_up) COBALT_CUDA_TRY(cudaMemsetAsync(grad_w_gate_up, 0, 2 * bytes, s));
+        if (grad_w_down) COBALT_CUDA_TRY(cudaMemsetAsync(grad_w_down, 0, bytes, s));
+        return COBALT_OK;
     }
-    if (grad_w_gate_up)
-        ffn_weights_kernel<<<dim3(tiles(H), tiles(2 * static_cast<int64_t>(F)), E), 256, 0, s>>>(
-            p.grad_pre, 2 * static_cast<int64_t>(F), p.rows, H, dest_offsets, slot_expert, P, D, static_cast<bf16*>(grad_w_gate_up));
-    if (grad_w_down)
-        ffn_weights_kernel<<<dim3(tiles(F), tiles(H), E), 256, 0, s>>>(p.grad_out, H, p.act_in, F, dest_offsets, slot_expert, P, D,
-                                                                       static_cast<bf16*>(grad_w_down));
-    COBALT_CUDA_TRY(cudaGetLastError());
+    p.plan = plan_view(workspace, P, D, E);
+    p.E = E;
+    p.F = F;
+    const int64_t row_tiles = max_row_tiles(P, static_cast<int>(P < D ? P : D));
+    CUtensorMap a, b, part;
+    const bool weights = grad_w_gate_up || grad_w_down;
+    COBALT_TRY(launch_plan(dest_offsets, slot_expert, P, D, p, weights, s));
+    if (grad_rows || grad_w_gate_up) {
+        COBALT_TRY(weights_map(&a, w_down, E, H, F, kBlockK));
+        COBALT_TRY(rows_map(&b, grad_out, P, H, 128));
+        COBALT_TRY(rows_map(&part, grad_out, P, H, 16));
+        p.M = F;
+        p.K = H;
+        p.pre_in = static_cast<const bf16*>(pre);
+        p.out = static_cast<bf16*>(grad_pre);
+        COBALT_TRY(launch_product<kDownBackward>(a, b, part, p, row_tiles * m_tiles(p.M), s));
+    }
+    if (grad_rows) {
+        COBALT_TRY(weights_map(&a, w_gate_up, E, 2 * static_cast<int64_t>(F), H, kBlockK));
+        COBALT_TRY(rows_map(&b, grad_pre, P, 2 * static_cast<int64_t>(F), 128));
+        COBALT_TRY(rows_map(&part, grad_pre, P, 2 * static_cast<int64_t>(F), 16));
+        p.M = H;
+        p.K = 2 * F;
+        p.out = static_cast<bf16*>(grad_rows);
+        COBALT_TRY(launch_product<kUpBackward>(a, b, part, p, row_tiles * m_tiles(p.M), s));
+    }
+    if (grad_w_gate_up) {
+        COBALT_TRY(rows_map(&a, grad_pre, P, 2 * static_cast<int64_t>(F), kBlockK));
+        COBALT_TRY(rows_map(&b, rows, P, H, kBlockK));
+        p.M = 2 * F;
+        p.N = H;
+        p.out = static_cast<bf16*>(grad_w_gate_up);
+        COBALT_TRY(launch_product<kWeights>(a, b, b, p, E * m_tiles(p.M) * m_tiles(p.N), s));
+    }
+    if (grad_w_down) {
+        COBALT_TRY(rows_map(&a, grad_out, P, H, kBlockK));
+        COBALT_TRY(rows_map(&b, act, P, F, kBlockK));
+        p.M = H;
+        p.N = F;
+        p.out = static_cast<bf16*>(grad_w_down);
+        COBALT_TRY(launch_product<kWeights>(a, b, b, p, E * m_tiles(p.M) * m_tiles(p.N), s));
+    }
     return COBALT_OK;
 }
 
