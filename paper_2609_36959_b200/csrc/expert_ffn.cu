@@ -283,6 +283,7 @@ __device__ __forceinline__ void clear_tail(uint32_t slot_addr, int boxes_b, int 
         for (int i = lane; i < vectors; i += 32) store_shared16(at + i * 16, make_uint4(0, 0, 0, 0));
     }
     fence_async_shared();
+    fence_cluster();                                          // the leading CTA issues the products that read them
     __syncwarp();
 }
 
