@@ -299,7 +299,7 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     const uint32_t bars = staging + S::kStaging;
     const uint32_t full = bars, empty = bars + 8 * S::kRing, relay = bars + 16 * S::kRing;
     const uint32_t acc_full = bars + 24 * S::kRing, acc_empty = acc_full + 16, drain = acc_full + 32, tmem_slot = acc_full + 40;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
 
     if (threadIdx.x == 0) {
@@ -330,52 +330,59 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 
     if (warp == 0) {
         // ---- loads of this CTA's halves --------------------------------------------------------------------
-        if (lane == 0) {
-            Ring ring;
-            int64_t issued = 0;
-            for (int t = first; t < tiles && ok; t += step) {
-                const Tile w = get_tile<kStage>(p, t);
-                const int half = w.n / 2, m0 = w.m0 + static_cast<int>(rank) * 128;
-                if (kStage == kWeights) {
-                    const int boxes_b = (half + 63) / 64, n0 = w.n0 + static_cast<int>(rank) * half;
-                    for (int s = p.plan.seg_start[w.expert], z = p.plan.seg_start[w.expert + 1]; s < z && ok; ++s) {
-                        const int2 seg = p.plan.segs[s];
-                        for (int r = 0; r < seg.y; r += kBlockK) {
-                            if (!(ok = barrier_wait(empty + 8 * ring.slot, ring.phase ^ 1))) break;
-                            const uint32_t bar = full + 8 * ring.slot, a = base + ring.slot * kSlotBytes;
-                            barrier_expect(bar, (2 + boxes_b) * kBoxBytes);
-                            for (int i = 0; i < 2; ++i) tma_load_2d(a + i * kBoxBytes, &map_a, bar, m0 + 64 * i, seg.x + r);
-                            for (int i = 0; i < boxes_b; ++i)
-                                tma_load_2d(a + kHalfBytes + i * kBoxBytes, &map_b, bar, n0 + 64 * i, seg.x + r);
-                            ring.next<S::kRing>();
-                            ++issued;
-                        }
-                    }
-                } else {
-                    const int row0 = w.row0 + static_cast<int>(rank) * half;
-                    for (int k = 0; k < w.blocks; ++k) {
+        Ring ring;
+        int64_t issued = 0;
+        for (int t = first; t < tiles && ok; t += step) {
+            const Tile w = get_tile<kStage>(p, t);
+            const int half = w.n / 2, m0 = w.m0 + static_cast<int>(rank) * 128;
+            if (kStage == kWeights) {
+                const int boxes_b = (half + 63) / 64, n0 = w.n0 + static_cast<int>(rank) * half;
+                for (int s = p.plan.seg_start[w.expert], z = p.plan.seg_start[w.expert + 1]; s < z && ok; ++s) {
+                    const int2 seg = p.plan.segs[s];
+                    for (int r = 0; r < seg.y; r += kBlockK) {
                         if (!(ok = barrier_wait(empty + 8 * ring.slot, ring.phase ^ 1))) break;
-                        const uint32_t bar = full + 8 * ring.slot, a = base + ring.slot * kSlotBytes, b = a + kHalfBytes;
-                        barrier_expect(bar, kHalfBytes + half * kBlockK * 2);
-                        if (kStage == kUp) tma_load_5d(a, &map_a, bar, k * kBlockK, 0, 0, m0 / 16, w.expert);
-                        if (kStage == kDown) tma_load_3d(a, &map_a, bar, k * kBlockK, m0, w.expert);
-                        if (S::kAMn)
-                            for (int i = 0; i < 2; ++i) tma_load_3d(a + i * kBoxBytes, &map_a, bar, m0 + 64 * i, k * kBlockK, w.expert);
-                        if (half == 128)
-                            tma_load_2d(b, &map_b, bar, k * kBlockK, row0);
-                        else
-                            for (int i = 0; i < half; i += 16) tma_load_2d(b + i * 128, &map_b_part, bar, k * kBlockK, row0 + i);
+                        const uint32_t bar = full + 8 * ring.slot, a = base + ring.slot * kSlotBytes;
+                        if (elect_one()) {
+                            barrier_expect(bar, (2 + boxes_b) * kBoxBytes);
+                            tma_load_2d(a, &map_a, bar, m0, seg.x + r);
+                            tma_load_2d(a + kBoxBytes, &map_a, bar, m0 + 64, seg.x + r);
+                            tma_load_2d(a + kHalfBytes, &map_b, bar, n0, seg.x + r);
+                            if (boxes_b > 1) tma_load_2d(a + kHalfBytes + kBoxBytes, &map_b, bar, n0 + 64, seg.x + r);
+                        }
+                        __syncwarp();
                         ring.next<S::kRing>();
                         ++issued;
                     }
                 }
+            } else {
+                const int row0 = w.row0 + static_cast<int>(rank) * half;
+                for (int k = 0; k < w.blocks; ++k) {
+                    if (!(ok = barrier_wait(empty + 8 * ring.slot, ring.phase ^ 1))) break;
+                    const uint32_t bar = full + 8 * ring.slot, a = base + ring.slot * kSlotBytes, b = a + kHalfBytes;
+                    if (elect_one()) {
+                        barrier_expect(bar, kHalfBytes + half * kBlockK * 2);
+                        if (kStage == kUp) tma_load_5d(a, &map_a, bar, k * kBlockK, 0, 0, m0 / 16, w.expert);
+                        if (kStage == kDown) tma_load_3d(a, &map_a, bar, k * kBlockK, m0, w.expert);
+                        if (S::kAMn) {
+                            tma_load_3d(a, &map_a, bar, m0, k * kBlockK, w.expert);
+                            tma_load_3d(a + kBoxBytes, &map_a, bar, m0 + 64, k * kBlockK, w.expert);
+                        }
+                        if (half == 128)
+                            tma_load_2d(b, &map_b, bar, k * kBlockK, row0);
+                        else
+                            for (int i = 0; i < half; i += 16) tma_load_2d(b + i * 128, &map_b_part, bar, k * kBlockK, row0 + i);
+                    }
+                    __syncwarp();
+                    ring.next<S::kRing>();
+                    ++issued;
+                }
             }
-            if (!ok) {
-                // the copies in flight have to land before this CTA's shared memory is given back
-                flag_error(p.err_word, COBALT_DEVERR_WAIT_TIMEOUT);
-                for (int64_t i = issued > S::kRing ? issued - S::kRing : 0; i < issued; ++i)
-                    (void)barrier_wait(full + 8 * static_cast<int>(i % S::kRing), static_cast<uint32_t>(i / S::kRing) & 1);
-            }
+        }
+        if (!ok) {
+            // the copies in flight have to land before this CTA's shared memory is given back
+            if (lane == 0) flag_error(p.err_word, COBALT_DEVERR_WAIT_TIMEOUT);
+            for (int64_t i = issued > S::kRing ? issued - S::kRing : 0; i < issued; ++i)
+                (void)barrier_wait(full + 8 * static_cast<int>(i % S::kRing), static_cast<uint32_t>(i / S::kRing) & 1);
         }
         __syncwarp();
     } else if (warp == 1) {
@@ -407,32 +414,35 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                     if (left <= 0 && ++s < z) left = p.plan.segs[s].y;
                 }
                 if (rank != 0) {
-                    if (lane == 0) barrier_arrive_cluster(peer_address(relay + 8 * ring.slot, 0));
+                    if (elect_one()) barrier_arrive_cluster(peer_address(relay + 8 * ring.slot, 0));
+                    __syncwarp();
                 } else {
                     if (!(ok = barrier_wait(relay + 8 * ring.slot, ring.phase))) break;
                     tmem_fence_after();
-                    if (lane == 0) {
+                    if (elect_one()) {
+                        // K-major: 16 values of k are 32 bytes further in the swizzled row; MN-major: two 8-row groups
+                        const uint64_t da = S::kAMn ? matrix_descriptor(a, kBoxBytes, 1024) : matrix_descriptor(a, 16, 1024);
+                        const uint64_t db = S::kWeightsStage ? matrix_descriptor(a + kHalfBytes, kBoxBytes, 1024)
+                                                             : matrix_descriptor(a + kHalfBytes, 16, 1024);
+                        constexpr uint32_t step_a = (S::kAMn ? 2048 : 32) >> 4, step_b = (S::kWeightsStage ? 2048 : 32) >> 4;
 #pragma unroll
-                        for (int i = 0; i < kBlockK / 16; ++i) {
-                            // K-major: 16 values of k are 32 bytes further in the swizzled row; MN-major: two 8-row groups
-                            const uint64_t da = S::kAMn ? matrix_descriptor(a + i * 2048, kBoxBytes, 1024) : matrix_descriptor(a + i * 32, 16, 1024);
-                            const uint64_t db = S::kWeightsStage ? matrix_descriptor(a + kHalfBytes + i * 2048, kBoxBytes, 1024)
-                                                                 : matrix_descriptor(a + kHalfBytes + i * 32, 16, 1024);
-                            mma_pair(d, da, db, idesc, k > 0 || i > 0);
-                        }
+                        for (uint32_t i = 0; i < kBlockK / 16; ++i) mma_pair(d, da + i * step_a, db + i * step_b, idesc, k > 0 || i > 0);
                         mma_commit_pair(empty + 8 * ring.slot);
                     }
                     __syncwarp();
                 }
                 ring.next<S::kRing>();
             }
-            if (rank == 0 && ok && lane == 0) mma_commit_pair(acc_full + 8 * acc);
+            if (rank == 0 && ok) {
+                if (elect_one()) mma_commit_pair(acc_full + 8 * acc);
+                __syncwarp();
+            }
             ++turn;
         }
-        if (!ok && lane == 0) {
-            flag_error(p.err_word, COBALT_DEVERR_WAIT_TIMEOUT);
+        if (!ok) {
+            if (lane == 0) flag_error(p.err_word, COBALT_DEVERR_WAIT_TIMEOUT);
             if (rank == 0) {                     // products in flight end before the tensor memory is freed
-                mma_commit_pair(drain);
+                if (elect_one()) mma_commit_pair(drain);
                 (void)barrier_wait(drain, 0);
             }
         }

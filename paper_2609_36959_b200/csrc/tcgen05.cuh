@@ -12,6 +12,16 @@ namespace cobalt {
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 
+// One lane of the warp, the same one every time.  The compiler knows that a branch on it holds for one thread and
+// keeps the operands of tensor-core and copy instructions in uniform registers; behind `lane == 0` it re-broadcast
+// them for every instruction (about 90 cycles each).
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+
 __device__ __forceinline__ uint32_t cluster_rank()
 {
     uint32_t r;
@@ -66,19 +76,15 @@ __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity)
     return done != 0;
 }
 
-// Waits for a phase of an mbarrier, two seconds at most; false if they ran out.
+// Waits for a phase of an mbarrier, 2^32 cycles (two to three seconds) at most; false if they ran out.
 __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity)
 {
     if (barrier_try(bar, parity)) return true;
-    uint64_t start, now;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(start));
-    while (true) {
-#pragma unroll 1
-        for (int i = 0; i < 64; ++i)
-            if (barrier_try(bar, parity)) return true;
-        asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
-        if (now - start > 2000000000ull) return false;
-    }
+    const long long start = clock64();       // (the global timer is far slower to read, and this is the ring's path)
+    do {
+        if (barrier_try(bar, parity)) return true;
+    } while (clock64() - start < (1ll << 32));
+    return false;
 }
 
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y)
