@@ -53,6 +53,66 @@ struct Vec16<float> {
     }
 };
 
+// Two fp32 values in a register pair: sm_100 adds, multiplies and fuses both with one instruction (PTX .f32x2).
+struct Pair {
+    float2 v;
+};
+
+__device__ __forceinline__ Pair pair(float a, float b) { return Pair{make_float2(a, b)}; }
+__device__ __forceinline__ Pair pair(float a) { return Pair{make_float2(a, a)}; }
+__device__ __forceinline__ uint64_t pair_bits(const Pair& p)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(p.v.x), "f"(p.v.y));
+    return r;
+}
+__device__ __forceinline__ Pair bits_pair(uint64_t b)
+{
+    Pair r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.v.x), "=f"(r.v.y) : "l"(b));
+    return r;
+}
+__device__ __forceinline__ Pair operator+(const Pair& a, const Pair& b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair_bits(a)), "l"(pair_bits(b)));
+    return bits_pair(r);
+}
+__device__ __forceinline__ Pair operator*(const Pair& a, const Pair& b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair_bits(a)), "l"(pair_bits(b)));
+    return bits_pair(r);
+}
+__device__ __forceinline__ Pair fma2(const Pair& a, const Pair& b, const Pair& c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(pair_bits(a)), "l"(pair_bits(b)), "l"(pair_bits(c)));
+    return bits_pair(r);
+}
+
+// A 16-byte vector as pairs of neighbouring values.
+template <typename T>
+__device__ __forceinline__ void unpack_pairs(const uint4& v, Pair (&f)[Vec16<T>::kElems / 2])
+{
+    float e[Vec16<T>::kElems];
+    Vec16<T>::unpack(v, e);
+#pragma unroll
+    for (int i = 0; i < Vec16<T>::kElems / 2; ++i) f[i] = pair(e[2 * i], e[2 * i + 1]);
+}
+
+template <typename T>
+__device__ __forceinline__ uint4 pack_pairs(const Pair (&f)[Vec16<T>::kElems / 2])
+{
+    float e[Vec16<T>::kElems];
+#pragma unroll
+    for (int i = 0; i < Vec16<T>::kElems / 2; ++i) {
+        e[2 * i] = f[i].v.x;
+        e[2 * i + 1] = f[i].v.y;
+    }
+    return Vec16<T>::pack(e);
+}
+
 // A 16-byte load of data that the same thread may overwrite later (in-place calls): like ld_stream16 without the
 // read-only path, and kept in program order with st_stream16.
 __device__ __forceinline__ uint4 ld_once16(const void* p)
