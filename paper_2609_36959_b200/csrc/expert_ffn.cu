@@ -36,7 +36,7 @@ constexpr int kBlockK = 64;              // depth of one ring slot: 128 bytes, o
 // Workspace: header, row tiles, experts' segment lists.
 struct PlanView {
     int32_t* row_tiles;                  // [1] number of row tiles
-    int4* tile;                          // {first row, rows | slot's tiles << 9, expert, slot's first tile}
+    int4* tile;                          // {first row, rows | expert's row tiles << 9, expert, expert's first tile}
     int32_t* seg_start;                  // [E + 1] into segs
     int32_t* expert_blocks;              // [E] 64-row blocks of the expert's rows
     int2* segs;                          // [D] {first row, rows}, slots in ascending order
@@ -95,72 +95,108 @@ __device__ __forceinline__ int block_prefix(int v, int* scratch, int* total)
     return s - v + (warp > 0 ? scratch[warp - 1] : 0);
 }
 
+// Shared memory of the plan kernel, in ints: five arrays by slot, four by expert, and per group of 32 * k consecutive
+// slots (one a warp) the number of slots of every expert.
+__host__ __device__ inline int plan_groups(int D) { return D <= kPlanThreads ? (D + 31) / 32 : kPlanThreads / 32; }
+static size_t plan_smem(int D, int E) { return 4 * (5 * static_cast<size_t>(D) + 4 * static_cast<size_t>(E)) + 2 * static_cast<size_t>(plan_groups(D)) * E; }
+
 // One CTA.  Offsets that decrease or pass P are clamped, rows of a slot without a valid expert skipped, both flagged.
+// The slots with rows are sorted by expert (counting sort, stable), and row tiles listed in that order, so that the
+// slots of an expert's replicas share its weights in L2.
 __global__ void __launch_bounds__(kPlanThreads)
 ffn_plan_kernel(const uint32_t* __restrict__ offsets, const int32_t* __restrict__ slot_expert, int64_t P, int D, int E, PlanView out,
-                bool with_experts, uint32_t* __restrict__ err_word)
+                uint32_t* __restrict__ err_word)
 {
+    launch_dependents();
     __shared__ int scratch[32];
-    extern __shared__ int per_slot[];            // [4][D]
-    int *s_first = per_slot, *s_rows = per_slot + D, *s_tile = per_slot + 2 * D, *s_expert = per_slot + 3 * D;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int tiles_before = 0;
-    for (int base = 0; base < D; base += kPlanThreads) {
-        const int d = base + threadIdx.x;
-        int rows = 0, tiles = 0;
-        if (d < D) {
-            const int64_t a = offsets[d], b = offsets[d + 1];
-            const int64_t lo = a < P ? a : P, hi = b < P ? b : P;
-            const int e = slot_expert[d];
-            bool bad = b < a || b > P;
-            rows = hi > lo ? static_cast<int>(hi - lo) : 0;
-            if (rows > 0 && (e < 0 || e >= E)) {
-                bad = true;
-                rows = 0;
-            }
-            if (bad) flag_error(err_word, COBALT_DEVERR_BAD_SLOT);
-            s_first[d] = static_cast<int>(lo);
-            s_rows[d] = rows;
-            s_expert[d] = rows > 0 ? e : -1;
-            tiles = (rows + kTileN - 1) / kTileN;
+    extern __shared__ int plan_shared[];
+    int *s_first = plan_shared, *s_rows = s_first + D, *s_expert = s_rows + D, *s_rank = s_expert + D, *s_order = s_rank + D;
+    int *e_tiles = s_order + D, *e_blocks = e_tiles + E, *e_start = e_blocks + E, *e_first = e_start + E;
+    uint16_t* group_count = reinterpret_cast<uint16_t*>(e_first + E);      // [groups][E]
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, groups = plan_groups(D), per_group = (D + groups - 1) / groups;
+    const int span = (per_group + 31) / 32 * 32;                           // slots of a group
+
+    for (int i = threadIdx.x; i < groups * E; i += kPlanThreads) group_count[i] = 0;
+    for (int i = threadIdx.x; i < E; i += kPlanThreads) e_tiles[i] = e_blocks[i] = e_first[i] = 0;
+    for (int d = threadIdx.x; d < D; d += kPlanThreads) {
+        const int64_t a = offsets[d], b = offsets[d + 1];
+        const int64_t lo = a < P ? a : P, hi = b < P ? b : P;
+        const int e = slot_expert[d];
+        bool bad = b < a || b > P;
+        int rows = hi > lo ? static_cast<int>(hi - lo) : 0;
+        if (rows > 0 && (e < 0 || e >= E)) {
+            bad = true;
+            rows = 0;
         }
+        if (bad) flag_error(err_word, COBALT_DEVERR_BAD_SLOT);
+        s_first[d] = static_cast<int>(lo);
+        s_rows[d] = rows;
+        s_expert[d] = rows > 0 ? e : -1;
+    }
+    __syncthreads();
+    if (warp < groups) {
+        for (int d0 = warp * span; d0 < min(D, (warp + 1) * span); d0 += 32) {
+            const int d = d0 + lane, e = d < D ? s_expert[d] : -1;
+            const uint32_t same = __match_any_sync(0xFFFFFFFFu, e);
+            if (e >= 0) {
+                const int before = group_count[warp * E + e], ahead = __popc(same & ((1u << lane) - 1u));
+                s_rank[d] = before + ahead;
+                atomicAdd(&e_tiles[e], (s_rows[d] + kTileN - 1) / kTileN);
+                atomicAdd(&e_blocks[e], (s_rows[d] + kBlockK - 1) / kBlockK);
+            }
+            __syncwarp();
+            if (e >= 0 && (same >> lane) == 1u) group_count[warp * E + e] += static_cast<uint16_t>(__popc(same));   // the last of its kind
+            __syncwarp();
+        }
+    }
+    __syncthreads();
+    // E <= 1024: an expert a thread
+    int slots = 0;
+    if (threadIdx.x < E)
+        for (int g = 0; g < groups; ++g) {
+            const int n = group_count[g * E + threadIdx.x];
+            group_count[g * E + threadIdx.x] = static_cast<uint16_t>(slots);
+            slots += n;
+        }
+    int used;
+    const int start = block_prefix(slots, scratch, &used);
+    if (threadIdx.x < E) {
+        e_start[threadIdx.x] = start;
+        out.seg_start[threadIdx.x] = start;
+        out.expert_blocks[threadIdx.x] = e_blocks[threadIdx.x];
+    }
+    if (threadIdx.x == 0) out.seg_start[E] = used;
+    __syncthreads();
+    for (int d = threadIdx.x; d < D; d += kPlanThreads) {
+        const int e = s_expert[d];
+        if (e >= 0) s_order[e_start[e] + group_count[(d / span) * E + e] + s_rank[d]] = d;
+    }
+    __syncthreads();
+    int* s_tile = s_rank;                                                  // by sorted position from here on
+    int tiles_before = 0;
+    for (int base = 0; base < used; base += kPlanThreads) {
+        const int i = base + threadIdx.x, d = i < used ? s_order[i] : 0;
         int total;
-        const int at = block_prefix(tiles, scratch, &total);
-        if (d < D) s_tile[d] = tiles_before + at;
+        const int at = tiles_before + block_prefix(i < used ? (s_rows[d] + kTileN - 1) / kTileN : 0, scratch, &total);
+        if (i < used) {
+            s_tile[i] = at;
+            if (e_start[s_expert[d]] == i) e_first[s_expert[d]] = at;
+            out.segs[i] = make_int2(s_first[d], s_rows[d]);
+        }
         tiles_before += total;
     }
     if (threadIdx.x == 0) *out.row_tiles = tiles_before;
     __syncthreads();
-    for (int d = warp; d < D; d += kPlanThreads / 32) {
-        const int rows = s_rows[d], n = (rows + kTileN - 1) / kTileN;
-        if (n == 0) continue;
-        // the slot's rows in equal tiles of a multiple of 32 rows: all but the last are full
-        const int step = ((rows + n - 1) / n + 31) / 32 * 32;
-        for (int i = lane; i < n; i += 32) {
-            const int left = rows - i * step;
-            out.tile[s_tile[d] + i] = make_int4(s_first[d] + i * step, (left < step ? left : step) | (n << 9), s_expert[d], s_tile[d]);
+    for (int i = warp; i < used; i += kPlanThreads / 32) {
+        // the slot's rows in tiles of as equal a number of 32-row units as can be: tiles that share weights then take
+        // the same time and stay together
+        const int d = s_order[i], e = s_expert[d], rows = s_rows[d];
+        const int n = (rows + kTileN - 1) / kTileN, units = (rows + 31) / 32, least = units / n, more = units - least * n;
+        for (int k = lane; k < n; k += 32) {
+            const int unit = k * least + min(k, more), own = least + (k < more), left = rows - 32 * unit;
+            out.tile[s_tile[i] + k] = make_int4(s_first[d] + 32 * unit, min(left, 32 * own) | (e_tiles[e] << 9), e, e_first[e]);
         }
     }
-    if (!with_experts) return;
-    // segments of every expert in ascending slot order (E <= 1024: an expert a thread)
-    const int e = threadIdx.x;
-    int count = 0, blocks = 0;
-    if (e < E)
-        for (int d = 0; d < D; ++d)
-            if (s_expert[d] == e) {
-                count += 1;
-                blocks += (s_rows[d] + kBlockK - 1) / kBlockK;
-            }
-    int total;
-    int at = block_prefix(count, scratch, &total);
-    if (e < E) {
-        out.seg_start[e] = at;
-        out.expert_blocks[e] = blocks;
-        if (count > 0)
-            for (int d = 0; d < D; ++d)
-                if (s_expert[d] == e) out.segs[at++] = make_int2(s_first[d], s_rows[d]);
-    }
-    if (threadIdx.x == 0) out.seg_start[E] = total;
 }
 
 // ---- the product kernel ------------------------------------------------------------------------------------------
@@ -203,10 +239,16 @@ struct Shape {
     static constexpr int kSmem = kRing * kSlotBytes + kStaging + kBarriers;
 };
 
+// Tiles of an expert run in bands of eight row tiles (kWeights: eight tiles of M), the other extent outside: the 74
+// pairs at work then cover about 8 x 9 tiles and share both operands in L2.
+constexpr int kBand = 8;
+
 struct Tile {
     int expert, m0, n0, n;       // n: extent of the instruction's N (multiple of 32)
     int row0, rows;              // row stages
     int blocks;                  // 64-deep blocks of k
+    int seg, seg_end;            // kWeights: the expert's segments
+    int2 head;                   // kWeights: the first one
 };
 
 template <int kStage>
@@ -225,25 +267,30 @@ __device__ __forceinline__ Tile get_tile(const ProductArgs& p, int t)
     if (kStage == kWeights) {
         const int nt = (p.N + kTileN - 1) / kTileN;
         r.expert = t / (mt * nt);
-        const int in = t - r.expert * mt * nt;
-        r.m0 = in / nt * kTileM;
-        r.n0 = in % nt * kTileN;
+        const int in = t - r.expert * mt * nt, band = in / (kBand * nt), high = min(kBand, mt - band * kBand), at = in - band * kBand * nt;
+        r.m0 = (band * kBand + at % high) * kTileM;
+        r.n0 = at / high * kTileN;
         r.n = min(kTileN, (p.N - r.n0 + 31) / 32 * 32);
         r.row0 = r.rows = 0;
         r.blocks = p.plan.expert_blocks[r.expert];
+        r.seg = p.plan.seg_start[r.expert];
+        r.seg_end = p.plan.seg_start[r.expert + 1];
+        r.head = r.blocks > 0 ? p.plan.segs[r.seg] : make_int2(0, 0);
     } else {
-        // tiles of a slot lie together, its row tiles innermost: what runs at one time shares weights and rows in L2.
-        // All entries between a slot's first and last tile carry its first tile and count.
+        // all entries between an expert's first and last tile carry its first tile and count
         const int4 any = p.plan.tile[t / mt];
         const int count = static_cast<int>(static_cast<uint32_t>(any.y) >> 9), in = t - any.w * mt;
-        const int4 own = p.plan.tile[any.w + in % count];
+        const int band = in / (kBand * mt), high = min(kBand, count - band * kBand), at = in - band * kBand * mt;
+        const int4 own = p.plan.tile[any.w + band * kBand + at % high];
         r.expert = own.z;
-        r.m0 = in / count * kTileM;
+        r.m0 = at / high * kTileM;
         r.n0 = 0;
         r.row0 = own.x;
         r.rows = own.y & 511;
         r.n = (r.rows + 31) / 32 * 32;
         r.blocks = (p.K + kBlockK - 1) / kBlockK;
+        r.seg = r.seg_end = 0;
+        r.head = make_int2(0, 0);
     }
     return r;
 }
@@ -321,6 +368,8 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     tmem_fence_before();
     cluster_sync();
     tmem_fence_after();
+    wait_for_prior_kernel();                     // the plan, and what the kernel before wrote
+    launch_dependents();
     uint32_t tmem;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot) : "memory");
 
@@ -332,49 +381,51 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         // ---- loads of this CTA's halves --------------------------------------------------------------------
         Ring ring;
         int64_t issued = 0;
+        // a band reads its row tiles (kWeights: tiles of M) again for every tile of the other extent, and that one once
+        const uint64_t once = policy_normal(), again = policy_evict_last();
+        const uint64_t policy_a = S::kWeightsStage ? again : once, policy_b = S::kWeightsStage ? once : again;
+        Tile next = {};
+        if (first < tiles) next = get_tile<kStage>(p, first);
         for (int t = first; t < tiles && ok; t += step) {
-            const Tile w = get_tile<kStage>(p, t);
+            const Tile w = next;
             const int half = w.n / 2, m0 = w.m0 + static_cast<int>(rank) * 128;
-            if (kStage == kWeights) {
-                const int boxes_b = (half + 63) / 64, n0 = w.n0 + static_cast<int>(rank) * half;
-                for (int s = p.plan.seg_start[w.expert], z = p.plan.seg_start[w.expert + 1]; s < z && ok; ++s) {
-                    const int2 seg = p.plan.segs[s];
-                    for (int r = 0; r < seg.y; r += kBlockK) {
-                        if (!(ok = barrier_wait(empty + 8 * ring.slot, ring.phase ^ 1))) break;
-                        const uint32_t bar = full + 8 * ring.slot, a = base + ring.slot * kSlotBytes;
-                        if (elect_one()) {
-                            barrier_expect(bar, (2 + boxes_b) * kBoxBytes);
-                            tma_load_2d(a, &map_a, bar, m0, seg.x + r);
-                            tma_load_2d(a + kBoxBytes, &map_a, bar, m0 + 64, seg.x + r);
-                            tma_load_2d(a + kHalfBytes, &map_b, bar, n0, seg.x + r);
-                            if (boxes_b > 1) tma_load_2d(a + kHalfBytes + kBoxBytes, &map_b, bar, n0 + 64, seg.x + r);
-                        }
-                        __syncwarp();
-                        ring.next<S::kRing>();
-                        ++issued;
-                    }
-                }
-            } else {
-                const int row0 = w.row0 + static_cast<int>(rank) * half;
-                for (int k = 0; k < w.blocks; ++k) {
-                    if (!(ok = barrier_wait(empty + 8 * ring.slot, ring.phase ^ 1))) break;
-                    const uint32_t bar = full + 8 * ring.slot, a = base + ring.slot * kSlotBytes, b = a + kHalfBytes;
-                    if (elect_one()) {
+            const int boxes_b = (half + 63) / 64, n0 = w.n0 + static_cast<int>(rank) * half;    // kWeights
+            const int row0 = w.row0 + static_cast<int>(rank) * half;                           // row stages
+            int seg = w.seg, done = 0;
+            int2 rows = w.head;
+            if (w.blocks == 0 && t + step < tiles) next = get_tile<kStage>(p, t + step);
+            for (int k = 0; k < w.blocks; ++k) {
+                // the list's loads are under way before the next tile needs them
+                if (k == w.blocks / 2 && t + step < tiles) next = get_tile<kStage>(p, t + step);
+                if (!(ok = barrier_wait(empty + 8 * ring.slot, ring.phase ^ 1))) break;
+                const uint32_t bar = full + 8 * ring.slot, a = base + ring.slot * kSlotBytes, b = a + kHalfBytes;
+                if (elect_one()) {
+                    if (kStage == kWeights) {
+                        barrier_expect(bar, (2 + boxes_b) * kBoxBytes);
+                        tma_load_2d(a, &map_a, bar, policy_a, m0, rows.x + done);
+                        tma_load_2d(a + kBoxBytes, &map_a, bar, policy_a, m0 + 64, rows.x + done);
+                        tma_load_2d(b, &map_b, bar, policy_b, n0, rows.x + done);
+                        if (boxes_b > 1) tma_load_2d(b + kBoxBytes, &map_b, bar, policy_b, n0 + 64, rows.x + done);
+                    } else {
                         barrier_expect(bar, kHalfBytes + half * kBlockK * 2);
-                        if (kStage == kUp) tma_load_5d(a, &map_a, bar, k * kBlockK, 0, 0, m0 / 16, w.expert);
-                        if (kStage == kDown) tma_load_3d(a, &map_a, bar, k * kBlockK, m0, w.expert);
+                        if (kStage == kUp) tma_load_5d(a, &map_a, bar, policy_a, k * kBlockK, 0, 0, m0 / 16, w.expert);
+                        if (kStage == kDown) tma_load_3d(a, &map_a, bar, policy_a, k * kBlockK, m0, w.expert);
                         if (S::kAMn) {
-                            tma_load_3d(a, &map_a, bar, m0, k * kBlockK, w.expert);
-                            tma_load_3d(a + kBoxBytes, &map_a, bar, m0 + 64, k * kBlockK, w.expert);
+                            tma_load_3d(a, &map_a, bar, policy_a, m0, k * kBlockK, w.expert);
+                            tma_load_3d(a + kBoxBytes, &map_a, bar, policy_a, m0 + 64, k * kBlockK, w.expert);
                         }
                         if (half == 128)
-                            tma_load_2d(b, &map_b, bar, k * kBlockK, row0);
+                            tma_load_2d(b, &map_b, bar, policy_b, k * kBlockK, row0);
                         else
-                            for (int i = 0; i < half; i += 16) tma_load_2d(b + i * 128, &map_b_part, bar, k * kBlockK, row0 + i);
+                            for (int i = 0; i < half; i += 16) tma_load_2d(b + i * 128, &map_b_part, bar, policy_b, k * kBlockK, row0 + i);
                     }
-                    __syncwarp();
-                    ring.next<S::kRing>();
-                    ++issued;
+                }
+                __syncwarp();
+                ring.next<S::kRing>();
+                ++issued;
+                if (kStage == kWeights && (done += kBlockK) >= rows.y && ++seg < w.seg_end) {
+                    rows = p.plan.segs[seg];
+                    done = 0;
                 }
             }
         }
@@ -389,9 +440,14 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         // ---- products (leading CTA); the other CTA passes on that its loads have landed -------------------------
         Ring ring;
         int turn = 0;                            // accumulators used so far
+        Tile next = {};
+        if (first < tiles) next = get_tile<kStage>(p, first);
         for (int t = first; t < tiles && ok; t += step) {
-            const Tile w = get_tile<kStage>(p, t);
-            if (w.blocks == 0) continue;
+            const Tile w = next;
+            if (w.blocks == 0) {
+                if (t + step < tiles) next = get_tile<kStage>(p, t + step);
+                continue;
+            }
             const int half = w.n / 2;
             const uint32_t acc = turn & 1, d = tmem + acc * 256;
             const uint32_t idesc = instruction_descriptor(w.n, S::kAMn, S::kWeightsStage);
@@ -399,19 +455,15 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 if (!(ok = barrier_wait(acc_empty + 8 * acc, ((turn >> 1) & 1) ^ 1))) break;
                 tmem_fence_after();
             }
-            int s = 0, z = 0, left = 0;
-            if (kStage == kWeights) {
-                s = p.plan.seg_start[w.expert];
-                z = p.plan.seg_start[w.expert + 1];
-                left = p.plan.segs[s].y;
-            }
+            int seg = w.seg, left = w.head.y;
             for (int k = 0; k < w.blocks; ++k) {
+                if (k == w.blocks / 2 && t + step < tiles) next = get_tile<kStage>(p, t + step);
                 if (!(ok = barrier_wait(full + 8 * ring.slot, ring.phase))) break;
                 const uint32_t a = base + ring.slot * kSlotBytes;
                 if (kStage == kWeights) {
                     if (left < kBlockK) clear_tail(a, (half + 63) / 64, left, lane);
                     left -= kBlockK;
-                    if (left <= 0 && ++s < z) left = p.plan.segs[s].y;
+                    if (left <= 0 && ++seg < w.seg_end) left = p.plan.segs[seg].y;
                 }
                 if (rank != 0) {
                     if (elect_one()) barrier_arrive_cluster(peer_address(relay + 8 * ring.slot, 0));
@@ -455,7 +507,7 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         for (int t = first; t < tiles && ok; t += step) {
             const Tile w = get_tile<kStage>(p, t);
             const uint32_t acc = turn & 1;
-            if (w.blocks > 0) {
+            if (w.blocks > 0 && kStage != kDownBackward) {
                 // one verdict for the four warps: none is left alone at the barriers below
                 ok = named_barrier_and(1, 128, barrier_wait(acc_full + 8 * acc, (turn >> 1) & 1));
                 if (!ok) break;
@@ -533,15 +585,24 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 const int f0 = w.m0 + static_cast<int>(rank) * 128;
                 const int v = tid & 31, f = f0 + 8 * (v & 15);
                 const int64_t col = (v < 16 ? 0 : F) + f;
-                for (int c = 0; c < w.n; c += 32) {
-                    // gate and up of the chunk come in by rows; each thread reads and later overwrites the same vectors
+                // gate and up come in by rows, a chunk ahead; each thread reads and later overwrites the same vectors
+                uint4 x[8];
+                auto fetch = [&](int c) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const int tok = i * 4 + (tid >> 5);
-                        uint4 x = make_uint4(0, 0, 0, 0);
-                        if (c + tok < w.rows && f < F) x = ld_once16(p.pre_in + static_cast<int64_t>(w.row0 + c + tok) * 2 * F + col);
-                        store_shared16(staging + tok * S::kPitch + v * 16, x);
+                        x[i] = make_uint4(0, 0, 0, 0);
+                        if (c + tok < w.rows && f < F) x[i] = ld_once16(p.pre_in + static_cast<int64_t>(w.row0 + c + tok) * 2 * F + col);
                     }
+                };
+                fetch(0);
+                ok = named_barrier_and(1, 128, barrier_wait(acc_full + 8 * acc, (turn >> 1) & 1));
+                if (!ok) break;
+                tmem_fence_after();
+                for (int c = 0; c < w.n; c += 32) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) store_shared16(staging + (i * 4 + (tid >> 5)) * S::kPitch + v * 16, x[i]);
+                    if (c + 32 < w.n) fetch(c + 32);
                     named_barrier(1, 128);
 #pragma unroll
                     for (int hl = 0; hl < 2; ++hl) {
@@ -697,19 +758,29 @@ static int launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUte
     rc = sm_count(&sms);
     if (rc != COBALT_OK) return rc;
     const int64_t pairs = max_tiles < sms / 2 ? max_tiles : sms / 2;
-    ffn_product_kernel<kStage><<<static_cast<unsigned>(2 * (pairs < 1 ? 1 : pairs)), kProductThreads, Shape<kStage>::kSmem, s>>>(a, b, b_part, p);
-    COBALT_CUDA_TRY(cudaGetLastError());
+    // may start while the kernel before it (the plan, or a product of the same call) is at its end; it waits for that
+    // one before it touches memory
+    cudaLaunchAttribute attr;
+    set_programmatic_launch(&attr, true);
+    cudaLaunchConfig_t config = {};
+    config.gridDim = dim3(static_cast<unsigned>(2 * (pairs < 1 ? 1 : pairs)));
+    config.blockDim = dim3(kProductThreads);
+    config.dynamicSmemBytes = Shape<kStage>::kSmem;
+    config.stream = s;
+    config.attrs = &attr;
+    config.numAttrs = 1;
+    COBALT_CUDA_TRY(cudaLaunchKernelEx(&config, ffn_product_kernel<kStage>, a, b, b_part, p));
     return COBALT_OK;
 }
 
-static int launch_plan(const uint32_t* offsets, const int32_t* slot_expert, int64_t P, int D, const ProductArgs& p, bool with_experts,
-                       cudaStream_t s)
+static int launch_plan(const uint32_t* offsets, const int32_t* slot_expert, int64_t P, int D, const ProductArgs& p, cudaStream_t s)
 {
-    const size_t bytes = 16 * static_cast<size_t>(D);
+    const size_t bytes = plan_smem(D, p.E);
     // the attribute is set to the most that any call needs, so that concurrent calls agree on it
-    const int rc = ensure_kernel_attributes(reinterpret_cast<const void*>(ffn_plan_kernel), 16 * COBALT_MAX_DESTS, false);
+    const int rc = ensure_kernel_attributes(reinterpret_cast<const void*>(ffn_plan_kernel),
+                                            plan_smem(COBALT_MAX_DESTS, COBALT_MAX_EXPERTS), false);
     if (rc != COBALT_OK) return rc;
-    ffn_plan_kernel<<<1, kPlanThreads, bytes, s>>>(offsets, slot_expert, P, D, p.E, p.plan, with_experts, p.err_word);
+    ffn_plan_kernel<<<1, kPlanThreads, bytes, s>>>(offsets, slot_expert, P, D, p.E, p.plan, p.err_word);
     COBALT_CUDA_TRY(cudaGetLastError());
     return COBALT_OK;
 }
@@ -771,7 +842,7 @@ int cobalt_expert_ffn(const void* rows, const uint32_t* dest_offsets, const int3
     COBALT_TRY(rows_map(&b2, act, P, F, 128));
     COBALT_TRY(rows_map(&part2, act, P, F, 16));
 
-    COBALT_TRY(launch_plan(dest_offsets, slot_expert, P, D, p, false, s));
+    COBALT_TRY(launch_plan(dest_offsets, slot_expert, P, D, p, s));
     p.M = 2 * F;
     p.K = H;
     p.out = static_cast<bf16*>(act);
@@ -811,8 +882,7 @@ int cobalt_expert_ffn_backward(const void* grad_out, const void* rows, const uin
     p.F = F;
     const int64_t row_tiles = max_row_tiles(P, static_cast<int>(P < D ? P : D));
     CUtensorMap a, b, part;
-    const bool weights = grad_w_gate_up || grad_w_down;
-    COBALT_TRY(launch_plan(dest_offsets, slot_expert, P, D, p, weights, s));
+    COBALT_TRY(launch_plan(dest_offsets, slot_expert, P, D, p, s));
     if (grad_rows || grad_w_gate_up) {
         COBALT_TRY(weights_map(&a, w_down, E, H, F, kBlockK));
         COBALT_TRY(rows_map(&b, grad_out, P, H, 128));
