@@ -18,22 +18,34 @@ namespace cobalt {
 
 constexpr int kDropoutThreads = 256;
 constexpr int kDropoutBlock = 8;         // elements of one counter
-constexpr int kDropoutUnroll = 1;        // blocks a thread has in flight
 
-__device__ __forceinline__ uint4 philox_4x32_10(uint32_t c0, uint32_t c1, uint32_t k0, uint32_t k1)
+// The ten round keys.  Known on the host they are kernel arguments, which the rounds read as constant operands.
+struct PhiloxKeys {
+    uint32_t k0[10], k1[10];
+    __host__ __device__ void set(uint64_t seed)
+    {
+        for (int r = 0; r < 10; ++r) {
+            k0[r] = static_cast<uint32_t>(seed) + static_cast<uint32_t>(r) * 0x9E3779B9u;
+            k1[r] = static_cast<uint32_t>(seed >> 32) + static_cast<uint32_t>(r) * 0xBB67AE85u;
+        }
+    }
+};
+
+__device__ __forceinline__ void philox_4x32_10(uint32_t c0, uint32_t c1, const PhiloxKeys& key, uint32_t (&w)[4])
 {
     uint32_t c2 = 0, c3 = 0;
 #pragma unroll
     for (int r = 0; r < 10; ++r) {
         const uint64_t a = static_cast<uint64_t>(c0) * 0xD2511F53u, b = static_cast<uint64_t>(c2) * 0xCD9E8D57u;
-        c0 = static_cast<uint32_t>(b >> 32) ^ c1 ^ k0;
+        c0 = static_cast<uint32_t>(b >> 32) ^ c1 ^ key.k0[r];
         c1 = static_cast<uint32_t>(b);
-        c2 = static_cast<uint32_t>(a >> 32) ^ c3 ^ k1;
+        c2 = static_cast<uint32_t>(a >> 32) ^ c3 ^ key.k1[r];
         c3 = static_cast<uint32_t>(a);
-        k0 += 0x9E3779B9u;
-        k1 += 0xBB67AE85u;
     }
-    return make_uint4(c0, c1, c2, c3);
+    w[0] = c0;
+    w[1] = c1;
+    w[2] = c2;
+    w[3] = c3;
 }
 
 // The threshold in the upper half of a word, to which whole words compare: the high half-word decides there alone, and
@@ -44,66 +56,71 @@ struct DropoutRule {
     float scale;
 };
 
-__device__ __forceinline__ float dropout_value(float v, uint32_t word, int e, const DropoutRule& rule)
+__device__ __forceinline__ bool dropout_keeps(uint32_t word, int e, const DropoutRule& rule)
 {
     const uint32_t w = (e & 1) ? word : word << 16;
-    return (w >= rule.limit && rule.any) ? v * rule.scale : 0.0f;      // a select: a dropped infinity is 0 too
+    return w >= rule.limit && rule.any;
 }
 
-template <typename T>
+// A thread owns one block.  A dropped element is selected away before the arithmetic, so that a dropped infinity is 0 too.
+template <typename T, bool kAdd, bool kDeviceSeed>
 __global__ void __launch_bounds__(kDropoutThreads)
-dropout_kernel(const T* x, const T* add, T* out, int64_t n, uint64_t seed, const uint64_t* seed_ptr, DropoutRule rule)
+dropout_kernel(const T* x, const T* add, T* out, int64_t n, PhiloxKeys key, const uint64_t* seed_ptr, DropoutRule rule)
 {
     constexpr int N = Vec16<T>::kElems, kVecs = kDropoutBlock / N;
-    if (seed_ptr) seed = *seed_ptr;
-    const uint32_t k0 = static_cast<uint32_t>(seed), k1 = static_cast<uint32_t>(seed >> 32);
-    const int64_t whole = n / kDropoutBlock, stride = static_cast<int64_t>(gridDim.x) * kDropoutThreads * kDropoutUnroll;
-    for (int64_t base = static_cast<int64_t>(blockIdx.x) * kDropoutThreads * kDropoutUnroll + threadIdx.x; base < whole; base += stride) {
-        uint4 xv[kDropoutUnroll][kVecs], av[kDropoutUnroll][kVecs];
+    const int64_t b = static_cast<int64_t>(blockIdx.x) * kDropoutThreads + threadIdx.x, at = b * kDropoutBlock;
+    if (at >= n) return;
+    const bool whole = at + kDropoutBlock <= n;
+    uint4 xv[kVecs], av[kVecs];
+    if (whole) {
 #pragma unroll
-        for (int u = 0; u < kDropoutUnroll; ++u) {
-            const int64_t b = base + u * kDropoutThreads;
-#pragma unroll
-            for (int v = 0; v < kVecs; ++v) {
-                if (b < whole) {
-                    xv[u][v] = ld_once16(x + b * kDropoutBlock + v * N);
-                    if (add) av[u][v] = ld_once16(add + b * kDropoutBlock + v * N);
-                }
-            }
+        for (int v = 0; v < kVecs; ++v) {
+            xv[v] = ld_once16(x + at + v * N);
+            if (kAdd) av[v] = ld_once16(add + at + v * N);
         }
+    }
+    if (kDeviceSeed) key.set(*seed_ptr);
+    uint32_t w[4];
+    philox_4x32_10(static_cast<uint32_t>(b), static_cast<uint32_t>(b >> 32), key, w);
+    if (whole) {
 #pragma unroll
-        for (int u = 0; u < kDropoutUnroll; ++u) {
-            const int64_t b = base + u * kDropoutThreads;
-            if (b >= whole) break;
-            const uint4 rnd = philox_4x32_10(static_cast<uint32_t>(b), static_cast<uint32_t>(b >> 32), k0, k1);
-            const uint32_t w[4] = {rnd.x, rnd.y, rnd.z, rnd.w};
+        for (int v = 0; v < kVecs; ++v) {
+            float f[N], a[N];
+            Vec16<T>::unpack(xv[v], f);
+            if (kAdd) Vec16<T>::unpack(av[v], a);
 #pragma unroll
-            for (int v = 0; v < kVecs; ++v) {
-                float f[N], a[N];
-                Vec16<T>::unpack(xv[u][v], f);
-                if (add) Vec16<T>::unpack(av[u][v], a);
+            for (int i = 0; i < N; ++i) {
+                const int e = v * N + i;
+                const float kept = dropout_keeps(w[e >> 1], e, rule) ? f[i] : 0.0f;
+                f[i] = kAdd ? fmaf(kept, rule.scale, a[i]) : kept * rule.scale;
+            }
+            st_stream16(out + at + v * N, Vec16<T>::pack(f));
+        }
+    } else {                                               // the last n % 8 elements
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const int e = v * N + i;
-                    const float kept = dropout_value(f[i], w[e >> 1], e, rule);
-                    f[i] = add ? a[i] + kept : kept;
-                }
-                st_stream16(out + b * kDropoutBlock + v * N, Vec16<T>::pack(f));
+        for (int e = 0; e < kDropoutBlock; ++e) {
+            if (at + e < n) {
+                const float kept = dropout_keeps(w[e >> 1], e, rule) ? static_cast<float>(x[at + e]) : 0.0f;
+                out[at + e] = static_cast<T>(kAdd ? fmaf(kept, rule.scale, static_cast<float>(add[at + e])) : kept * rule.scale);
             }
         }
     }
-    // the last n % 8 elements
-    if (blockIdx.x == 0 && threadIdx.x < n % kDropoutBlock) {
-        const uint4 rnd = philox_4x32_10(static_cast<uint32_t>(whole), static_cast<uint32_t>(whole >> 32), k0, k1);
-        const uint32_t w[4] = {rnd.x, rnd.y, rnd.z, rnd.w};
-        const int64_t at = whole * kDropoutBlock + threadIdx.x;
-#pragma unroll
-        for (int e = 0; e < kDropoutBlock; ++e) {
-            if (e == static_cast<int>(threadIdx.x)) {
-                const float kept = dropout_value(static_cast<float>(x[at]), w[e >> 1], e, rule);
-                out[at] = static_cast<T>(add ? static_cast<float>(add[at]) + kept : kept);
-            }
-        }
+}
+
+template <typename T>
+static void launch_dropout_kernel(const void* x, const void* add, void* out, int64_t n, uint64_t seed, const uint64_t* seed_ptr,
+                                  const DropoutRule& rule, unsigned grid, cudaStream_t s)
+{
+    PhiloxKeys key;
+    key.set(seed);
+    const T *xt = static_cast<const T*>(x), *at = static_cast<const T*>(add);
+    T* ot = static_cast<T*>(out);
+    if (seed_ptr) {
+        if (add) dropout_kernel<T, true, true><<<grid, kDropoutThreads, 0, s>>>(xt, at, ot, n, key, seed_ptr, rule);
+        else dropout_kernel<T, false, true><<<grid, kDropoutThreads, 0, s>>>(xt, at, ot, n, key, seed_ptr, rule);
+    } else {
+        if (add) dropout_kernel<T, true, false><<<grid, kDropoutThreads, 0, s>>>(xt, at, ot, n, key, seed_ptr, rule);
+        else dropout_kernel<T, false, false><<<grid, kDropoutThreads, 0, s>>>(xt, at, ot, n, key, seed_ptr, rule);
     }
 }
 
@@ -125,17 +142,11 @@ static int launch_dropout(const void* x, const void* add, int64_t n, int32_t dty
     rule.limit = threshold << 16;
     rule.any = threshold < 65536u;
     rule.scale = rule.any ? static_cast<float>(65536.0 / (65536.0 - threshold)) : 0.0f;
-    const int64_t per_cta = static_cast<int64_t>(kDropoutThreads) * kDropoutUnroll * kDropoutBlock;
-    const int64_t ctas = (n + per_cta - 1) / per_cta;
-    const unsigned grid = static_cast<unsigned>(ctas < 0x7FFFFFFFll ? ctas : 0x7FFFFFFFll);
+    const int64_t ctas = ((n + kDropoutBlock - 1) / kDropoutBlock + kDropoutThreads - 1) / kDropoutThreads;
+    if (ctas > 0x7FFFFFFFll) return COBALT_ERR_UNSUPPORTED;           // over 2^42 elements
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (dtype == COBALT_BF16)
-        dropout_kernel<__nv_bfloat16><<<grid, kDropoutThreads, 0, s>>>(static_cast<const __nv_bfloat16*>(x),
-                                                                       static_cast<const __nv_bfloat16*>(add),
-                                                                       static_cast<__nv_bfloat16*>(out), n, seed, seed_ptr, rule);
-    else
-        dropout_kernel<float><<<grid, kDropoutThreads, 0, s>>>(static_cast<const float*>(x), static_cast<const float*>(add),
-                                                               static_cast<float*>(out), n, seed, seed_ptr, rule);
+    if (dtype == COBALT_BF16) launch_dropout_kernel<__nv_bfloat16>(x, add, out, n, seed, seed_ptr, rule, static_cast<unsigned>(ctas), s);
+    else launch_dropout_kernel<float>(x, add, out, n, seed, seed_ptr, rule, static_cast<unsigned>(ctas), s);
     COBALT_CUDA_TRY(cudaGetLastError());
     return COBALT_OK;
 }

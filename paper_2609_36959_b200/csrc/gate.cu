@@ -5,12 +5,12 @@
 //           = s_k / sum_j s_j,  s = 1 / (1 + exp(-l))             sigmoid, renormalised over the chosen
 //   dl_k    = w_k (g_k - sum_j g_j w_j)  [ * (1 - s_k) with sigmoid ], 0 for the experts that were not chosen
 //
-// One warp a token, its E logits in registers (element e in lane e % 32).  The K-th largest of the 32 lane maxima is a
-// bound that at least K logits reach, and few more do (about 10 of 256 for K = 8).  Those go to shared memory, and
-// their rank is the number of larger ones.  A token with NaNs, or with more candidates than the list holds (many equal
-// logits), takes K rounds over all its logits instead: largest key by an integer reduction of the warp, lowest id among
-// equal keys by a second one.  Bound by instructions (about 200 a token against 480 for the rounds alone at E = 256,
-// K = 8), then by the 4E bytes that a token reads.
+// L = 8, 16 or 32 lanes take a token, its E logits in their registers; L is at least K, and a warp holds 32 / L tokens.
+// Each lane keeps the maxima of four parts of its logits; the K-th largest of these 4L maxima is a bound that K logits
+// reach at least, and few more do (about 10 of 256 for K = 8).  Those go to shared memory, and their rank is the number
+// of larger ones.  A token with NaNs, or with more candidates than the list holds (many equal logits), takes K rounds
+// over all its logits instead.  Bound by instructions, which several tokens a warp share, then by the 4E bytes that a
+// token reads.
 #include "numeric.cuh"
 
 namespace cobalt {
@@ -30,11 +30,18 @@ __device__ __forceinline__ uint32_t order_key(float v)
     return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
 
-// The larger of two values, NaN if one is.
+// The larger and the lesser of two values, NaN if one is.
 __device__ __forceinline__ float max_nan(float a, float b)
 {
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+__device__ __forceinline__ float min_nan(float a, float b)
+{
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
 
@@ -49,13 +56,13 @@ __device__ __forceinline__ float load_logit(const __nv_bfloat16* p)
     return __uint_as_float(static_cast<uint32_t>(__ldg(reinterpret_cast<const unsigned short*>(p))) << 16);
 }
 
-// Weights of the chosen logits: lane k < K holds value v.
-__device__ __forceinline__ float chosen_weight(float v, int K, int lane, bool sigmoid)
+// Weights of the chosen logits among L lanes: lane k < K of them holds value v, the first one the largest.
+template <int L>
+__device__ __forceinline__ float chosen_weight(float v, int K, int k, bool sigmoid)
 {
-    const float top = __shfl_sync(kAll, v, 0);
-    if (top == -INFINITY) return 0.0f;                     // every expert masked: no weight, and no NaN
+    const float top = __shfl_sync(kAll, v, 0, L);
     float score = 0.0f;
-    if (lane < K) {
+    if (k < K) {
         if (sigmoid) {
             // s_k up to the common factor exp(min(top, 0)): the ratio survives where s itself underflows
             const float m = fminf(top, 0.0f);
@@ -64,154 +71,213 @@ __device__ __forceinline__ float chosen_weight(float v, int K, int lane, bool si
             score = expf(v - top);
         }
     }
-    const float sum = warp_sum(score);
-    return score / sum;
+    float sum = score;
+#pragma unroll
+    for (int off = 1; off < L; off <<= 1) sum += __shfl_xor_sync(kAll, sum, off);
+    return top == -INFINITY ? 0.0f : score / sum;          // every expert masked: no weight, and no NaN
 }
 
-// K rounds over all logits of the token; lane k gets the k-th.
-template <int VPL>
-__device__ void choose_by_rounds(const float (&v)[VPL], int E, int K, int lane, uint32_t* my_key, int* my_id)
+// Where logit j of a lane stands in the row: chunks of kChunk neighbouring logits (one 16-byte load) go to the L lanes in
+// turn; kChunk = 1 for rows that are no whole vectors.
+template <int L, int kChunk>
+__device__ __forceinline__ int logit_place(int j, int sub)
 {
-    uint32_t key[VPL];
+    return (j / kChunk * L + sub) * kChunk + j % kChunk;
+}
+
+// The lane's logits; -inf behind the row's end.
+template <int L, int VPL, int kChunk, typename T>
+__device__ __forceinline__ void load_logits(const T* row, int E, int sub, float (&v)[VPL])
+{
 #pragma unroll
-    for (int j = 0; j < VPL; ++j) key[j] = j * 32 + lane < E ? order_key(v[j]) : 0u;
-    for (int k = 0; k < K; ++k) {
-        uint32_t best = 0;
-        int at = 0;
+    for (int j = 0; j < VPL; j += kChunk) {
+        const int e = logit_place<L, kChunk>(j, sub);
+        if constexpr (kChunk == 1) {
+            v[j] = e < E ? load_logit(row + e) : -INFINITY;
+        } else {
+            float f[kChunk];
 #pragma unroll
-        for (int j = 0; j < VPL; ++j)
-            if (key[j] > best) {                            // strictly larger: the lowest id of a lane stays
-                best = key[j];
-                at = j;
-            }
-        const uint32_t top = __reduce_max_sync(kAll, best);
-        const int id = __reduce_min_sync(kAll, best == top ? at * 32 + lane : 0x7FFFFFFF);
+            for (int k = 0; k < kChunk; ++k) f[k] = -INFINITY;
+            if (e < E) Vec16<T>::unpack(__ldg(reinterpret_cast<const uint4*>(row + e)), f);
 #pragma unroll
-        for (int j = 0; j < VPL; ++j)
-            if (j * 32 + lane == id) key[j] = 0;
-        if (lane == k) {
-            *my_key = top;
-            *my_id = id;
+            for (int k = 0; k < kChunk; ++k) v[j + k] = f[k];
         }
     }
 }
 
-// VPL: logits a lane holds (E <= 32 * VPL).
-template <typename T, int VPL>
+// A candidate as one integer, larger ones first: the value's order, then the lower id.
+__device__ __forceinline__ unsigned long long candidate(float v, int id)
+{
+    return (static_cast<unsigned long long>(order_key(v)) << 32) | ~static_cast<uint32_t>(id);
+}
+
+// K rounds over all logits of the token, read again each time; lane k gets the k-th candidate.
+template <int L, typename T>
+__device__ __noinline__ unsigned long long choose_by_rounds(const T* row, int E, int K, int sub)
+{
+    unsigned long long mine = 0, last = ~0ull;
+    for (int k = 0; k < K; ++k) {
+        unsigned long long best = 0;                        // the largest below the one before
+        for (int e = sub; e < E; e += L) {
+            const unsigned long long c = candidate(load_logit(row + e), e);
+            if (c < last && c > best) best = c;
+        }
+        for (int off = 1; off < L; off <<= 1) {
+            const unsigned long long o = __shfl_xor_sync(kAll, best, off);
+            best = o > best ? o : best;
+        }
+        last = best;
+        if (sub == k) mine = best;
+    }
+    return mine;
+}
+
+__device__ __forceinline__ void order_pair(float& a, float& b)
+{
+    const float hi = max_nan(a, b), lo = min_nan(a, b);
+    a = hi;
+    b = lo;
+}
+
+// VPL: logits a lane holds (E <= L * VPL).
+template <typename T, int L, int VPL, int kChunk>
 __global__ void __launch_bounds__(kGateThreads)
 gate_topk_kernel(const T* __restrict__ logits, int64_t T_, int E, int K, bool sigmoid, int32_t* __restrict__ ids,
                  float* __restrict__ weights)
 {
-    // a candidate: its key, then the complement of its id, so that a larger word comes first
-    __shared__ unsigned long long list[kGateWarps][kGateList];
-    __shared__ unsigned long long chosen[kGateWarps][COBALT_MAX_TOPK];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t t = static_cast<int64_t>(blockIdx.x) * kGateWarps + warp;
-    if (t >= T_) return;
-    const T* row = logits + t * E;
+    constexpr int kTokens = 32 / L;                         // of a warp
+    __shared__ unsigned long long list[kGateWarps][kTokens][kGateList];
+    __shared__ unsigned long long chosen[kGateWarps][kTokens][COBALT_MAX_TOPK];
+    __shared__ int listed[kGateWarps][kTokens];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % L, own = lane / L;
+    const int64_t t0 = (static_cast<int64_t>(blockIdx.x) * kGateWarps + warp) * kTokens, t = t0 + own;
+    if (t0 >= T_) return;
+    const T* row = logits + (t < T_ ? t : T_ - 1) * E;
     float v[VPL];
+    load_logits<L, VPL, kChunk>(row, E, sub, v);
+    if (sub == 0) listed[warp][own] = 0;
+    // (a NaN stays a NaN through all of this, and every comparison with the bound is then false: no candidates)
+    float part[4];
 #pragma unroll
-    for (int j = 0; j < VPL; ++j) v[j] = j * 32 + lane < E ? load_logit(row + j * 32 + lane) : -INFINITY;
-    uint32_t my_key = 0;
-    int my_id = 0;
-    bool ranked = false;
-    if (VPL > 1) {
-        float best = v[0];
+    for (int q = 0; q < 4; ++q) {
+        part[q] = v[q * (VPL / 4)];
 #pragma unroll
-        for (int j = 1; j < VPL; ++j) best = max_nan(best, v[j]);
-        uint32_t key = order_key(best), bound = 0;
-        const bool any_nan = __any_sync(kAll, best != best);
-        for (int k = 0; k < K; ++k) {                       // equal maxima leave together: the bound is then lower still
-            bound = __reduce_max_sync(kAll, key);
-            if (key == bound) key = 0;
-        }
-        // (all lanes gone: fewer than K different maxima, take every logit)
-        const float least = bound == 0 ? -INFINITY : key_value(bound);
-        uint32_t mask = 0;
+        for (int j = 1; j < VPL / 4; ++j) part[q] = max_nan(part[q], v[q * (VPL / 4) + j]);
+    }
+    order_pair(part[0], part[1]);
+    order_pair(part[2], part[3]);
+    order_pair(part[0], part[2]);
+    order_pair(part[1], part[3]);
+    order_pair(part[1], part[2]);
+    float least = 0.0f;
+    for (int k = 0; k < K; ++k) {                           // equal maxima of several lanes leave together
+        least = part[0];
 #pragma unroll
-        for (int j = 0; j < VPL; ++j)
-            if (v[j] >= least && j * 32 + lane < E) mask |= 1u << j;
-        const int count = __popc(mask);
-        int at = count;
-#pragma unroll
-        for (int off = 1; off < 32; off <<= 1) {
-            const int o = __shfl_up_sync(kAll, at, off);
-            if (lane >= off) at += o;
-        }
-        const int n = __shfl_sync(kAll, at, 31);
-        at -= count;
-        if (n <= kGateList && !any_nan) {
-            ranked = true;
-#pragma unroll
-            for (int j = 0; j < VPL; ++j)
-                if ((mask >> j) & 1u)
-                    list[warp][at++] = (static_cast<unsigned long long>(order_key(v[j])) << 32) | ~static_cast<uint32_t>(j * 32 + lane);
-            __syncwarp();
-            for (int i = lane; i < n; i += 32) {
-                const unsigned long long mine = list[warp][i];
-                int rank = 0;
-                for (int c = 0; c < n; ++c) rank += list[warp][c] > mine;
-                if (rank < K) chosen[warp][rank] = mine;
-            }
-            __syncwarp();
-            if (lane < K) {
-                const unsigned long long c = chosen[warp][lane];
-                my_key = static_cast<uint32_t>(c >> 32);
-                my_id = static_cast<int>(~static_cast<uint32_t>(c));
-            }
+        for (int off = 1; off < L; off <<= 1) least = max_nan(least, __shfl_xor_sync(kAll, least, off));
+        if (part[0] == least) {
+            part[0] = part[1];
+            part[1] = part[2];
+            part[2] = part[3];
+            part[3] = -INFINITY;
         }
     }
-    if (!ranked) choose_by_rounds<VPL>(v, E, K, lane, &my_key, &my_id);
-    const float value = my_key == 0xFFFFFFFFu ? __int_as_float(0x7FC00000) : key_value(my_key);
-    const float w = chosen_weight(value, K, lane, sigmoid);
-    if (lane < K) {
-        ids[t * K + lane] = my_id;
-        weights[t * K + lane] = w;
+    uint32_t mask = 0;
+    if (E == L * VPL) {
+#pragma unroll
+        for (int j = 0; j < VPL; ++j)
+            if (v[j] >= least) mask |= 1u << j;
+    } else {
+#pragma unroll
+        for (int j = 0; j < VPL; ++j)
+            if (v[j] >= least && logit_place<L, kChunk>(j, sub) < E) mask |= 1u << j;
+    }
+    __syncwarp();
+    // places in the list are dealt in any order: the ranks do not depend on it
+    int at = 0;
+    if (mask != 0) at = atomicAdd(&listed[warp][own], __popc(mask));
+    __syncwarp();
+    const int n = listed[warp][own];
+    const bool ranked = n >= K && n <= kGateList;
+    if (ranked) {
+        while (mask != 0) {                                 // one or two a lane: read again, the registers cannot be indexed
+            const int e = logit_place<L, kChunk>(__ffs(mask) - 1, sub);
+            mask &= mask - 1;
+            list[warp][own][at++] = candidate(load_logit(row + e), e);
+        }
+    }
+    __syncwarp();
+    if (ranked)
+        for (int i = sub; i < n; i += L) {
+            const unsigned long long a = list[warp][own][i];
+            int rank = 0;
+#pragma unroll 4
+            for (int c = 0; c < n; ++c) rank += list[warp][own][c] > a;
+            if (rank < K) chosen[warp][own][rank] = a;
+        }
+    __syncwarp();
+    unsigned long long mine = ranked && sub < K ? chosen[warp][own][sub] : 0;
+    if (!__all_sync(kAll, ranked)) {
+        const unsigned long long slow = choose_by_rounds<L>(row, E, K, sub);
+        if (!ranked) mine = slow;
+    }
+    const uint32_t key = static_cast<uint32_t>(mine >> 32);
+    const float value = key == 0xFFFFFFFFu ? __int_as_float(0x7FC00000) : key_value(key);
+    const float w = chosen_weight<L>(value, K, sub, sigmoid);
+    if (sub < K && t < T_) {
+        ids[t * K + sub] = static_cast<int>(~static_cast<uint32_t>(mine));
+        weights[t * K + sub] = w;
     }
 }
 
 __device__ __forceinline__ void store_grad(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_grad(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
+// A warp takes 32 / lanes tokens, `lanes` (K or the next power of two) lanes each for the chosen, all lanes for the zeros.
 // The sigmoid's 1 - s_k needs the sum S of the chosen sigmoids, s_k = w_k S: S = s_0 / w_0 from the first logit alone,
-// one gathered sector a token instead of K (41 to 33 us at T = 131072, E = 256, K = 8).
+// one gathered sector a token instead of K.
 template <typename T, bool kVector>
 __global__ void __launch_bounds__(kGateThreads)
 gate_topk_backward_kernel(const float* __restrict__ grad_w, const T* __restrict__ logits, const int32_t* __restrict__ ids,
-                          const float* __restrict__ weights, int64_t T_, int E, int K, bool sigmoid,
+                          const float* __restrict__ weights, int64_t T_, int E, int K, int lanes, bool sigmoid,
                           T* __restrict__ grad_logits, uint32_t* __restrict__ err_word)
 {
-    const int lane = threadIdx.x & 31;
-    const int64_t t = static_cast<int64_t>(blockIdx.x) * kGateWarps + (threadIdx.x >> 5);
-    if (t >= T_) return;
-    T* row = grad_logits + t * E;
-    if (kVector) {                                          // rows are whole 16-byte vectors
-        for (int e = lane * Vec16<T>::kElems; e < E; e += 32 * Vec16<T>::kElems)
-            *reinterpret_cast<uint4*>(row + e) = make_uint4(0, 0, 0, 0);
-    } else {
-        for (int e = lane; e < E; e += 32) store_grad(row + e, 0.0f);
-    }
+    const int lane = threadIdx.x & 31, tokens = 32 / lanes;
+    const int64_t t0 = (static_cast<int64_t>(blockIdx.x) * kGateWarps + (threadIdx.x >> 5)) * tokens;
+    if (t0 >= T_) return;
+    const int k = lane & (lanes - 1);
+    const int64_t t = t0 + lane / lanes;
     int id = -1;
     float g = 0.0f, w = 0.0f;
-    if (lane < K) {
-        id = ids[t * K + lane];
-        g = grad_w[t * K + lane];
-        w = weights[t * K + lane];
+    if (k < K && t < T_) {
+        id = ids[t * K + k];
+        g = grad_w[t * K + k];
+        w = weights[t * K + k];
         if (id < 0 || id >= E) {
             flag_error(err_word, COBALT_DEVERR_BAD_EXPERT_ID);
             id = -1;
         }
     }
-    const float dot = warp_sum(g * w);
+    float top = 0.0f;
+    if (sigmoid && k == 0 && id >= 0) top = load_logit(logits + t * E + id);
+    // the zeros of the warp's rows, which lie one after another
+    const int64_t count = (T_ - t0 < tokens ? T_ - t0 : tokens) * E;
+    T* rows = grad_logits + t0 * E;
+    if (kVector) {                                          // rows are whole 16-byte vectors
+        for (int64_t e = lane * Vec16<T>::kElems; e < count; e += 32 * Vec16<T>::kElems)
+            *reinterpret_cast<uint4*>(rows + e) = make_uint4(0, 0, 0, 0);
+    } else {
+        for (int64_t e = lane; e < count; e += 32) store_grad(rows + e, 0.0f);
+    }
+    float dot = g * w;
+    for (int off = 1; off < lanes; off <<= 1) dot += __shfl_xor_sync(kAll, dot, off);
     float d = w * (g - dot);
     if (sigmoid) {
-        float total = 0.0f;
-        if (lane == 0 && id >= 0 && w > 0.0f) total = 1.0f / (1.0f + expf(-load_logit(logits + t * E + id))) / w;
-        total = __shfl_sync(kAll, total, 0);
+        float total = w > 0.0f && id >= 0 ? 1.0f / (1.0f + expf(-top)) / w : 0.0f;       // of the first lane
+        total = __shfl_sync(kAll, total, lane & ~(lanes - 1));
         d *= 1.0f - w * total;
     }
     __syncwarp();                                           // the zeros of other lanes come before the chosen values
-    if (id >= 0) store_grad(row + id, d);
+    if (id >= 0) store_grad(grad_logits + t * E + id, d);
 }
 
 static int check_gate(int64_t T, int32_t E, int32_t K, int32_t dtype, uint32_t flags)
@@ -222,17 +288,49 @@ static int check_gate(int64_t T, int32_t E, int32_t K, int32_t dtype, uint32_t f
     return COBALT_OK;
 }
 
+static int power_of_two(int k)
+{
+    int n = 1;
+    while (n < k) n *= 2;
+    return n;
+}
+
+template <typename T, int kChunk, int L>
+static bool launch_gate_lanes(const T* l, int64_t T_, int E, int K, bool sigmoid, int32_t* ids, float* w, cudaStream_t s)
+{
+    const int64_t per_cta = static_cast<int64_t>(kGateWarps) * (32 / L);
+    const unsigned grid = static_cast<unsigned>((T_ + per_cta - 1) / per_cta);
+#define COBALT_GATE(VPL)                                                                                          \
+    do {                                                                                                          \
+        gate_topk_kernel<T, L, VPL, kChunk><<<grid, kGateThreads, 0, s>>>(l, T_, E, K, sigmoid, ids, w);          \
+        return true;                                                                                              \
+    } while (0)
+    if constexpr (L < 32) {                                 // 32 lanes only take what is too long for 16
+        if constexpr (kChunk <= 4)
+            if (E <= 4 * L) COBALT_GATE(4);
+        if (E <= 8 * L) COBALT_GATE(8);
+        if (E <= 16 * L) COBALT_GATE(16);
+    }
+    if (E <= 32 * L) COBALT_GATE(32);
+#undef COBALT_GATE
+    return false;
+}
+
+// As few lanes a token as hold its K chosen and, at 32 logits a lane, its row.
+template <typename T, int kChunk>
+static void launch_gate_chunk(const T* l, int64_t T_, int E, int K, bool sigmoid, int32_t* ids, float* w, cudaStream_t s)
+{
+    if (K <= 8 && launch_gate_lanes<T, kChunk, 8>(l, T_, E, K, sigmoid, ids, w, s)) return;
+    if (launch_gate_lanes<T, kChunk, 16>(l, T_, E, K, sigmoid, ids, w, s)) return;
+    (void)launch_gate_lanes<T, kChunk, 32>(l, T_, E, K, sigmoid, ids, w, s);
+}
+
 template <typename T>
 static void launch_gate(const void* logits, int64_t T_, int E, int K, bool sigmoid, int32_t* ids, float* w, cudaStream_t s)
 {
-    const unsigned grid = static_cast<unsigned>((T_ + kGateWarps - 1) / kGateWarps);
     const T* l = static_cast<const T*>(logits);
-    if (E <= 32) gate_topk_kernel<T, 1><<<grid, kGateThreads, 0, s>>>(l, T_, E, K, sigmoid, ids, w);
-    else if (E <= 64) gate_topk_kernel<T, 2><<<grid, kGateThreads, 0, s>>>(l, T_, E, K, sigmoid, ids, w);
-    else if (E <= 128) gate_topk_kernel<T, 4><<<grid, kGateThreads, 0, s>>>(l, T_, E, K, sigmoid, ids, w);
-    else if (E <= 256) gate_topk_kernel<T, 8><<<grid, kGateThreads, 0, s>>>(l, T_, E, K, sigmoid, ids, w);
-    else if (E <= 512) gate_topk_kernel<T, 16><<<grid, kGateThreads, 0, s>>>(l, T_, E, K, sigmoid, ids, w);
-    else gate_topk_kernel<T, 32><<<grid, kGateThreads, 0, s>>>(l, T_, E, K, sigmoid, ids, w);
+    if (E % Vec16<T>::kElems == 0) launch_gate_chunk<T, Vec16<T>::kElems>(l, T_, E, K, sigmoid, ids, w, s);
+    else launch_gate_chunk<T, 1>(l, T_, E, K, sigmoid, ids, w, s);
 }
 
 }  // namespace cobalt
@@ -271,12 +369,14 @@ int cobalt_gate_topk_backward(const float* grad_gate_w, const void* logits, cons
     uint32_t* err_word = nullptr;
     rc = device_error_word(&err_word);
     if (rc != COBALT_OK) return rc;
-    const unsigned grid = static_cast<unsigned>((T + kGateWarps - 1) / kGateWarps);
+    const int lanes = power_of_two(K);
+    const int64_t per_cta = static_cast<int64_t>(kGateWarps) * (32 / lanes);
+    const unsigned grid = static_cast<unsigned>((T + per_cta - 1) / per_cta);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool vector = E % (dtype == COBALT_BF16 ? 8 : 4) == 0;
 #define COBALT_GATE_BACKWARD(TT, VECTOR)                                                                                      \
     gate_topk_backward_kernel<TT, VECTOR><<<grid, kGateThreads, 0, s>>>(grad_gate_w, static_cast<const TT*>(logits), topk_ids, gate_w, \
-                                                                        T, E, K, sigmoid, static_cast<TT*>(grad_logits), err_word)
+                                                                        T, E, K, lanes, sigmoid, static_cast<TT*>(grad_logits), err_word)
     if (dtype == COBALT_BF16) {
         if (vector) COBALT_GATE_BACKWARD(__nv_bfloat16, true);
         else COBALT_GATE_BACKWARD(__nv_bfloat16, false);

@@ -22,10 +22,10 @@ constexpr int kNormMaxH = 16384;
 constexpr int kWarpRowVecs = 128;        // 16-byte vectors of a row up to which one warp takes it
 constexpr int kWarpRowThreads = 256;
 
-// Sums of v[0..N) over the CTA, N = 1, 2 or 4.  The first log2 N steps of the warp's tree halve the values a lane holds
+// post(sum) of v[0..N) over the CTA, N = 1, 2 or 4; what is computed of a sum is computed by one lane.  The first log2 N steps of the warp's tree halve the values a lane holds
 // (six shuffles for four values, not twenty).  `scratch`: N x 32 floats, not in use by an earlier call.
-template <int N>
-__device__ __forceinline__ void cta_sums(float (&v)[N], float* scratch)
+template <int N, typename Post>
+__device__ __forceinline__ void cta_sums(float (&v)[N], float* scratch, Post post)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     constexpr uint32_t kLanes = 0xFFFFFFFFu;
@@ -49,6 +49,7 @@ __device__ __forceinline__ void cta_sums(float (&v)[N], float* scratch)
         if (lane + 32 * k < warps * N) r += scratch[lane + 32 * k];
 #pragma unroll
     for (int off = N; off < 32; off <<= 1) r += __shfl_xor_sync(kLanes, r, off);
+    r = post(r);
 #pragma unroll
     for (int k = 0; k < N; ++k) v[k] = N == 1 ? r : __shfl_sync(kLanes, r, k);
 }
@@ -89,15 +90,16 @@ layer_norm_kernel(const T* x, const float* __restrict__ gamma, const float* __re
             for (int k = 0; k < N; ++k) mu[r] += f[k];
         }
     }
+    auto to_mean = [h](float sum) { return sum / h; };       // a division: a constant row has z = 0 exactly
+    auto to_rstd = [h, eps](float sum) { return 1.0f / sqrtf(sum / h + eps); };
     if constexpr (kCta) {
-        cta_sums<1>(mu, scratch[0]);
+        cta_sums<1>(mu, scratch[0], to_mean);
     } else {
 #pragma unroll
-        for (int r = 0; r < R; ++r) mu[r] = warp_sum(mu[r]);
+        for (int r = 0; r < R; ++r) mu[r] = to_mean(warp_sum(mu[r]));
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        mu[r] /= h;                          // a division: a constant row has z = 0 exactly
         rs[r] = 0.0f;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
@@ -110,14 +112,13 @@ layer_norm_kernel(const T* x, const float* __restrict__ gamma, const float* __re
         }
     }
     if constexpr (kCta) {
-        cta_sums<1>(rs, scratch[1]);
+        cta_sums<1>(rs, scratch[1], to_rstd);
     } else {
 #pragma unroll
-        for (int r = 0; r < R; ++r) rs[r] = warp_sum(rs[r]);
+        for (int r = 0; r < R; ++r) rs[r] = to_rstd(warp_sum(rs[r]));
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        rs[r] = 1.0f / sqrtf(rs[r] / h + eps);
         if (lane == 0 && r0 + r < rows) {
             mean[r0 + r] = mu[r];
             rstd[r0 + r] = rs[r];
@@ -237,9 +238,10 @@ __device__ __forceinline__ void bulk_load_row(uint32_t dst, const void* src, uin
                  : "memory");
 }
 
-// Threads of a ring CTA: 896 leave 72 registers each; fp32 rows of more than 3584 vectors need all 1024.
-template <int VPT>
-constexpr int kRingThreads = VPT == 4 ? 1024 : 896;
+// Most threads of a ring CTA: 896 leave 72 registers each; of the rows of more than 1792 vectors, fp32 ones have up to
+// 4096 and bf16 ones up to 2048.
+template <typename T, int VPT>
+constexpr int kRingThreads = VPT == 4 ? (sizeof(T) == 4 ? 1024 : 512) : 896;
 
 // The ring of a persistent CTA: turn i takes rows start + i step .. + R of `Tensors` tensors; a slot holds R rows of the
 // first tensor, then R rows of the second.
@@ -282,7 +284,7 @@ struct RowRing {
 
 // Forward: gamma and beta of the thread's columns stay in registers, its part of the R rows too.
 template <typename T, int VPT, int R>
-__global__ void __launch_bounds__(kRingThreads<VPT>)
+__global__ void __launch_bounds__(kRingThreads<T, VPT>)
 layer_norm_ring_kernel(const T* x, const float* __restrict__ gamma, const float* __restrict__ beta, int64_t rows, int H, float eps, T* y,
                        float* __restrict__ mean, float* __restrict__ rstd, int slots, uint32_t* __restrict__ err_word)
 {
@@ -332,12 +334,11 @@ layer_norm_ring_kernel(const T* x, const float* __restrict__ gamma, const float*
             }
             mu[r] = acc.v.x + acc.v.y;
         }
-        cta_sums<R>(mu, scratch[0]);
+        cta_sums<R>(mu, scratch[0], [h](float sum) { return sum / h; });       // a division: a constant row has z = 0 exactly
         // behind that barrier every thread has its part of the slot in registers
         if (tid == 0 && turn + slots < ring.turns) ring.load(turn + slots, s);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            mu[r] /= h;                      // a division: a constant row has z = 0 exactly
             Pair acc = pair(0.0f);
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
@@ -353,10 +354,9 @@ layer_norm_ring_kernel(const T* x, const float* __restrict__ gamma, const float*
             }
             rs[r] = acc.v.x + acc.v.y;
         }
-        cta_sums<R>(rs, scratch[1]);
+        cta_sums<R>(rs, scratch[1], [h, eps](float sum) { return 1.0f / sqrtf(sum / h + eps); });
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            rs[r] = 1.0f / sqrtf(rs[r] / h + eps);
             if (r0 + r >= rows) continue;
             if (tid == 0) {
                 mean[r0 + r] = mu[r];
@@ -386,7 +386,7 @@ layer_norm_ring_kernel(const T* x, const float* __restrict__ gamma, const float*
 
 // Backward: partial: [CTAs][2][H].
 template <typename T, int VPT, int R>
-__global__ void __launch_bounds__(kRingThreads<VPT>)
+__global__ void __launch_bounds__(kRingThreads<T, VPT>)
 layer_norm_backward_ring_kernel(const T* grad_y, const T* __restrict__ x, const float* __restrict__ gamma, const float* __restrict__ mean,
                                 const float* __restrict__ rstd, int64_t rows, int H, T* grad_x, float* __restrict__ partial, int slots,
                                 uint32_t* __restrict__ err_word)
@@ -394,6 +394,7 @@ layer_norm_backward_ring_kernel(const T* grad_y, const T* __restrict__ x, const 
     constexpr int N = Vec16<T>::kElems;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ float scratch[2][2 * R * 32];
+    __shared__ float2 stats[2][R];
     __shared__ volatile int dead;
     const int tid = threadIdx.x, n_vec = H / N;
     const float inv_h = 1.0f / static_cast<float>(H);
@@ -413,12 +414,11 @@ layer_norm_backward_ring_kernel(const T* grad_y, const T* __restrict__ x, const 
             db[i][k / 2] = pair(0.0f);
         }
     }
-    float mu[R], rs[R];
-#pragma unroll
-    for (int j = 0; j < R; ++j) {
-        mu[j] = ring.start + j < rows ? __ldg(mean + ring.start + j) : 0.0f;
-        rs[j] = ring.start + j < rows ? __ldg(rstd + ring.start + j) : 0.0f;
-    }
+    // mean and rstd of a turn's rows: read two turns ahead by the first R threads, in shared memory one turn ahead
+    auto row_stats = [&](int64_t r) { return tid < R && r < rows ? make_float2(__ldg(mean + r), __ldg(rstd + r)) : make_float2(0.0f, 0.0f); };
+    if (tid < R) stats[0][tid] = row_stats(ring.start + tid);
+    float2 ahead = row_stats(ring.start + ring.step + tid);
+    __syncthreads();
     int s = 0, before = 0;
     uint32_t phase = 0;
     for (int64_t turn = 0; turn < ring.turns; ++turn) {
@@ -428,9 +428,11 @@ layer_norm_backward_ring_kernel(const T* grad_y, const T* __restrict__ x, const 
             flag_error(err_word, COBALT_DEVERR_WAIT_TIMEOUT);
         }
         const uint8_t* slot = smem + static_cast<size_t>(s) * ring.slot_bytes();
-        float sum[2 * R];
+        float sum[2 * R], mu[R], rs[R];
 #pragma unroll
         for (int j = 0; j < R; ++j) {
+            mu[j] = stats[turn & 1][j].x;
+            rs[j] = stats[turn & 1][j].y;
             Pair s1 = pair(0.0f), s2 = pair(0.0f);
             if (r + j < rows) {
 #pragma unroll
@@ -454,20 +456,15 @@ layer_norm_backward_ring_kernel(const T* grad_y, const T* __restrict__ x, const 
             sum[2 * j] = s1.v.x + s1.v.y;
             sum[2 * j + 1] = s2.v.x + s2.v.y;
         }
-        float next_mu[R], next_rs[R];
-#pragma unroll
-        for (int j = 0; j < R; ++j) {
-            const bool more = r + ring.step + j < rows;
-            next_mu[j] = more ? __ldg(mean + r + ring.step + j) : 0.0f;
-            next_rs[j] = more ? __ldg(rstd + r + ring.step + j) : 0.0f;
-        }
-        cta_sums<2 * R>(sum, scratch[turn & 1]);
+        if (tid < R) stats[(turn + 1) & 1][tid] = ahead;     // last read before the barrier of the turn before
+        ahead = row_stats(r + 2 * ring.step + tid);
+        cta_sums<2 * R>(sum, scratch[turn & 1], [inv_h](float total) { return total * inv_h; });
         // behind that barrier every thread is done with the slot before this one
         if (tid == 0 && slots > 1 && turn > 0 && turn - 1 + slots < ring.turns) ring.load(turn - 1 + slots, before);
 #pragma unroll
         for (int j = 0; j < R; ++j) {
             if (r + j >= rows) continue;
-            const float c1 = sum[2 * j] * inv_h, c2 = sum[2 * j + 1] * inv_h;
+            const float c1 = sum[2 * j], c2 = sum[2 * j + 1];
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
                 const int at = tid + i * blockDim.x;
@@ -487,11 +484,6 @@ layer_norm_backward_ring_kernel(const T* grad_y, const T* __restrict__ x, const 
         if (slots == 1) {                    // the slot itself comes next
             __syncthreads();
             if (tid == 0 && turn + 1 < ring.turns) ring.load(turn + 1, 0);
-        }
-#pragma unroll
-        for (int j = 0; j < R; ++j) {
-            mu[j] = next_mu[j];
-            rs[j] = next_rs[j];
         }
         before = s;
         if (++s == slots) {
