@@ -6,6 +6,7 @@ binding is loaded on first use and raises if the shared library is missing: ther
 CPU or eager fallback.
 """
 import importlib
+import types
 
 __all__ = ["binding", "build"]
 
@@ -15,6 +16,9 @@ def __getattr__(name):
         return importlib.import_module(f"{__name__}.{name}")
     binding = importlib.import_module(f"{__name__}.binding")
     try:
-        return getattr(binding, name)
+        value = getattr(binding, name)
     except AttributeError:
         raise AttributeError(f"module {__name__!r} has no attribute {name!r}") from None
+    if isinstance(value, types.FunctionType):      # the next call finds it without the import machinery (about 1 us)
+        globals()[name] = value
+    return value

@@ -18,6 +18,9 @@
 //   - CTAs are persistent, a pair for every two SMs, and deal the tiles of all slots round robin; the tile list is
 //     built on the device from dest_offsets (no copy to the host).
 //
+// A call of a few rows (a token of generation) is bound by streaming the weights of their experts once; tiles leave SMs
+// without work there, so each warp takes one feature of one row on the fp32 units instead (ffn_few_rows_kernel).
+//
 // Every wait is bounded: when one runs out the kernel sets COBALT_DEVERR_WAIT_TIMEOUT, drains its copies, frees its
 // tensor memory and returns.
 #include "numeric.cuh"
@@ -211,7 +214,7 @@ enum Stage {
 
 struct ProductArgs {
     PlanView plan;
-    int E, M, N;             // features of the M side; columns of the N side (kWeights)
+    int P, E, M, N;          // rows; experts; features of the M side; columns of the N side (kWeights)
     int K;                   // summed extent (row stages)
     int F;                   // kUp, kDownBackward: columns of act
     bf16* out;               // kUp: act; kDown, kUpBackward, kWeights: the result; kDownBackward: grad_pre
@@ -389,8 +392,13 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         for (int t = first; t < tiles && ok; t += step) {
             const Tile w = next;
             const int half = w.n / 2, m0 = w.m0 + static_cast<int>(rank) * 128;
-            const int boxes_b = (half + 63) / 64, n0 = w.n0 + static_cast<int>(rank) * half;    // kWeights
+            // Boxes wholly outside their tensor are left out: what is in the ring slot then only reaches features, columns or
+            // rows of the tile that are not stored.
+            const int n0 = w.n0 + static_cast<int>(rank) * half;                               // kWeights
+            const int boxes_a = m0 >= p.M ? 0 : !S::kAMn || m0 + 64 >= p.M ? 1 : 2;
+            const int boxes_b = n0 >= p.N ? 0 : min((half + 63) / 64, (p.N - n0 + 63) / 64);    // kWeights
             const int row0 = w.row0 + static_cast<int>(rank) * half;                           // row stages
+            const int parts_b = min(half, (p.P - row0 + 15) / 16 * 16);                         // rows to load, by 16
             int seg = w.seg, done = 0;
             int2 rows = w.head;
             if (w.blocks == 0 && t + step < tiles) next = get_tile<kStage>(p, t + step);
@@ -401,23 +409,23 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 const uint32_t bar = full + 8 * ring.slot, a = base + ring.slot * kSlotBytes, b = a + kHalfBytes;
                 if (elect_one()) {
                     if (kStage == kWeights) {
-                        barrier_expect(bar, (2 + boxes_b) * kBoxBytes);
-                        tma_load_2d(a, &map_a, bar, policy_a, m0, rows.x + done);
-                        tma_load_2d(a + kBoxBytes, &map_a, bar, policy_a, m0 + 64, rows.x + done);
-                        tma_load_2d(b, &map_b, bar, policy_b, n0, rows.x + done);
+                        barrier_expect(bar, (boxes_a + boxes_b) * kBoxBytes);
+                        if (boxes_a > 0) tma_load_2d(a, &map_a, bar, policy_a, m0, rows.x + done);
+                        if (boxes_a > 1) tma_load_2d(a + kBoxBytes, &map_a, bar, policy_a, m0 + 64, rows.x + done);
+                        if (boxes_b > 0) tma_load_2d(b, &map_b, bar, policy_b, n0, rows.x + done);
                         if (boxes_b > 1) tma_load_2d(b + kBoxBytes, &map_b, bar, policy_b, n0 + 64, rows.x + done);
                     } else {
-                        barrier_expect(bar, kHalfBytes + half * kBlockK * 2);
-                        if (kStage == kUp) tma_load_5d(a, &map_a, bar, policy_a, k * kBlockK, 0, 0, m0 / 16, w.expert);
-                        if (kStage == kDown) tma_load_3d(a, &map_a, bar, policy_a, k * kBlockK, m0, w.expert);
+                        barrier_expect(bar, boxes_a * (S::kAMn ? kBoxBytes : kHalfBytes) + max(parts_b, 0) * kBlockK * 2);
+                        if (kStage == kUp && boxes_a > 0) tma_load_5d(a, &map_a, bar, policy_a, k * kBlockK, 0, 0, m0 / 16, w.expert);
+                        if (kStage == kDown && boxes_a > 0) tma_load_3d(a, &map_a, bar, policy_a, k * kBlockK, m0, w.expert);
                         if (S::kAMn) {
-                            tma_load_3d(a, &map_a, bar, policy_a, m0, k * kBlockK, w.expert);
-                            tma_load_3d(a + kBoxBytes, &map_a, bar, policy_a, m0 + 64, k * kBlockK, w.expert);
+                            if (boxes_a > 0) tma_load_3d(a, &map_a, bar, policy_a, m0, k * kBlockK, w.expert);
+                            if (boxes_a > 1) tma_load_3d(a + kBoxBytes, &map_a, bar, policy_a, m0 + 64, k * kBlockK, w.expert);
                         }
-                        if (half == 128)
+                        if (parts_b == 128)
                             tma_load_2d(b, &map_b, bar, policy_b, k * kBlockK, row0);
                         else
-                            for (int i = 0; i < half; i += 16) tma_load_2d(b + i * 128, &map_b_part, bar, policy_b, k * kBlockK, row0 + i);
+                            for (int i = 0; i < parts_b; i += 16) tma_load_2d(b + i * 128, &map_b_part, bar, policy_b, k * kBlockK, row0 + i);
                     }
                 }
                 __syncwarp();
@@ -685,7 +693,146 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     if (warp == 1) tmem_free_pair(tmem, 512);
 }
 
+// ---- a few rows ---------------------------------------------------------------------------------------------------
+
+constexpr int kFewThreads = 256;
+constexpr int kFewResident = 4;          // CTAs of the grid an SM
+// Most rows of a call that takes this form.  Measured with every row at another expert (us, this form / tiles): H 7168, F 2048:
+// 1 row 22 / 45, 6 rows 88 / 110, 8 rows 115 / 128, 12 rows 167 / 178; H 2048, F 1408: 8 rows 33 / 41.  Rows at one expert read its
+// weights once each here: 8 rows 82 / 45.
+constexpr int kFewRows = 8;
+constexpr int kFewVecs = 2048;           // longest summed extent, in 16-byte vectors: a row in shared memory
+
+__device__ __forceinline__ float dot8(const uint4& w, const uint4& x, float acc)
+{
+    float a[8], b[8];
+    Vec16<bf16>::unpack(w, a);
+    Vec16<bf16>::unpack(x, b);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc = fmaf(a[i], b[i], acc);
+    return acc;
+}
+
+// Expert of row p: that of the lowest slot whose range holds the row, -1 for none.  Bad ranges are flagged by one CTA, as
+// in the plan.  The three loads of a slot are under way together.
+__device__ __forceinline__ int expert_of_row(const uint32_t* offsets, const int32_t* slot_expert, int P, int D, int E, int p, bool check,
+                                             uint32_t* err_word, int* found)
+{
+    if (threadIdx.x == 0) *found = 0x7FFFFFFF;
+    __syncthreads();
+    for (int d = threadIdx.x; d < D; d += kFewThreads) {
+        const uint32_t a = __ldg(offsets + d), b = __ldg(offsets + d + 1);
+        const int e = __ldg(slot_expert + d);
+        const bool valid = e >= 0 && e < E;
+        // slot in the upper bits, so that the lowest one wins; expert + 1 below (E <= 1024), 0 for none
+        if (a <= static_cast<uint32_t>(p) && static_cast<uint32_t>(p) < b) atomicMin(found, d << 12 | (valid ? e + 1 : 0));
+        if (check) {
+            const uint32_t n = static_cast<uint32_t>(P), lo = min(a, n), hi = min(b, n);
+            if (b < a || b > n || (hi > lo && !valid)) flag_error(err_word, COBALT_DEVERR_BAD_SLOT);
+        }
+    }
+    __syncthreads();
+    return *found == 0x7FFFFFFF ? -1 : (*found & 4095) - 1;
+}
+
+// kUp: act (and pre) of one row, a warp a feature: its gate and its up row of the weights.  kDown: out of one row, a warp
+// two neighbouring features.  blockIdx.y is the row.  Summed in fp32, a lane 8 values of every 256.
+template <int kStage>
+__global__ void __launch_bounds__(kFewThreads)
+ffn_few_rows_kernel(const bf16* x, const bf16* weights, const uint32_t* __restrict__ offsets,
+                    const int32_t* __restrict__ slot_expert, int P, int D, int E, int M, int K, bf16* __restrict__ out,
+                    bf16* __restrict__ pre, uint32_t* __restrict__ err_word)
+{
+    extern __shared__ __align__(16) uint4 x_row[];           // [K / 8]
+    __shared__ int found;
+    const int lane = threadIdx.x & 31, row = blockIdx.y, vecs = K / 8;
+    const int tasks = kStage == kUp ? M : M / 2, step = gridDim.x * (kFewThreads / 32);
+    if (kStage == kUp) launch_dependents();
+    const int e = expert_of_row(offsets, slot_expert, P, D, E, row, kStage == kUp && blockIdx.x == 0 && row == 0, err_word, &found);
+    if (e < 0) return;                                        // a row of no slot (uniform over the CTA)
+    constexpr int kAhead = 4;                                 // vectors of each weight row a lane has in flight
+    uint4 a[kAhead], b[kAhead];
+    // Two rows of the weights: gate and up of feature m, or features m and m + 1.  Task and vector are clamped, not
+    // guarded: every address that is formed lies in the expert's weights (what a lane has too many counts as zero).
+    auto load = [&](int task, int base) {
+        const int own = min(task, tasks - 1);
+        const int64_t m = kStage == kUp ? static_cast<int64_t>(e) * 2 * M + own : static_cast<int64_t>(e) * M + 2 * own;
+        const bf16 *w0 = weights + m * K, *w1 = w0 + (kStage == kUp ? static_cast<int64_t>(M) : 1) * K;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int v = min(base + lane + 32 * i, vecs - 1);
+            a[i] = ld_once16(w0 + 8 * v);
+            b[i] = ld_once16(w1 + 8 * v);
+        }
+    };
+    int task = blockIdx.x * (kFewThreads / 32) + (threadIdx.x >> 5);
+    load(task, 0);
+    if (kStage == kDown) wait_for_prior_kernel();             // x is what the kernel before writes; the weights are not
+    for (int i = threadIdx.x; i < vecs; i += kFewThreads) x_row[i] = ld_once16(x + static_cast<int64_t>(row) * K + i * 8);
+    __syncthreads();
+    for (; task < tasks; task += step) {
+        float s0 = 0.0f, s1 = 0.0f;
+        for (int base = 0; base < vecs; base += 32 * kAhead) {
+            uint4 ca[kAhead], cb[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                ca[i] = a[i];
+                cb[i] = b[i];
+            }
+            // the next vectors, or the first ones of the next task
+            const bool last = base + 32 * kAhead >= vecs;
+            if (!last || task + step < tasks) load(last ? task + step : task, last ? 0 : base + 32 * kAhead);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int v = base + lane + 32 * i;
+                if (v < vecs) {
+                    s0 = dot8(ca[i], x_row[v], s0);
+                    s1 = dot8(cb[i], x_row[v], s1);
+                }
+            }
+        }
+        s0 = warp_sum(s0);
+        s1 = warp_sum(s1);
+        if (lane == 0) {
+            if (kStage == kUp) {
+                out[static_cast<int64_t>(row) * M + task] = __float2bfloat16_rn(s0 * sigmoid(s0) * s1);
+                if (pre) {
+                    pre[static_cast<int64_t>(row) * 2 * M + task] = __float2bfloat16_rn(s0);
+                    pre[static_cast<int64_t>(row) * 2 * M + M + task] = __float2bfloat16_rn(s1);
+                }
+            } else {                                          // (M is a multiple of 8)
+                *reinterpret_cast<uint32_t*>(out + static_cast<int64_t>(row) * M + 2 * task) = pack2(s0, s1);
+            }
+        }
+    }
+}
+
 // ---- host side ----------------------------------------------------------------------------------------------------
+
+template <int kStage>
+static int launch_few_rows(const void* x, const void* weights, const uint32_t* offsets, const int32_t* slot_expert, int P, int D, int E,
+                           int M, int K, void* out, void* pre, uint32_t* err_word, cudaStream_t s)
+{
+    const size_t smem = static_cast<size_t>(K) * sizeof(bf16);
+    const int tasks = kStage == kUp ? M : M / 2, warps = kFewThreads / 32;
+    int sms = 0;
+    const int rc = sm_count(&sms);
+    if (rc != COBALT_OK) return rc;
+    // about one wave: a CTA looks its row up once and takes several features
+    const int all = (tasks + warps - 1) / warps, most = kFewResident * sms / P > 1 ? kFewResident * sms / P : 1;
+    cudaLaunchAttribute attr;
+    set_programmatic_launch(&attr, true);
+    cudaLaunchConfig_t config = {};
+    config.gridDim = dim3(all < most ? all : most, P);
+    config.blockDim = dim3(kFewThreads);
+    config.dynamicSmemBytes = smem;
+    config.stream = s;
+    config.attrs = &attr;
+    config.numAttrs = kStage == kDown ? 1 : 0;
+    COBALT_CUDA_TRY(cudaLaunchKernelEx(&config, ffn_few_rows_kernel<kStage>, static_cast<const bf16*>(x), static_cast<const bf16*>(weights),
+                                       offsets, slot_expert, P, D, E, M, K, static_cast<bf16*>(out), static_cast<bf16*>(pre), err_word));
+    return COBALT_OK;
+}
 
 typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -827,10 +974,15 @@ int cobalt_expert_ffn(const void* rows, const uint32_t* dest_offsets, const int3
     if (!workspace || workspace_bytes < plan_bytes(P, D, E)) return COBALT_ERR_WORKSPACE_TOO_SMALL;
     ProductArgs p = {};
     COBALT_TRY(device_error_word(&p.err_word));
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (P <= kFewRows && H <= 8 * kFewVecs && F <= 8 * kFewVecs) {
+        COBALT_TRY(launch_few_rows<kUp>(rows, w_gate_up, dest_offsets, slot_expert, static_cast<int>(P), D, E, F, H, act, pre, p.err_word, s));
+        return launch_few_rows<kDown>(act, w_down, dest_offsets, slot_expert, static_cast<int>(P), D, E, H, F, out, nullptr, p.err_word, s);
+    }
     p.plan = plan_view(workspace, P, D, E);
+    p.P = static_cast<int>(P);
     p.E = E;
     p.F = F;
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int64_t row_tiles = max_row_tiles(P, static_cast<int>(P < D ? P : D));
 
     CUtensorMap a, b, part;
@@ -878,6 +1030,7 @@ int cobalt_expert_ffn_backward(const void* grad_out, const void* rows, const uin
         return COBALT_OK;
     }
     p.plan = plan_view(workspace, P, D, E);
+    p.P = static_cast<int>(P);
     p.E = E;
     p.F = F;
     const int64_t row_tiles = max_row_tiles(P, static_cast<int>(P < D ? P : D));

@@ -132,6 +132,26 @@ def test_expert_ffn_against_plain(counts, experts, E, H, F):
         assert torch.equal(alone[k].view(torch.int16), r[k].view(torch.int16))
 
 
+@pytest.mark.parametrize("P", [1, 2, 7, 8, 9, 16])
+@pytest.mark.parametrize("H,F", [(8, 8), (264, 200), (2048, 1408), (1032, 16)])
+def test_a_few_rows(P, H, F):
+    """Calls of one row up to the size where tiles take over, rows outside the slots and bad slots among them."""
+    import paper_2609_36959_b200 as cb
+    counts = [0, 1, 0, P - 1, 0]
+    c = _case(P + H, counts, [2, 0, 1, 3, -1], 4, H, F, lead=0, tail=0)
+    _check(c, _run(c))
+    both = _case(P + F, [P // 2, P - P // 2], [1, 1], 2, H, F)      # replicas of one expert
+    _check(both, _run(both))
+    if P > 2:
+        c = _case(P, [1, P - 2], [0, 1], 2, H, F, lead=1)
+        _check(c, _run(c))
+        good = _run(c)
+        c["slots"] = torch.tensor([0, 7], dtype=torch.int32, device="cuda")
+        r = _run(c, backward=False)
+        assert cb.read_and_clear_device_error() == cb.DEVERR_BAD_SLOT
+        assert torch.equal(r["out"][1:2], good["out"][1:2]) and (r["out"][2:] == 7.0).all()
+
+
 def test_rows_outside_the_slots_stay_untouched():
     c = _case(5, [40, 0, 3, 130], [1, 0, 2, 0], 3, 128, 64, lead=13, tail=21)
     _check(c, _run(c))
