@@ -19,7 +19,7 @@
 namespace cobalt {
 
 constexpr int kNormMaxH = 16384;
-constexpr int kWarpRowVecs = 128;        // 16-byte vectors of a row up to which one warp takes it
+constexpr int kWarpRowVecs = 128;        // 16-byte vectors of a row up to which one warp takes it (forward: 256)
 constexpr int kWarpRowThreads = 256;
 
 // post(sum) of v[0..N) over the CTA, N = 1, 2 or 4; what is computed of a sum is computed by one lane.  The first log2 N steps of the warp's tree halve the values a lane holds
@@ -154,6 +154,7 @@ layer_norm_backward_warp_kernel(const T* grad_y, const T* __restrict__ x, const 
 {
     constexpr int N = Vec16<T>::kElems;
     extern __shared__ float sums[];          // [2][H]
+    launch_dependents();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = kWarpRowThreads / 32;
     const int n_vec = H / N;
     const float inv_h = 1.0f / static_cast<float>(H);
@@ -398,6 +399,7 @@ layer_norm_backward_ring_kernel(const T* grad_y, const T* __restrict__ x, const 
     __shared__ volatile int dead;
     const int tid = threadIdx.x, n_vec = H / N;
     const float inv_h = 1.0f / static_cast<float>(H);
+    launch_dependents();
     if (tid == 0) dead = 0;
     RowRing<T, R, 2> ring;
     ring.src[0] = x;
@@ -512,9 +514,10 @@ layer_norm_backward_ring_kernel(const T* grad_y, const T* __restrict__ x, const 
 
 // grad_gamma and grad_beta: column sums of the parts, 32 columns a CTA, every warp a slice of the parts.
 __global__ void __launch_bounds__(1024)
-layer_norm_reduce_kernel(const float* __restrict__ partial, int parts, int H, float* __restrict__ grad_gamma,
+layer_norm_reduce_kernel(const float* partial, int parts, int H, float* __restrict__ grad_gamma,
                          float* __restrict__ grad_beta)
 {
+    wait_for_prior_kernel();                             // the parts
     __shared__ float slice[32][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int col = blockIdx.x * 32 + lane;              // over 2H columns: gamma's, then beta's
@@ -540,16 +543,16 @@ struct NormShape {
     bool cta;
 };
 
-// One CTA a row without the ring: a thread holds one vector up to 256 of them, two up to 2048, four above.
+// Without the ring: one warp a row up to eight vectors a lane, one CTA above that, two vectors a thread up to 2048 of them.
 static NormShape norm_shape(int n_vec)
 {
     NormShape s;
-    s.cta = n_vec > kWarpRowVecs;
+    s.cta = n_vec > 2 * kWarpRowVecs;
     if (!s.cta) {
         s.threads = kWarpRowThreads;
-        s.vpt = n_vec <= 32 ? 1 : n_vec <= 64 ? 2 : 4;
+        s.vpt = n_vec <= 32 ? 1 : n_vec <= 64 ? 2 : n_vec <= 128 ? 4 : 8;
     } else {
-        s.vpt = n_vec <= 256 ? 1 : n_vec <= 2048 ? 2 : 4;
+        s.vpt = n_vec <= 2048 ? 2 : 4;
         s.threads = ((n_vec + s.vpt - 1) / s.vpt + 31) / 32 * 32;
     }
     return s;
@@ -571,7 +574,7 @@ static RingShape ring_shape(int H, int elem_bytes, int tensors, int most_rows)
     const int n_vec = H * elem_bytes / 16;
     s.vpt = n_vec <= 896 ? 1 : n_vec <= 1792 ? 2 : 4;
     s.threads = ((n_vec + s.vpt - 1) / s.vpt + 31) / 32 * 32;
-    s.resident = s.threads <= 256 ? 4 : s.threads <= 512 ? 2 : 1;
+    s.resident = s.threads <= 512 ? 2 : 1;
     const size_t row = static_cast<size_t>(tensors) * H * elem_bytes, room = kRingBytes / s.resident;
     s.rows = s.vpt == 1 && 2 * most_rows * row <= room ? most_rows : 1;
     s.slots = static_cast<int>(room / (s.rows * row));
@@ -658,8 +661,7 @@ static int launch_norm(const T* x, const float* gamma, const float* beta, int64_
 #define COBALT_NORM_FWD(VPT, R, CTA) \
     layer_norm_kernel<T, VPT, R, CTA><<<grid, shape.threads, 0, s>>>(x, gamma, beta, rows, H, eps, y, mean, rstd)
     if (shape.cta) {
-        if (shape.vpt == 1) COBALT_NORM_FWD(1, 1, true);
-        else if (shape.vpt == 2) COBALT_NORM_FWD(2, 1, true);
+        if (shape.vpt == 2) COBALT_NORM_FWD(2, 1, true);
         else if constexpr (sizeof(T) == 4) COBALT_NORM_FWD(4, 1, true);
     } else if (several) {
         if (shape.vpt == 1) COBALT_NORM_FWD(1, 4, false);
@@ -667,7 +669,8 @@ static int launch_norm(const T* x, const float* gamma, const float* beta, int64_
     } else {
         if (shape.vpt == 1) COBALT_NORM_FWD(1, 1, false);
         else if (shape.vpt == 2) COBALT_NORM_FWD(2, 1, false);
-        else COBALT_NORM_FWD(4, 1, false);
+        else if (shape.vpt == 4) COBALT_NORM_FWD(4, 1, false);
+        else COBALT_NORM_FWD(8, 1, false);
     }
 #undef COBALT_NORM_FWD
     return COBALT_OK;
@@ -774,9 +777,15 @@ int cobalt_layer_norm_backward(const void* grad_y, const void* x, const float* g
                                   static_cast<float*>(grad_x), partial, sms, &parts, err_word, s);
     if (rc != COBALT_OK) return rc;
     COBALT_CUDA_TRY(cudaGetLastError());
-    layer_norm_reduce_kernel<<<static_cast<unsigned>((2 * H + 31) / 32), 1024, 0, s>>>(partial, parts, H, grad_gamma,
-                                                                                       grad_beta);
-    COBALT_CUDA_TRY(cudaGetLastError());
+    cudaLaunchAttribute attr;
+    set_programmatic_launch(&attr, true);
+    cudaLaunchConfig_t config = {};
+    config.gridDim = dim3((2 * H + 31) / 32);
+    config.blockDim = dim3(1024);
+    config.stream = s;
+    config.attrs = &attr;
+    config.numAttrs = 1;
+    COBALT_CUDA_TRY(cudaLaunchKernelEx(&config, layer_norm_reduce_kernel, static_cast<const float*>(partial), parts, H, grad_gamma, grad_beta));
     return COBALT_OK;
 }
 
