@@ -12,7 +12,7 @@ __all__ = ["binding", "build"]
 
 
 def __getattr__(name):
-    if name in ("binding", "build", "router"):
+    if name in ("binding", "build", "router", "moe"):
         return importlib.import_module(f"{__name__}.{name}")
     binding = importlib.import_module(f"{__name__}.binding")
     try:
