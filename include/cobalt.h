@@ -386,15 +386,16 @@ int cobalt_gate_topk_backward(const float* grad_gate_w, const void* logits, cons
  * whose expert is slot_expert[d] (device int32 [D]; -1 = empty).  With e that expert, w_gate_up bf16
  * [E, 2F, H] (F gate rows, then F up rows) and w_down bf16 [E, H, F]:
  *   pre = x w_gate_up[e]^T = (g, u)     act = g * sigmoid(g) * u     out = act w_down[e]^T
- * act bf16 [P, F] is scratch for inference and an input of the backward call; pre bf16 [P, 2F] is only
- * needed by the backward call (NULL for inference).
- * Backward: grad_pre bf16 [P, 2F] is scratch (it may be `pre` itself, which is then overwritten);
+ * act bf16 [P, F] is scratch for inference and an input of the backward call; pre [P, 2F] (two bytes an
+ * element, in a format of the library's own: a sign, six exponent and nine mantissa bits, saturating at 2^32) is
+ * only needed by the backward call (NULL for inference).
+ * Backward: grad_pre [P, 2F] is scratch (it may be `pre` itself, which is then overwritten);
  *   d_act = grad_out w_down[e]     d_u = d_act g s     d_g = d_act u s (1 + g (1 - s)),  s = sigmoid(g)
  *   grad_rows = (d_g, d_u) w_gate_up[e]      grad_w_gate_up[e] = sum (d_g, d_u)^T x
  *   grad_w_down[e] = sum grad_out^T act      sums over the rows of ALL slots that hold e
  * Weight gradients are bf16 in the weights' layout and overwritten (0 for an expert without rows);
- * any of the three results may be NULL, but not all.  act and the pre-activations are rounded to bf16
- * once each, products accumulate in fp32.  Rows outside [dest_offsets[0], dest_offsets[D]) are neither
+ * any of the three results may be NULL, but not all.  act is rounded to bf16 once, products accumulate
+ * in fp32.  Rows outside [dest_offsets[0], dest_offsets[D]) are neither
  * read nor written.  dest_offsets must not decrease or pass P (clamped), and a slot with rows must hold an
  * expert in [0, E): otherwise COBALT_DEVERR_BAD_SLOT is set and its rows are skipped.
  * H and F multiples of 8, at most COBALT_FFN_MAX_WIDTH; D <= 4096, E <= 1024, P < 2^31. */

@@ -649,7 +649,8 @@ def expert_ffn(rows: torch.Tensor, dest_offsets: torch.Tensor, slot_expert: torc
 
     rows, out bfloat16 [P, H] in the order of the send buffer; dest_offsets int32 [D+1] and slot_expert int32 [D] on
     the device; w_gate_up [E, 2F, H] (gate rows first), w_down [E, H, F].  act [P, F] and, if a backward pass follows,
-    pre [P, 2F] are written and kept for expert_ffn_backward."""
+    pre [P, 2F] are written and kept for expert_ffn_backward (pre holds 16-bit codes of the library's own, not bfloat16
+    values)."""
     P, H, E, F, D = _ffn_sizes(rows, dest_offsets, slot_expert, w_gate_up, w_down, "expert_ffn")
     _check(_lib.cobalt_expert_ffn(_ptr(rows, torch.bfloat16, "rows"), _ptr(dest_offsets, torch.int32, "dest_offsets"),
                                   _ptr(slot_expert, torch.int32, "slot_expert"), P, D, E, H, F,

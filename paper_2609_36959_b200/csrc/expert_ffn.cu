@@ -318,8 +318,35 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi)
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-__device__ __forceinline__ float low_half(uint32_t v) { return __uint_as_float(v << 16); }
-__device__ __forceinline__ float high_half(uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); }
+// The saved pre-activations are 16-bit floats of one sign, six exponent and nine mantissa bits: four times finer than
+// bf16 (whose rounding here alone made the gradients of rows and weights 1.3 times as inexact as the two roundings that
+// they cannot do without: 3.0e-3 against 2.4e-3 in the 2-norm), over 2^-30 .. 2^32, with gradual underflow to 2^-39.
+// Larger values become the largest one, a NaN stays a NaN.  Scaled by 2^-96, such a value is an fp32 number whose
+// exponent fits six bits.
+constexpr uint32_t kPreNan = 0x7E00u;
+
+__device__ __forceinline__ uint32_t pack_pre(float lo, float hi)
+{
+    const float scale = __uint_as_float(0x0F800000u);                       // 2^-96
+    const float most = __uint_as_float((62u << 23) | (0x1FFu << 14));
+    float v[2] = {lo * scale, hi * scale};
+    uint32_t c[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        asm("min.NaN.f32 %0, %0, %1;" : "+f"(v[i]) : "f"(most));
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(v[i]) : "f"(-most));
+        const uint32_t b = __float_as_uint(v[i]) + 0x2000u;                 // to nearest, halves up
+        c[i] = v[i] == v[i] ? ((b >> 14) & 0x7FFFu) | ((b >> 16) & 0x8000u) : kPreNan;
+    }
+    return c[0] | (c[1] << 16);
+}
+
+__device__ __forceinline__ float unpack_pre(uint32_t code)                  // in the upper half of the word
+{
+    const float scale = __uint_as_float(0x6F800000u);                       // 2^96
+    const float v = __uint_as_float(((code >> 2) & 0x1FFFC000u) | (code & 0x80000000u)) * scale;
+    return ((code >> 16) & kPreNan) == kPreNan ? __uint_as_float(0x7FC00000u) : v;
+}
 
 // 1 / (1 + exp(-g)): the fast exponential and division are good to a few units of fp32, far below the bf16 results
 __device__ __forceinline__ float sigmoid(float g) { return __fdividef(1.0f, 1.0f + __expf(-g)); }
@@ -536,8 +563,10 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                             const float g0 = __uint_as_float(r[4 * i]), g1 = __uint_as_float(r[4 * i + 1]);
                             const float u0 = __uint_as_float(r[4 * i + 2]), u1 = __uint_as_float(r[4 * i + 3]);
                             a[i] = pack2(g0 * sigmoid(g0) * u0, g1 * sigmoid(g1) * u1);
-                            g[i] = pack2(g0, g1);
-                            u[i] = pack2(u0, u1);
+                            if (p.pre) {
+                                g[i] = pack_pre(g0, g1);
+                                u[i] = pack_pre(u0, u1);
+                            }
                         }
                         const uint32_t at = buf + lane * S::kPitch + (16 * quarter + 8 * hl) * 2;
                         stmatrix_x4_trans(at, a[0], a[1], a[2], a[3]);
@@ -624,7 +653,7 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                             ldmatrix_x4_trans(at + 256, uv);
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
-                                const float g0 = low_half(gv[i]), g1 = high_half(gv[i]), u0 = low_half(uv[i]), u1 = high_half(uv[i]);
+                                const float g0 = unpack_pre(gv[i] << 16), g1 = unpack_pre(gv[i]), u0 = unpack_pre(uv[i] << 16), u1 = unpack_pre(uv[i]);
                                 const float d0 = __uint_as_float(r[4 * i + 2 * o]), d1 = __uint_as_float(r[4 * i + 2 * o + 1]);
                                 const float s0 = sigmoid(g0), s1 = sigmoid(g1);
                                 gv[i] = pack2(d0 * u0 * s0 * (1.0f + g0 * (1.0f - s0)), d1 * u1 * s1 * (1.0f + g1 * (1.0f - s1)));
@@ -797,8 +826,10 @@ ffn_few_rows_kernel(const bf16* x, const bf16* weights, const uint32_t* __restri
             if (kStage == kUp) {
                 out[static_cast<int64_t>(row) * M + task] = __float2bfloat16_rn(s0 * sigmoid(s0) * s1);
                 if (pre) {
-                    pre[static_cast<int64_t>(row) * 2 * M + task] = __float2bfloat16_rn(s0);
-                    pre[static_cast<int64_t>(row) * 2 * M + M + task] = __float2bfloat16_rn(s1);
+                    const uint32_t both = pack_pre(s0, s1);
+                    uint16_t* at = reinterpret_cast<uint16_t*>(pre) + static_cast<int64_t>(row) * 2 * M + task;
+                    at[0] = static_cast<uint16_t>(both);
+                    at[M] = static_cast<uint16_t>(both >> 16);
                 }
             } else {                                          // (M is a multiple of 8)
                 *reinterpret_cast<uint32_t*>(out + static_cast<int64_t>(row) * M + 2 * task) = pack2(s0, s1);

@@ -83,6 +83,14 @@ def ffn_backward(dy, rows, ranges, w_gate_up, w_down):
     return dict(dx=dx, dgu=dgu, ddn=ddn, act=act, pre=pre, d_act=d_act, d_pre=d_pre)
 
 
+def decode_pre(codes):
+    """Values of the saved pre-activations: one sign, six exponent (bias 31) and nine mantissa bits."""
+    c = codes.view(torch.int16).to(torch.int64) & 0xFFFF
+    sign, e, m = 1.0 - 2.0 * (c >> 15), (c >> 9) & 63, (c & 511).to(F64)
+    value = torch.where(e > 0, torch.exp2((e - 31).to(F64)) * (1 + m / 512), 2.0 ** -30 * m / 512)
+    return torch.where(e == 63, torch.full_like(value, math.nan), sign * value)
+
+
 def philox_words(counter, key):
     """Philox-4x32-10 on Python integers: the four words of one counter (c0..c3) under key (k0, k1)."""
     c, k, low = list(counter), list(key), 0xFFFFFFFF

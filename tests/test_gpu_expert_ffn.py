@@ -1,7 +1,8 @@
 """The experts' feed-forward block and its gradients against the 64-bit plain form.
 
-Bounds, element by element (h = 2^-9, half a unit of bf16; u = 2^-24): the kernel rounds act, pre and grad_pre to bf16
-once each and accumulates in fp32, so
+Bounds, element by element (h = 2^-9, half a unit of bf16; q = 2^-10, half a unit of the nine-bit mantissa of pre, with
+2^-40 where it underflows; u = 2^-24): the kernel rounds act and grad_pre to bf16 and pre to its own 16 bits once each and
+accumulates in fp32, so
   act    h |act| + what g and u are off by, (H u) (|x| |W|^T) times the slopes, at most 1.1 |u| and |silu(g)|
   out    sum |d act| |Wd| + F u sum |act| |Wd| + h |out|
   d_pre  d_act is off by H u (|dy| |Wd|); from the rounded g and u: |d_act| (1.1 h |g|) for d_u and
@@ -15,6 +16,7 @@ import layer_util as L
 
 pytestmark = pytest.mark.gpu
 h, U = L.ULP16, L.ULP32
+q, TINY = 2.0 ** -10, 2.0 ** -40
 
 
 def _case(seed, counts, experts, E, H, F, lead=0, tail=0, scale=1.0):
@@ -83,10 +85,10 @@ def _check(c, r, backward=True):
         within("out", r["out"][a:z], ref[a:z], t_act @ WD[e].t() + F * U * (act[a:z].abs() @ WD[e].t()) + h * ref[a:z].abs())
         if not backward:
             continue
-        within("pre", r["pre"][a:z] if r["pre"] is not r["d_pre"] else pre[a:z], pre[a:z], off + h * pre[a:z].abs())
+        within("pre", L.decode_pre(r["pre"][a:z]) if r["pre"] is not r["d_pre"] else pre[a:z], pre[a:z], off + q * pre[a:z].abs() + TINY)
         da = b["d_act"][a:z].abs()
         off_da = H * U * (DY[a:z] @ WD[e])
-        og, ou = off[:, :F] + h * g.abs(), off[:, F:] + h * u.abs()
+        og, ou = off[:, :F] + q * g.abs() + TINY, off[:, F:] + q * u.abs() + TINY
         t_g = off_da * 1.1 * u.abs() + da * (1.1 * ou + 0.5 * u.abs() * og) + h * b["d_pre"][a:z, :F].abs()
         t_u = off_da * silu + da * 1.1 * og + h * b["d_pre"][a:z, F:].abs()
         t = torch.cat([t_g, t_u], 1)
@@ -201,6 +203,33 @@ def test_non_finite_rows_stay_in_their_slot(bad):
     for k in ("out", "dx"):
         for a, b in ((0, 37), (87, 157)):
             assert torch.equal(r[k][a:b].view(torch.int16), clean[k][a:b].view(torch.int16)), k
+
+
+@pytest.mark.parametrize("P", [3, 40])
+def test_saved_preactivations_over_their_range(P):
+    """Values from below the finest code to above the largest: nearest codes, gradual underflow, saturation, NaN kept."""
+    import paper_2609_36959_b200 as cb
+    H = F = 8
+    scale = [2.0 ** e for e in (-45, -39, -30, 0, 20, 31, 40, 100)]
+    rows = torch.zeros((P, H), dtype=torch.bfloat16, device="cuda")
+    for i in range(P):
+        rows[i, i % H] = 1.0 + (i % 5) * 0.375
+    wgu = torch.zeros((1, 2 * F, H), dtype=torch.bfloat16, device="cuda")
+    for f in range(2 * F):
+        for k in range(H):
+            wgu[0, f, k] = scale[(f + k) % 8] * (1 if f % 2 else -1)
+    wgu[0, 3, 1] = float("nan")
+    act, out, pre = (torch.full((P, n), 7.0, dtype=torch.bfloat16, device="cuda") for n in (F, H, 2 * F))
+    ws = torch.empty(cb.expert_ffn_workspace_bytes(P, 1, 1, H, F), dtype=torch.uint8, device="cuda")
+    cb.expert_ffn(rows, torch.tensor([0, P], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"), wgu,
+                  torch.zeros((1, H, F), dtype=torch.bfloat16, device="cuda"), act, out, ws, pre=pre)
+    got = L.decode_pre(pre)
+    want = torch.stack([wgu[0].double() @ rows[i].double() for i in range(P)])
+    nan = torch.isnan(want)
+    assert torch.equal(torch.isnan(got), nan)
+    most = 2.0 ** 31 * (1 + 511 / 512)
+    want = want.clamp(-most, most)
+    assert ((got - want)[~nan].abs() <= (q * want.abs() + TINY)[~nan]).all()
 
 
 def test_large_gates_saturate_without_nan():
