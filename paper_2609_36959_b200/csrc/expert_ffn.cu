@@ -13,7 +13,7 @@
 //     every tile: a slot of 40 rows costs 64, not 128 or 256, and a single token streams the weights once.
 //     The weight gradients have features on both sides and the rows as the summed extent.
 //   - Warp 0 of each CTA feeds a ring of 64-deep blocks by tensor-map loads, warp 1 of the leading CTA issues the
-//     products, warps 2 to 5 run the epilogue.  Two accumulators (2 x 256 of 512 columns) let the epilogue of a tile
+//     products, warps 2 to 5 run the epilogue (and warp 6 clears the ragged ends of slots for the weight gradients).  Two accumulators (2 x 256 of 512 columns) let the epilogue of a tile
 //     run under the products of the next one.
 //   - CTAs are persistent, a pair for every two SMs, and deal the tiles of all slots round robin; the tile list is
 //     built on the device from dest_offsets (no copy to the host).
@@ -223,7 +223,8 @@ struct ProductArgs {
     uint32_t* err_word;
 };
 
-constexpr int kProductThreads = 192;
+template <int kStage>
+constexpr int kProductThreads = kStage == 4 /* kWeights */ ? 224 : 192;
 constexpr int kHalfBytes = 128 * kBlockK * 2;      // one operand of one CTA in a ring slot: 128 x 64 bf16
 constexpr int kSlotBytes = 2 * kHalfBytes;
 constexpr int kBoxBytes = 64 * kBlockK * 2;        // MN-major box: 64 values of M or N x 64 of k
@@ -365,7 +366,7 @@ __device__ __forceinline__ void clear_tail(uint32_t slot_addr, int boxes_b, int 
 }
 
 template <int kStage>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads<kStage>, 1)
 ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                    const __grid_constant__ CUtensorMap map_b_part, const __grid_constant__ ProductArgs p)
 {
@@ -383,7 +384,8 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         for (int i = 0; i < S::kRing; ++i) {
             barrier_init(full + 8 * i, 1);       // this CTA's loads
             barrier_init(empty + 8 * i, 1);      // the products that read the slot are done
-            barrier_init(relay + 8 * i, 1);      // leading CTA: the other CTA's loads
+            // leading CTA: the other CTA's loads; kWeights: both CTAs' loads, with what is past a slot's end cleared
+            barrier_init(relay + 8 * i, S::kWeightsStage ? 2 : 1);
         }
         for (int i = 0; i < 2; ++i) {
             barrier_init(acc_full + 8 * i, 1);
@@ -472,34 +474,28 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         }
         __syncwarp();
     } else if (warp == 1) {
-        // ---- products (leading CTA); the other CTA passes on that its loads have landed -------------------------
+        // ---- products (leading CTA); in a row stage the other CTA passes on that its loads have landed -----------
         Ring ring;
         int turn = 0;                            // accumulators used so far
+        const bool part = rank == 0 || !S::kWeightsStage;
         Tile next = {};
-        if (first < tiles) next = get_tile<kStage>(p, first);
-        for (int t = first; t < tiles && ok; t += step) {
+        if (part && first < tiles) next = get_tile<kStage>(p, first);
+        for (int t = first; t < tiles && ok && part; t += step) {
             const Tile w = next;
             if (w.blocks == 0) {
                 if (t + step < tiles) next = get_tile<kStage>(p, t + step);
                 continue;
             }
-            const int half = w.n / 2;
             const uint32_t acc = turn & 1, d = tmem + acc * 256;
             const uint32_t idesc = instruction_descriptor(w.n, S::kAMn, S::kWeightsStage);
             if (rank == 0) {
                 if (!(ok = barrier_wait(acc_empty + 8 * acc, ((turn >> 1) & 1) ^ 1))) break;
                 tmem_fence_after();
             }
-            int seg = w.seg, left = w.head.y;
             for (int k = 0; k < w.blocks; ++k) {
                 if (k == w.blocks / 2 && t + step < tiles) next = get_tile<kStage>(p, t + step);
-                if (!(ok = barrier_wait(full + 8 * ring.slot, ring.phase))) break;
+                if (!S::kWeightsStage && !(ok = barrier_wait(full + 8 * ring.slot, ring.phase))) break;
                 const uint32_t a = base + ring.slot * kSlotBytes;
-                if (kStage == kWeights) {
-                    if (left < kBlockK) clear_tail(a, (half + 63) / 64, left, lane);
-                    left -= kBlockK;
-                    if (left <= 0 && ++seg < w.seg_end) left = p.plan.segs[seg].y;
-                }
                 if (rank != 0) {
                     if (elect_one()) barrier_arrive_cluster(peer_address(relay + 8 * ring.slot, 0));
                     __syncwarp();
@@ -533,6 +529,31 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 (void)barrier_wait(drain, 0);
             }
         }
+        __syncwarp();
+    } else if (S::kWeightsStage && warp == 6) {
+        // ---- weight gradients: k rows past the end of a slot, which belong to the next one, are cleared here, ahead of
+        // the products and off their path; then the leading CTA hears of the block
+        Ring ring;
+        Tile next = {};
+        if (first < tiles) next = get_tile<kStage>(p, first);
+        const uint32_t heard = peer_address(relay, 0);
+        for (int t = first; t < tiles && ok; t += step) {
+            const Tile w = next;
+            if (w.blocks == 0 && t + step < tiles) next = get_tile<kStage>(p, t + step);
+            const int boxes_b = (w.n / 2 + 63) / 64;
+            int seg = w.seg, left = w.head.y;
+            for (int k = 0; k < w.blocks; ++k) {
+                if (k == w.blocks / 2 && t + step < tiles) next = get_tile<kStage>(p, t + step);
+                if (!(ok = barrier_wait(full + 8 * ring.slot, ring.phase))) break;
+                if (left < kBlockK) clear_tail(base + ring.slot * kSlotBytes, boxes_b, left, lane);
+                if (elect_one()) barrier_arrive_cluster(heard + 8 * ring.slot);
+                __syncwarp();
+                left -= kBlockK;
+                if (left <= 0 && ++seg < w.seg_end) left = p.plan.segs[seg].y;
+                ring.next<S::kRing>();
+            }
+        }
+        if (!ok && lane == 0) flag_error(p.err_word, COBALT_DEVERR_WAIT_TIMEOUT);
         __syncwarp();
     } else {
         // ---- epilogue: quarter of the tensor memory lanes by warp, 32 accumulator columns at a time ---------------
@@ -942,7 +963,7 @@ static int launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUte
     set_programmatic_launch(&attr, true);
     cudaLaunchConfig_t config = {};
     config.gridDim = dim3(static_cast<unsigned>(2 * (pairs < 1 ? 1 : pairs)));
-    config.blockDim = dim3(kProductThreads);
+    config.blockDim = dim3(kProductThreads<kStage>);
     config.dynamicSmemBytes = Shape<kStage>::kSmem;
     config.stream = s;
     config.attrs = &attr;
@@ -958,6 +979,7 @@ static int launch_plan(const uint32_t* offsets, const int32_t* slot_expert, int6
     const int rc = ensure_kernel_attributes(reinterpret_cast<const void*>(ffn_plan_kernel),
                                             plan_smem(COBALT_MAX_DESTS, COBALT_MAX_EXPERTS), false);
     if (rc != COBALT_OK) return rc;
+    // (fewer threads for few slots: 12.7 us against 5 at 32 slots, one warp then writes all the tiles)
     ffn_plan_kernel<<<1, kPlanThreads, bytes, s>>>(offsets, slot_expert, P, D, p.E, p.plan, p.err_word);
     COBALT_CUDA_TRY(cudaGetLastError());
     return COBALT_OK;
