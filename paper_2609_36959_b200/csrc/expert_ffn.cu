@@ -752,10 +752,10 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 // ---- a few rows ---------------------------------------------------------------------------------------------------
 
 constexpr int kFewThreads = 256;
-constexpr int kFewResident = 4;          // CTAs of the grid an SM
+constexpr int kFewResident = 4;          // CTAs an SM
 // Most rows of a call that takes this form.  Measured with every row at another expert (us, this form / tiles): H 7168, F 2048:
-// 1 row 22 / 45, 6 rows 88 / 110, 8 rows 115 / 128, 12 rows 167 / 178; H 2048, F 1408: 8 rows 33 / 41.  Rows at one expert read its
-// weights once each here: 8 rows 82 / 45.
+// 1 row 23 / 45, 6 rows 85 / 110, 8 rows 113 / 128; H 2048, F 1408: 6 rows 23.7 / 31.2, 8 rows 28.8 / 41.  Beyond, the tiles read a
+// shared expert's weights once, this form once a row: 8 rows at one expert 84 / 45.
 constexpr int kFewRows = 8;
 constexpr int kFewVecs = 2048;           // longest summed extent, in 16-byte vectors: a row in shared memory
 
@@ -794,7 +794,7 @@ __device__ __forceinline__ int expert_of_row(const uint32_t* offsets, const int3
 // kUp: act (and pre) of one row, a warp a feature: its gate and its up row of the weights.  kDown: out of one row, a warp
 // two neighbouring features.  blockIdx.y is the row.  Summed in fp32, a lane 8 values of every 256.
 template <int kStage>
-__global__ void __launch_bounds__(kFewThreads)
+__global__ void __launch_bounds__(kFewThreads, kFewResident)
 ffn_few_rows_kernel(const bf16* x, const bf16* weights, const uint32_t* __restrict__ offsets,
                     const int32_t* __restrict__ slot_expert, int P, int D, int E, int M, int K, bf16* __restrict__ out,
                     bf16* __restrict__ pre, uint32_t* __restrict__ err_word)
@@ -809,7 +809,9 @@ ffn_few_rows_kernel(const bf16* x, const bf16* weights, const uint32_t* __restri
         if (kStage == kDown) wait_for_prior_kernel();         // this kernel ends after the one before it all the same
         return;
     }
-    constexpr int kAhead = 4;                                 // vectors of each weight row a lane has in flight
+    // Vectors of each weight row a lane has in flight.  Two, with four CTAs an SM in one wave, against four with two CTAs:
+    // 6 rows, H 2048, F 1408 23.7 us against 26.6; 8 rows, H 7168, F 2048 the same 113 us.
+    constexpr int kAhead = 2;
     uint4 a[kAhead], b[kAhead];
     // Two rows of the weights: gate and up of feature m, or features m and m + 1.  Task and vector are clamped, not
     // guarded: every address that is formed lies in the expert's weights (what a lane has too many counts as zero).
@@ -879,7 +881,7 @@ static int launch_few_rows(const void* x, const void* weights, const uint32_t* o
     int sms = 0;
     const int rc = sm_count(&sms);
     if (rc != COBALT_OK) return rc;
-    // about one wave: a CTA looks its row up once and takes several features
+    // one wave: a CTA looks its row up once and takes several features
     const int all = (tasks + warps - 1) / warps, most = kFewResident * sms / P > 1 ? kFewResident * sms / P : 1;
     cudaLaunchAttribute attr;
     set_programmatic_launch(&attr, true);
