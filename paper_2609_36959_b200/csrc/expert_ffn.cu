@@ -13,8 +13,8 @@
 //     every tile: a slot of 40 rows costs 64, not 128 or 256, and a single token streams the weights once.
 //     The weight gradients have features on both sides and the rows as the summed extent.
 //   - Warp 0 of each CTA feeds a ring of 64-deep blocks by tensor-map loads, warp 1 of the leading CTA issues the
-//     products, warps 2 to 5 run the epilogue (and warp 6 clears the ragged ends of slots for the weight gradients).  Two accumulators (2 x 256 of 512 columns) let the epilogue of a tile
-//     run under the products of the next one.
+//     products, warps 2 to 5 run the epilogue (and warp 6 clears the ragged ends of slots for the weight gradients).
+//     Two accumulators (2 x 256 of 512 columns) let the epilogue of a tile run under the products of the next one.
 //   - CTAs are persistent, a pair for every two SMs, and deal the tiles of all slots round robin; the tile list is
 //     built on the device from dest_offsets (no copy to the host).
 //
@@ -1003,8 +1003,8 @@ static int64_t m_tiles(int64_t features) { return (features + kTileM - 1) / kTil
 static int check_ffn(int64_t P, int32_t D, int32_t E, int32_t H, int32_t F)
 {
     if (P < 0 || D < 1 || E < 1 || H < 1 || F < 1) return COBALT_ERR_INVALID_ARG;
-    // (row coordinates of a tile may pass the last row by up to a tile)
-    if (P >= (1ll << 31) - 1024 || D > COBALT_MAX_DESTS || E > COBALT_MAX_EXPERTS || H % 8 != 0 || F % 8 != 0 || H > COBALT_FFN_MAX_WIDTH ||
+    // (row coordinates of a tile may pass the last row by up to a tile, and an expert's tile count has to fit 23 bits)
+    if (P > (1ll << 31) - (1ll << 21) || D > COBALT_MAX_DESTS || E > COBALT_MAX_EXPERTS || H % 8 != 0 || F % 8 != 0 || H > COBALT_FFN_MAX_WIDTH ||
         F > COBALT_FFN_MAX_WIDTH)
         return COBALT_ERR_UNSUPPORTED;
     return COBALT_OK;
