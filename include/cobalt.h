@@ -396,8 +396,9 @@ int cobalt_gate_topk_backward(const float* grad_gate_w, const void* logits, cons
  * Weight gradients are bf16 in the weights' layout and overwritten (0 for an expert without rows);
  * any of the three results may be NULL, but not all.  act is rounded to bf16 once, products accumulate
  * in fp32.  Rows outside [dest_offsets[0], dest_offsets[D]) are neither
- * read nor written.  dest_offsets must not decrease or pass P (clamped), and a slot with rows must hold an
- * expert in [0, E): otherwise COBALT_DEVERR_BAD_SLOT is set and its rows are skipped.
+ * read nor written.  dest_offsets must not decrease or pass P, and a slot with rows must hold an expert in [0, E):
+ * otherwise COBALT_DEVERR_BAD_SLOT is set.  Offsets past P then count as P, offsets that decrease as their running maximum
+ * (a row is its first slot's, no row is two slots'), and rows of a slot without a valid expert are skipped.
  * H and F multiples of 8, at most COBALT_FFN_MAX_WIDTH; D <= 4096, E <= 1024, P <= 2^31 - 2^21. */
 #define COBALT_FFN_MAX_WIDTH 65536
 size_t cobalt_expert_ffn_workspace_bytes(int64_t P, int32_t D, int32_t E, int32_t H, int32_t F);

@@ -30,6 +30,7 @@
 #include <atomic>
 
 #include "numeric.cuh"
+#include "slot_ranges.h"
 #include "tcgen05.cuh"
 
 namespace cobalt {
@@ -51,7 +52,7 @@ struct PlanView {
     int2* segs;                          // [D] {first row, rows}, slots in ascending order
 };
 
-__host__ __device__ inline int64_t max_row_tiles(int64_t P, int D) { return P / kTileN + D; }
+__host__ __device__ inline int64_t max_row_tiles(int64_t P, int D) { return most_row_tiles(P, D, kTileN); }
 
 static size_t plan_bytes(int64_t P, int D, int E)
 {
@@ -109,7 +110,8 @@ __device__ __forceinline__ int block_prefix(int v, int* scratch, int* total)
 __host__ __device__ inline int plan_groups(int D) { return D <= kPlanThreads ? (D + 31) / 32 : kPlanThreads / 32; }
 static size_t plan_smem(int D, int E) { return 4 * (5 * static_cast<size_t>(D) + 4 * static_cast<size_t>(E)) + 2 * static_cast<size_t>(plan_groups(D)) * E; }
 
-// One CTA.  Offsets that decrease or pass P are clamped, rows of a slot without a valid expert skipped, both flagged.
+// One CTA.  Offsets that decrease are read as their running maximum (disjoint slots: what bounds the tile list, and keeps
+// two tiles from writing the same rows), those past P clamped, rows of a slot without a valid expert skipped; all flagged.
 // The slots with rows are sorted by expert (counting sort, stable), and row tiles listed in that order, so that the
 // slots of an expert's replicas share its weights in L2.
 __global__ void __launch_bounds__(kPlanThreads)
@@ -127,8 +129,10 @@ ffn_plan_kernel(const uint32_t* __restrict__ offsets, const int32_t* __restrict_
 
     for (int i = threadIdx.x; i < groups * E; i += kPlanThreads) group_count[i] = 0;
     for (int i = threadIdx.x; i < E; i += kPlanThreads) e_tiles[i] = e_blocks[i] = e_first[i] = 0;
+    bool decreases = false;
     for (int d = threadIdx.x; d < D; d += kPlanThreads) {
         const int64_t a = offsets[d], b = offsets[d + 1];
+        decreases |= b < a;
         const int64_t lo = a < P ? a : P, hi = b < P ? b : P;
         const int e = slot_expert[d];
         bool bad = b < a || b > P;
@@ -142,7 +146,13 @@ ffn_plan_kernel(const uint32_t* __restrict__ offsets, const int32_t* __restrict_
         s_rows[d] = rows;
         s_expert[d] = rows > 0 ? e : -1;
     }
-    __syncthreads();
+    if (__syncthreads_or(decreases)) {                                     // one thread: no call in order comes here
+        if (threadIdx.x == 0) {
+            const int64_t end = offsets[D];
+            make_slots_disjoint(D, static_cast<int32_t>(end < P ? end : P), s_first, s_rows, s_expert);
+        }
+        __syncthreads();
+    }
     if (warp < groups) {
         for (int d0 = warp * span; d0 < min(D, (warp + 1) * span); d0 += 32) {
             const int d = d0 + lane, e = d < D ? s_expert[d] : -1;
@@ -769,8 +779,9 @@ __device__ __forceinline__ float dot8(const uint4& w, const uint4& x, float acc)
     return acc;
 }
 
-// Expert of row p: that of the lowest slot whose range holds the row, -1 for none.  Bad ranges are flagged by one CTA, as
-// in the plan.  The three loads of a slot are under way together.
+// Expert of row p, -1 for none.  The row's slot is the first one that ends behind it, if the first slot starts no later:
+// the plan's rule, offsets as their running maximum.  Bad ranges are flagged by one CTA, as in the plan.  The three loads of
+// a slot are under way together.
 __device__ __forceinline__ int expert_of_row(const uint32_t* offsets, const int32_t* slot_expert, int P, int D, int E, int p, bool check,
                                              uint32_t* err_word, int* found)
 {
@@ -781,14 +792,14 @@ __device__ __forceinline__ int expert_of_row(const uint32_t* offsets, const int3
         const int e = __ldg(slot_expert + d);
         const bool valid = e >= 0 && e < E;
         // slot in the upper bits, so that the lowest one wins; expert + 1 below (E <= 1024), 0 for none
-        if (a <= static_cast<uint32_t>(p) && static_cast<uint32_t>(p) < b) atomicMin(found, d << 12 | (valid ? e + 1 : 0));
+        if (static_cast<uint32_t>(p) < b) atomicMin(found, d << 12 | (valid ? e + 1 : 0));
         if (check) {
             const uint32_t n = static_cast<uint32_t>(P), lo = min(a, n), hi = min(b, n);
             if (b < a || b > n || (hi > lo && !valid)) flag_error(err_word, COBALT_DEVERR_BAD_SLOT);
         }
     }
     __syncthreads();
-    return *found == 0x7FFFFFFF ? -1 : (*found & 4095) - 1;
+    return *found == 0x7FFFFFFF || __ldg(offsets) > static_cast<uint32_t>(p) ? -1 : (*found & 4095) - 1;
 }
 
 // kUp: act (and pre) of one row, a warp a feature: its gate and its up row of the weights.  kDown: out of one row, a warp
