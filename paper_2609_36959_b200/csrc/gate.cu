@@ -21,11 +21,14 @@ constexpr uint32_t kAll = 0xFFFFFFFFu;
 
 constexpr int kGateList = 64;                               // candidates of a token that are ranked directly
 
-// Unsigned integers in the order of the values: -inf < ... < -0 = +0 < ... < +inf < NaN (a NaN is chosen first and
-// shows in the weights).  The smallest key of a value is 0x007FFFFF (-inf), so 0 marks "taken or absent".
+// Unsigned integers in the order of the values: -inf < ... < -0 = +0 < ... < +inf (0xFF800000) < NaN (a NaN is chosen first
+// and shows in the weights).  The smallest key of a value is 0x007FFFFF (-inf), so 0 marks "taken or absent"; the largest
+// word is left free for "above every candidate".
+constexpr uint32_t kNanKey = 0xFFFFFFFEu;
+
 __device__ __forceinline__ uint32_t order_key(float v)
 {
-    if (v != v) return 0xFFFFFFFFu;
+    if (v != v) return kNanKey;
     const uint32_t b = __float_as_uint(v + 0.0f);          // -0 + 0 = +0
     return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
@@ -115,7 +118,7 @@ __device__ __forceinline__ unsigned long long candidate(float v, int id)
 template <int L, typename T>
 __device__ __noinline__ unsigned long long choose_by_rounds(const T* row, int E, int K, int sub)
 {
-    unsigned long long mine = 0, last = ~0ull;
+    unsigned long long mine = 0, last = ~0ull;               // above every candidate
     for (int k = 0; k < K; ++k) {
         unsigned long long best = 0;                        // the largest below the one before
         for (int e = sub; e < E; e += L) {
@@ -221,7 +224,7 @@ gate_topk_kernel(const T* __restrict__ logits, int64_t T_, int E, int K, bool si
         if (!ranked) mine = slow;
     }
     const uint32_t key = static_cast<uint32_t>(mine >> 32);
-    const float value = key == 0xFFFFFFFFu ? __int_as_float(0x7FC00000) : key_value(key);
+    const float value = key == kNanKey ? __int_as_float(0x7FC00000) : key_value(key);
     const float w = chosen_weight<L>(value, K, sub, sigmoid);
     if (sub < K && t < T_) {
         ids[t * K + sub] = static_cast<int>(~static_cast<uint32_t>(mine));
