@@ -5,8 +5,12 @@
 //   g  = dy gamma     dx = rstd (g - mean(g) - z mean(g z))      dgamma = sum_t dy z     dbeta = sum_t dy
 //
 // A row is read once and stays on the chip, so the variance is the sum of squares about the mean and not a
-// difference of two large sums.  All sums are fp32.  A group of threads owns a row: one warp while a lane needs at
-// most four 16-byte vectors, the whole CTA above that.
+// difference of two large sums.  All sums are fp32.  The fp32 sum of fp32 values is rounded, which would leave a row of
+// large equal values a z of its own; so their differences from that first mean are summed too, exactly where they are
+// small, and correct it:
+//   mu = mu1 + mean(d)    var = (sum d^2 - mean(d) sum d) / H    with d = x - mu1
+// (for bf16 values of one magnitude the first sum is exact: 8 + 14 bits).  A group of threads owns a row: one warp while a
+// lane needs at most four 16-byte vectors, the whole CTA above that.
 //
 // Rows of more than 128 vectors, many of them: persistent CTAs, a thread owns the same columns of every row (its gamma
 // and beta, or the sums of their gradients, stay in registers), and rows come in through a ring of bulk copies, so that
@@ -24,15 +28,34 @@ constexpr int kNormMaxH = 16384;
 constexpr int kWarpRowVecs = 128;        // 16-byte vectors of a row up to which one warp takes it (forward: 256)
 constexpr int kWarpRowThreads = 256;
 
-// post(sum) of v[0..N) over the CTA, N = 1, 2 or 4; what is computed of a sum is computed by one lane.  The first log2 N steps of the warp's tree halve the values a lane holds
-// (six shuffles for four values, not twenty).  `scratch`: N x 32 floats, not in use by an earlier call.
+// The mean's correction and 1 / sqrt(var + eps) from the sums of d and of d^2 (of h values).  The correction is a division:
+// exact for a constant row.  The other two are good to two units.
+__device__ __forceinline__ float mean_shift(float sum, float h) { return sum / h; }
+__device__ __forceinline__ float shifted_rstd(float shift, float sum, float squares, float inv_h, float eps)
+{
+    const float part = shift * sum;
+    float var = fabsf(part) < INFINITY ? squares - part : squares;     // where it overflows the squares have, too
+    if (var < 0.0f) var = 0.0f;                                        // rounding; a NaN stays
+    return rsqrtf(fmaf(var, inv_h, eps));
+}
+
+// post(sum) of v[0..N) over the CTA, N = 1, 2, 4 or 8; what is computed of a sum is computed by one lane (every lane l
+// calls post with the sum of value l % N).  The first log2 N steps of the warp's tree halve the values a lane holds (six
+// shuffles for four values, not twenty).  `scratch`: N x 32 floats, not in use by an earlier call.
 template <int N, typename Post>
 __device__ __forceinline__ void cta_sums(float (&v)[N], float* scratch, Post post)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     constexpr uint32_t kLanes = 0xFFFFFFFFu;
     float r;
-    if constexpr (N == 4) {
+    if constexpr (N == 8) {
+        float q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = ((lane & 1) ? v[2 * i + 1] : v[2 * i]) + __shfl_xor_sync(kLanes, (lane & 1) ? v[2 * i] : v[2 * i + 1], 1);
+        const float a = ((lane & 2) ? q[1] : q[0]) + __shfl_xor_sync(kLanes, (lane & 2) ? q[0] : q[1], 2);
+        const float b = ((lane & 2) ? q[3] : q[2]) + __shfl_xor_sync(kLanes, (lane & 2) ? q[2] : q[3], 2);
+        r = ((lane & 4) ? b : a) + __shfl_xor_sync(kLanes, (lane & 4) ? a : b, 4);
+    } else if constexpr (N == 4) {
         const float a = ((lane & 1) ? v[1] : v[0]) + __shfl_xor_sync(kLanes, (lane & 1) ? v[0] : v[1], 1);
         const float b = ((lane & 1) ? v[3] : v[2]) + __shfl_xor_sync(kLanes, (lane & 1) ? v[2] : v[3], 1);
         r = ((lane & 2) ? b : a) + __shfl_xor_sync(kLanes, (lane & 2) ? a : b, 2);
@@ -56,6 +79,22 @@ __device__ __forceinline__ void cta_sums(float (&v)[N], float* scratch, Post pos
     for (int k = 0; k < N; ++k) v[k] = N == 1 ? r : __shfl_sync(kLanes, r, k);
 }
 
+// post of cta_sums for sums of d (even) and of d^2 (odd) in turn: the mean's shift and rstd.
+struct ShiftAndRstd {
+    float h, inv_h, eps;
+    __device__ __forceinline__ float operator()(float sum) const
+    {
+        const float other = __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
+        const bool odd = threadIdx.x & 1;                              // (both by all lanes: a branch would run one after the other)
+        const float first = odd ? other : sum, squares = odd ? sum : other, shift = mean_shift(first, h);
+        const float rstd = shifted_rstd(shift, first, squares, inv_h, eps);
+        return odd ? rstd : shift;
+    }
+};
+
+template <typename T>
+constexpr bool kShiftMean = sizeof(T) == 4;
+
 // R rows a group, VPT vectors of each row a thread.
 template <typename T, int VPT, int R, bool kCta>
 __global__ void __launch_bounds__(1024)
@@ -63,12 +102,12 @@ layer_norm_kernel(const T* x, const float* __restrict__ gamma, const float* __re
                   float* __restrict__ mean, float* __restrict__ rstd)
 {
     constexpr int N = Vec16<T>::kElems;
-    __shared__ float scratch[2][32];
+    __shared__ float scratch[2][kShiftMean<T> ? 64 : 32];
     static_assert(!kCta || R == 1, "a CTA takes one row here");
     const int group = kCta ? blockDim.x : 32, lane = kCta ? threadIdx.x : (threadIdx.x & 31);
     const int groups = kCta ? 1 : (blockDim.x >> 5), own = kCta ? 0 : (threadIdx.x >> 5);
     const int n_vec = H / N;
-    const float h = static_cast<float>(H);
+    const float h = static_cast<float>(H), inv_h = 1.0f / h;
     const int64_t r0 = (static_cast<int64_t>(blockIdx.x) * groups + own) * R;
     if (r0 >= rows) return;
     uint4 v[R][VPT];
@@ -92,7 +131,8 @@ layer_norm_kernel(const T* x, const float* __restrict__ gamma, const float* __re
             for (int k = 0; k < N; ++k) mu[r] += f[k];
         }
     }
-    auto to_mean = [h](float sum) { return sum / h; };       // a division: a constant row has z = 0 exactly
+    // (a division where no correction follows: exact for a constant row of bf16 values)
+    auto to_mean = [h, inv_h](float sum) { return kShiftMean<T> ? sum * inv_h : sum / h; };
     auto to_rstd = [h, eps](float sum) { return 1.0f / sqrtf(sum / h + eps); };
     if constexpr (kCta) {
         cta_sums<1>(mu, scratch[0], to_mean);
@@ -100,21 +140,38 @@ layer_norm_kernel(const T* x, const float* __restrict__ gamma, const float* __re
 #pragma unroll
         for (int r = 0; r < R; ++r) mu[r] = to_mean(warp_sum(mu[r]));
     }
+    float first[R];                          // kShiftMean: sums of the differences
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        rs[r] = 0.0f;
+        rs[r] = first[r] = 0.0f;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             if (lane + i * group < n_vec) {
                 float f[N];
                 Vec16<T>::unpack(v[r][i], f);
 #pragma unroll
-                for (int k = 0; k < N; ++k) rs[r] = fmaf(f[k] - mu[r], f[k] - mu[r], rs[r]);
+                for (int k = 0; k < N; ++k) {
+                    const float d = f[k] - mu[r];
+                    if (kShiftMean<T>) first[r] += d;
+                    rs[r] = fmaf(d, d, rs[r]);
+                }
             }
         }
     }
-    if constexpr (kCta) {
+    if constexpr (kCta && kShiftMean<T>) {
+        float both[2] = {first[0], rs[0]};
+        cta_sums<2>(both, scratch[1], ShiftAndRstd{h, inv_h, eps});
+        mu[0] += both[0];
+        rs[0] = both[1];
+    } else if constexpr (kCta) {
         cta_sums<1>(rs, scratch[1], to_rstd);
+    } else if constexpr (kShiftMean<T>) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const float sum = warp_sum(first[r]), shift = mean_shift(sum, h);
+            rs[r] = shifted_rstd(shift, sum, warp_sum(rs[r]), inv_h, eps);
+            mu[r] += shift;
+        }
     } else {
 #pragma unroll
         for (int r = 0; r < R; ++r) rs[r] = to_rstd(warp_sum(rs[r]));
@@ -293,10 +350,10 @@ layer_norm_ring_kernel(const T* x, const float* __restrict__ gamma, const float*
 {
     constexpr int N = Vec16<T>::kElems;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ float scratch[2][R * 32];
+    __shared__ float scratch[2][(kShiftMean<T> ? 2 : 1) * R * 32];
     __shared__ volatile int dead;            // a wait ran out: the rest is not waited for
     const int tid = threadIdx.x, n_vec = H / N;
-    const float h = static_cast<float>(H);
+    const float h = static_cast<float>(H), inv_h = 1.0f / h;
     if (tid == 0) dead = 0;
     RowRing<T, R, 1> ring;
     ring.src[0] = x;
@@ -337,12 +394,13 @@ layer_norm_ring_kernel(const T* x, const float* __restrict__ gamma, const float*
             }
             mu[r] = acc.v.x + acc.v.y;
         }
-        cta_sums<R>(mu, scratch[0], [h](float sum) { return sum / h; });       // a division: a constant row has z = 0 exactly
+        cta_sums<R>(mu, scratch[0], [h, inv_h](float sum) { return kShiftMean<T> ? sum * inv_h : sum / h; });
         // behind that barrier every thread has its part of the slot in registers
         if (tid == 0 && turn + slots < ring.turns) ring.load(turn + slots, s);
+        float both[2 * R];                   // sums of the differences (kShiftMean) and of their squares
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            Pair acc = pair(0.0f);
+            Pair acc = pair(0.0f), first = pair(0.0f);
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
                 if (tid + i * blockDim.x < n_vec) {
@@ -351,13 +409,24 @@ layer_norm_ring_kernel(const T* x, const float* __restrict__ gamma, const float*
 #pragma unroll
                     for (int k = 0; k < N / 2; ++k) {
                         const Pair d = f[k] + pair(-mu[r]);
+                        if (kShiftMean<T>) first = first + d;
                         acc = fma2(d, d, acc);
                     }
                 }
             }
-            rs[r] = acc.v.x + acc.v.y;
+            both[2 * r] = first.v.x + first.v.y;
+            both[2 * r + 1] = rs[r] = acc.v.x + acc.v.y;
         }
-        cta_sums<R>(rs, scratch[1], [h, eps](float sum) { return 1.0f / sqrtf(sum / h + eps); });
+        if constexpr (kShiftMean<T>) {
+            cta_sums<2 * R>(both, scratch[1], ShiftAndRstd{h, inv_h, eps});
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                mu[r] += both[2 * r];
+                rs[r] = both[2 * r + 1];
+            }
+        } else {
+            cta_sums<R>(rs, scratch[1], [h, eps](float sum) { return 1.0f / sqrtf(sum / h + eps); });
+        }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             if (r0 + r >= rows) continue;
