@@ -45,6 +45,7 @@ class MoELayer:
         self.mean, self.rstd = new(T, dtype=f32), new(T, dtype=f32)
         self.logits = new(T, self.E)
         self.act, self.pre, self.out = new(self.P, F), new(self.P, 2 * F), new(T, H)
+        self.grad_pre = new(self.P, 2 * F)              # not `pre` itself: backward may be called again
         self.grad_y, self.grad_expert_out, self.grad_send = new(T, H), new(self.P, H), new(self.P, H)
         self.grad_gate_w, self.grad_logits, self.grad_n, self.grad_x = new(T, K, dtype=f32), new(T, self.E), new(T, H), new(T, H)
         self.grad_gamma, self.grad_beta = new(H, dtype=f32), new(H, dtype=f32)
@@ -52,6 +53,7 @@ class MoELayer:
         self.grad_w_gate_up, self.grad_w_down = torch.zeros_like(self.w_gate_up), torch.zeros_like(self.w_down)
         ws = max(cb.expert_ffn_workspace_bytes(self.P, layout.D, self.E, H, F), cb.layer_norm_workspace_bytes(T, H), 256)
         self.workspace = torch.empty((ws,), dtype=torch.uint8, device=dev)
+        self.x = None                                   # input of the last forward call
 
     def _experts(self, send: torch.Tensor, expert_out: torch.Tensor) -> None:
         cb.expert_ffn(send, self.step.dest_offsets, self.slot_expert, self.w_gate_up, self.w_down, self.act, expert_out,
@@ -59,7 +61,8 @@ class MoELayer:
 
     def forward(self, x: torch.Tensor, seed: int) -> torch.Tensor:
         """The layer's output for x bfloat16 [T, H] (a buffer of this object, overwritten by the next call).  step.src_rank
-        holds the tokens' source ranks; `seed` draws the replica picks and the dropout mask."""
+        holds the tokens' source ranks; `seed` draws the replica picks and the dropout mask.  x is kept by reference and
+        read again by backward; it may be the output buffer itself if no backward call follows."""
         s = self.step
         self.x, self.seed = x, seed
         cb.layer_norm(x, self.gamma, self.beta, self.eps, s.x, self.mean, self.rstd)
@@ -70,17 +73,21 @@ class MoELayer:
         return self.out
 
     def backward(self, grad_out: torch.Tensor) -> torch.Tensor:
-        """Gradient of x for the last forward call; the parameters' gradients are in the grad_* attributes."""
+        """Gradient of x for the last forward call (a buffer of this object); the parameters' gradients are in the grad_*
+        attributes.  May be called again for the same forward call, also with a gradient that it returned before."""
+        if self.x is None or (self.T > 0 and self.x.data_ptr() == self.out.data_ptr()):
+            raise cb.CobaltError(cb.ERR_INVALID_ARG, "MoELayer.backward (no forward call, or its output was written over its input)")
         s = self.step
         cb.dropout_add_backward(grad_out, self.p, self.seed, self.grad_y)
         cb.combine_backward(self.grad_y, s.expert_out, s.row_of_pair, s.gate_w, self.grad_expert_out, self.grad_gate_w)
         cb.expert_ffn_backward(self.grad_expert_out, s.send, s.dest_offsets, self.slot_expert, self.w_gate_up, self.w_down,
-                               self.pre, self.act, self.pre, self.workspace, grad_rows=self.grad_send,
+                               self.pre, self.act, self.grad_pre, self.workspace, grad_rows=self.grad_send,
                                grad_w_gate_up=self.grad_w_gate_up, grad_w_down=self.grad_w_down)
         cb.permute_backward(self.grad_send, s.row_of_pair, self.K, self.grad_n)
         cb.gate_topk_backward(self.grad_gate_w, self.logits, s.topk_ids, s.gate_w, self.grad_logits, flags=self.gate_flags)
         torch.mm(self.grad_logits.t(), s.x, out=self.grad_w_router)
         torch.addmm(self.grad_n, self.grad_logits, self.w_router, out=self.grad_n)
-        cb.layer_norm_backward(self.grad_n, self.x, self.gamma, self.mean, self.rstd, self.grad_x, self.grad_gamma,
+        cb.layer_norm_backward(self.grad_n, self.x, self.gamma, self.mean, self.rstd, self.grad_n, self.grad_gamma,
                                self.grad_beta, self.workspace)
-        return self.grad_x.add_(grad_out)                   # the residual branch
+        # the residual branch; element by element, so grad_out may be grad_x
+        return torch.add(self.grad_n, grad_out, out=self.grad_x)
