@@ -300,8 +300,8 @@ int cobalt_combine_backward(const void* grad_y, const void* expert_out, const in
     if (T < 0 || K < 1 || H < 1) return COBALT_ERR_INVALID_ARG;
     if (K > COBALT_MAX_TOPK || H % 8 != 0 || T * static_cast<int64_t>(K) >= (1ll << 31)) return COBALT_ERR_UNSUPPORTED;
     if ((flags & COBALT_IMPL_MASK) != 0 && (flags & COBALT_IMPL_MASK) != COBALT_IMPL_VECTOR) return COBALT_ERR_INVALID_ARG;
+    if (T == 0) return COBALT_OK;                // (tensors without elements have no address)
     if (!grad_expert_out && !grad_gate_w) return COBALT_ERR_INVALID_ARG;
-    if (T == 0) return COBALT_OK;
     if (!grad_y || !row_of_pair || !gate_w || (grad_gate_w && !expert_out)) return COBALT_ERR_INVALID_ARG;
     if (!aligned16(grad_y) || !aligned16(expert_out) || !aligned16(row_of_pair) || !aligned16(gate_w) ||
         !aligned16(grad_expert_out) || !aligned16(grad_gate_w))

@@ -1091,7 +1091,7 @@ int cobalt_expert_ffn_backward(const void* grad_out, const void* rows, const uin
 {
     COBALT_TRY(check_ffn(P, D, E, H, F));
     if (!dest_offsets || !slot_expert) return COBALT_ERR_INVALID_ARG;
-    if (!grad_rows && !grad_w_gate_up && !grad_w_down) return COBALT_ERR_INVALID_ARG;
+    if (P > 0 && !grad_rows && !grad_w_gate_up && !grad_w_down) return COBALT_ERR_INVALID_ARG;
     if (P > 0 && (!grad_out || !rows || !w_gate_up || !w_down || !pre || !act || !grad_pre)) return COBALT_ERR_INVALID_ARG;
     if (!aligned16(grad_out) || !aligned16(rows) || !aligned16(dest_offsets) || !aligned16(slot_expert) || !aligned16(w_gate_up) ||
         !aligned16(w_down) || !aligned16(pre) || !aligned16(act) || !aligned16(grad_pre) || !aligned16(grad_rows) ||

@@ -55,3 +55,14 @@ def test_backward_without_forward_is_refused():
     m, _, dy = _layer(w, 40, "softmax", 0.2)
     with pytest.raises(cb.CobaltError):
         m.backward(dy)
+
+
+def test_no_tokens():
+    import paper_2609_36959_b200 as cb
+    w = W.make_custom(0, 8, 2, 64, 2, 2, 3, seed=3, C=2)
+    m, x, dy = _layer(w, 40, "softmax", 0.2)
+    assert m.forward(x, 5).shape == (0, 64) and m.backward(dy).shape == (0, 64)
+    torch.cuda.synchronize()
+    assert cb.read_and_clear_device_error() == 0
+    for g in GRADS:
+        assert float(getattr(m, g).float().abs().sum()) == 0
