@@ -387,8 +387,8 @@ int cobalt_gate_topk_backward(const float* grad_gate_w, const void* logits, cons
  * [E, 2F, H] (F gate rows, then F up rows) and w_down bf16 [E, H, F]:
  *   pre = x w_gate_up[e]^T = (g, u)     act = g * sigmoid(g) * u     out = act w_down[e]^T
  * act bf16 [P, F] is scratch for inference and an input of the backward call; pre [P, 2F] (two bytes an
- * element, in a format of the library's own: a sign, six exponent and nine mantissa bits, saturating at 2^32) is
- * only needed by the backward call (NULL for inference).
+ * element, in a format of the library's own: a sign, six exponent and nine mantissa bits; finite values saturate at
+ * 2^32, infinities and NaN are kept) is only needed by the backward call (NULL for inference).
  * Backward: grad_pre [P, 2F] is scratch (it may be `pre` itself, which is then overwritten);
  *   d_act = grad_out w_down[e]     d_u = d_act g s     d_g = d_act u s (1 + g (1 - s)),  s = sigmoid(g)
  *   grad_rows = (d_g, d_u) w_gate_up[e]      grad_w_gate_up[e] = sum (d_g, d_u)^T x

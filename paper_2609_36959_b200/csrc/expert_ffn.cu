@@ -338,9 +338,9 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi)
 // The saved pre-activations are 16-bit floats of one sign, six exponent and nine mantissa bits: four times finer than
 // bf16 (whose rounding here alone made the gradients of rows and weights 1.3 times as inexact as the two roundings that
 // they cannot do without: 3.0e-3 against 2.4e-3 in the 2-norm), over 2^-30 .. 2^32, with gradual underflow to 2^-39.
-// Larger values become the largest one, a NaN stays a NaN.  Scaled by 2^-96, such a value is an fp32 number whose
-// exponent fits six bits.
-constexpr uint32_t kPreNan = 0x7E00u;
+// Larger finite values become the largest one; infinities and NaN stay (the largest exponent, with mantissa 0 and 1).
+// Scaled by 2^-96, such a value is an fp32 number whose exponent fits six bits.
+constexpr uint32_t kPreInf = 0x7E00u;
 
 __device__ __forceinline__ uint32_t pack_pre(float lo, float hi)
 {
@@ -350,10 +350,9 @@ __device__ __forceinline__ uint32_t pack_pre(float lo, float hi)
     uint32_t c[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        asm("min.NaN.f32 %0, %0, %1;" : "+f"(v[i]) : "f"(most));
-        asm("max.NaN.f32 %0, %0, %1;" : "+f"(v[i]) : "f"(-most));
-        const uint32_t b = __float_as_uint(v[i]) + 0x2000u;                 // to nearest, halves up
-        c[i] = v[i] == v[i] ? ((b >> 14) & 0x7FFFu) | ((b >> 16) & 0x8000u) : kPreNan;
+        const uint32_t sign = (__float_as_uint(v[i]) >> 16) & 0x8000u;
+        const uint32_t b = __float_as_uint(fminf(fabsf(v[i]), most)) + 0x2000u;        // to nearest, halves up
+        c[i] = sign | (fabsf(v[i]) < INFINITY ? b >> 14 : v[i] == v[i] ? kPreInf : kPreInf + 1);
     }
     return c[0] | (c[1] << 16);
 }
@@ -361,8 +360,10 @@ __device__ __forceinline__ uint32_t pack_pre(float lo, float hi)
 __device__ __forceinline__ float unpack_pre(uint32_t code)                  // in the upper half of the word
 {
     const float scale = __uint_as_float(0x6F800000u);                       // 2^96
-    const float v = __uint_as_float(((code >> 2) & 0x1FFFC000u) | (code & 0x80000000u)) * scale;
-    return ((code >> 16) & kPreNan) == kPreNan ? __uint_as_float(0x7FC00000u) : v;
+    const uint32_t sign = code & 0x80000000u, magnitude = (code >> 2) & 0x1FFFC000u;
+    const float v = __uint_as_float(magnitude | sign) * scale;
+    // the largest exponent: fp32's largest, with the mantissa that there is
+    return magnitude >= kPreInf << 14 ? __uint_as_float(sign | (0x7F800000u + (magnitude - (kPreInf << 14)))) : v;
 }
 
 // 1 / (1 + exp(-g)): the fast exponential and division are good to a few units of fp32, far below the bf16 results
