@@ -793,6 +793,7 @@ __device__ __forceinline__ int expert_of_row(const uint32_t* offsets, const int3
         const int e = __ldg(slot_expert + d);
         const bool valid = e >= 0 && e < E;
         // slot in the upper bits, so that the lowest one wins; expert + 1 below (E <= 1024), 0 for none
+        if (d == 0 && a > static_cast<uint32_t>(p)) atomicMin(found, -1);      // ahead of the first slot
         if (static_cast<uint32_t>(p) < b) atomicMin(found, d << 12 | (valid ? e + 1 : 0));
         if (check) {
             const uint32_t n = static_cast<uint32_t>(P), lo = min(a, n), hi = min(b, n);
@@ -800,7 +801,7 @@ __device__ __forceinline__ int expert_of_row(const uint32_t* offsets, const int3
         }
     }
     __syncthreads();
-    return *found == 0x7FFFFFFF || __ldg(offsets) > static_cast<uint32_t>(p) ? -1 : (*found & 4095) - 1;
+    return *found == 0x7FFFFFFF || *found < 0 ? -1 : (*found & 4095) - 1;
 }
 
 // kUp: act (and pre) of one row, a warp a feature: its gate and its up row of the weights.  kDown: out of one row, a warp
