@@ -104,11 +104,12 @@ __device__ __forceinline__ void flag_error(uint32_t* err_word, uint32_t bits)
     atomicOr(err_word, bits);
 }
 
-// streaming (read-once / write-once) 16-byte accesses that stay out of L1
+// streaming (read-once / write-once) 16-byte accesses that stay out of L1; volatile, so that a load behind a bounds check
+// is not run ahead of it
 __device__ __forceinline__ uint4 ld_stream16(const void* p)
 {
     uint4 v;
-    asm("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
                  : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
                  : "l"(p));
     return v;
