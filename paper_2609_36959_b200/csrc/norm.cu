@@ -629,8 +629,9 @@ static NormShape norm_shape(int n_vec)
     return s;
 }
 
-// The ring kernels: one vector a thread up to 896, so that what belongs to its columns takes few registers; `most_rows`
-// rows a slot where that leaves two slots, and as many slots as fit, at most four.
+// The ring kernels: one vector a thread up to 896, so that what belongs to its columns takes few registers; `many_rows`
+// rows a slot then (twice that fits for every such row, of one tensor times four as of two times two), one row above, and as
+// many slots as fit, at most four.
 struct RingShape {
     int vpt, threads, rows, slots;
     size_t smem;
@@ -638,8 +639,9 @@ struct RingShape {
 };
 
 constexpr size_t kRingBytes = 208 * 1024;
+static_assert(2 * 4 * 896 * 16 <= kRingBytes && 2 * 4 * 512 * 16 <= kRingBytes / 2, "two slots of four rows, or of two of two tensors");
 
-static RingShape ring_shape(int H, int elem_bytes, int tensors, int most_rows)
+static RingShape ring_shape(int H, int elem_bytes, int tensors, int many_rows)
 {
     RingShape s = {};
     const int n_vec = H * elem_bytes / 16;
@@ -647,7 +649,7 @@ static RingShape ring_shape(int H, int elem_bytes, int tensors, int most_rows)
     s.threads = ((n_vec + s.vpt - 1) / s.vpt + 31) / 32 * 32;
     s.resident = s.threads <= 512 ? 2 : 1;
     const size_t row = static_cast<size_t>(tensors) * H * elem_bytes, room = kRingBytes / s.resident;
-    s.rows = s.vpt == 1 && 2 * most_rows * row <= room ? most_rows : 1;
+    s.rows = s.vpt == 1 ? many_rows : 1;
     s.slots = static_cast<int>(room / (s.rows * row));
     if (s.slots > 4) s.slots = 4;
     if (s.slots < 1) s.slots = 1;
@@ -719,9 +721,7 @@ static int launch_norm(const T* x, const float* gamma, const float* beta, int64_
         uint32_t* err_word = nullptr;
         rc = device_error_word(&err_word);
         if (rc != COBALT_OK) return rc;
-        if (ring.vpt == 1)
-            return ring.rows == 4 ? launch_norm_ring<T, 1, 4>(x, gamma, beta, rows, H, eps, y, mean, rstd, ring, sms, err_word, s)
-                                  : launch_norm_ring<T, 1, 1>(x, gamma, beta, rows, H, eps, y, mean, rstd, ring, sms, err_word, s);
+        if (ring.vpt == 1) return launch_norm_ring<T, 1, 4>(x, gamma, beta, rows, H, eps, y, mean, rstd, ring, sms, err_word, s);
         if (ring.vpt == 4) return launch_norm_ring<T, 4, 1>(x, gamma, beta, rows, H, eps, y, mean, rstd, ring, sms, err_word, s);
         return launch_norm_ring<T, 2, 1>(x, gamma, beta, rows, H, eps, y, mean, rstd, ring, sms, err_word, s);
     }
@@ -775,9 +775,7 @@ static int launch_norm_backward(const T* grad_y, const T* x, const float* gamma,
 #undef COBALT_NORM_BWD
         return COBALT_OK;
     }
-    if (shape.vpt == 1)
-        return shape.rows == 2 ? launch_ring<T, 1, 2>(grad_y, x, gamma, mean, rstd, rows, H, grad_x, partial, shape, grid, err_word, s)
-                               : launch_ring<T, 1, 1>(grad_y, x, gamma, mean, rstd, rows, H, grad_x, partial, shape, grid, err_word, s);
+    if (shape.vpt == 1) return launch_ring<T, 1, 2>(grad_y, x, gamma, mean, rstd, rows, H, grad_x, partial, shape, grid, err_word, s);
     if (shape.vpt == 4) return launch_ring<T, 4, 1>(grad_y, x, gamma, mean, rstd, rows, H, grad_x, partial, shape, grid, err_word, s);
     return launch_ring<T, 2, 1>(grad_y, x, gamma, mean, rstd, rows, H, grad_x, partial, shape, grid, err_word, s);
 }
