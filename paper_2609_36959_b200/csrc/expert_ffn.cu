@@ -12,8 +12,9 @@
 //     the M side, so that a slot's ragged row count is the N extent of the instruction, a multiple of 32 chosen for
 //     every tile: a slot of 40 rows costs 64, not 128 or 256, and a single token streams the weights once.
 //     The weight gradients have features on both sides and the rows as the summed extent.
-//   - Warp 0 of each CTA feeds a ring of 64-deep blocks by tensor-map loads, warp 1 of the leading CTA issues the
-//     products, warps 2 to 5 run the epilogue (and warp 6 clears the ragged ends of slots for the weight gradients).
+//   - Warp 0 of each CTA feeds a ring of 64-deep blocks by tensor-map loads, which the leading CTA's barriers count for
+//     both; warp 1 of the leading CTA issues the products, warps 2 to 5 run the epilogue (and warp 6 clears the ragged ends
+//     of slots for the weight gradients).
 //     Two accumulators (2 x 256 of 512 columns) let the epilogue of a tile run under the products of the next one.
 //   - CTAs are persistent, a pair for every two SMs, and deal the tiles of all slots round robin; the tile list is
 //     built on the device from dest_offsets (no copy to the host).
@@ -369,7 +370,8 @@ __device__ __forceinline__ float unpack_pre(uint32_t code)                  // i
 // 1 / (1 + exp(-g)): the fast exponential and division are good to a few units of fp32, far below the bf16 results
 __device__ __forceinline__ float sigmoid(float g) { return __fdividef(1.0f, 1.0f + __expf(-g)); }
 
-// Clears k rows valid .. 63 of this CTA's boxes in a ring slot (the loads brought rows of the next slot there).
+// Clears k rows valid .. 63 of this CTA's boxes in a ring slot (the loads brought rows of the next slot there).  The
+// release that tells of it comes from one lane, behind the others' fences.
 __device__ __forceinline__ void clear_tail(uint32_t slot_addr, int boxes_b, int valid, int lane)
 {
     const int vectors = (kBlockK - valid) * 8;               // 16-byte vectors of a box
@@ -378,7 +380,6 @@ __device__ __forceinline__ void clear_tail(uint32_t slot_addr, int boxes_b, int 
         for (int i = lane; i < vectors; i += 32) store_shared16(at + i * 16, make_uint4(0, 0, 0, 0));
     }
     fence_async_shared();
-    fence_cluster();                                          // the leading CTA issues the products that read them
     __syncwarp();
 }
 
@@ -392,17 +393,18 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     const uint32_t base = smem_u32(smem);
     const uint32_t staging = base + S::kRing * kSlotBytes;
     const uint32_t bars = staging + S::kStaging;
-    const uint32_t full = bars, empty = bars + 8 * S::kRing, relay = bars + 16 * S::kRing;
+    const uint32_t ready = bars, empty = bars + 8 * S::kRing, landed = bars + 16 * S::kRing;
     const uint32_t acc_full = bars + 24 * S::kRing, acc_empty = acc_full + 16, drain = acc_full + 32, tmem_slot = acc_full + 40;
     const int warp = __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::kRing; ++i) {
-            barrier_init(full + 8 * i, 1);       // this CTA's loads
+            // leading CTA: the slot can be read.  Both CTAs' loads count on it themselves, so that what they brought is
+            // ordered before the products; where a slot's end was cleared, the warp that cleared it arrives instead.
+            barrier_init(ready + 8 * i, 2);
             barrier_init(empty + 8 * i, 1);      // the products that read the slot are done
-            // leading CTA: the other CTA's loads; kWeights: both CTAs' loads, with what is past a slot's end cleared
-            barrier_init(relay + 8 * i, S::kWeightsStage ? 2 : 1);
+            barrier_init(landed + 8 * i, 1);     // kWeights: this CTA's loads of a block with a slot's end
         }
         for (int i = 0; i < 2; ++i) {
             barrier_init(acc_full + 8 * i, 1);
@@ -428,6 +430,7 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 
     if (warp == 0) {
         // ---- loads of this CTA's halves --------------------------------------------------------------------
+        const uint32_t pair_ready = peer_address(ready, 0);
         Ring ring;
         int64_t issued = 0;
         // a band reads its row tiles (kWeights: tiles of M) again for every tile of the other extent, and that one once
@@ -452,16 +455,20 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 // the list's loads are under way before the next tile needs them
                 if (k == w.blocks / 2 && t + step < tiles) next = get_tile<kStage>(p, t + step);
                 if (!(ok = barrier_wait(empty + 8 * ring.slot, ring.phase ^ 1))) break;
-                const uint32_t bar = full + 8 * ring.slot, a = base + ring.slot * kSlotBytes, b = a + kHalfBytes;
+                const bool ends = kStage == kWeights && rows.y - done < kBlockK;     // a slot's rows end in this block
+                const uint32_t bar = ends ? landed + 8 * ring.slot : pair_ready + 8 * ring.slot;
+                const uint32_t a = base + ring.slot * kSlotBytes, b = a + kHalfBytes;
                 if (elect_one()) {
                     if (kStage == kWeights) {
-                        barrier_expect(bar, (boxes_a + boxes_b) * kBoxBytes);
+                        const uint32_t bytes = (boxes_a + boxes_b) * kBoxBytes;
+                        if (ends) barrier_expect(bar, bytes);
+                        else barrier_expect_cluster(bar, bytes);
                         if (boxes_a > 0) tma_load_2d(a, &map_a, bar, policy_a, m0, rows.x + done);
                         if (boxes_a > 1) tma_load_2d(a + kBoxBytes, &map_a, bar, policy_a, m0 + 64, rows.x + done);
                         if (boxes_b > 0) tma_load_2d(b, &map_b, bar, policy_b, n0, rows.x + done);
                         if (boxes_b > 1) tma_load_2d(b + kBoxBytes, &map_b, bar, policy_b, n0 + 64, rows.x + done);
                     } else {
-                        barrier_expect(bar, boxes_a * (S::kAMn ? kBoxBytes : kHalfBytes) + max(parts_b, 0) * kBlockK * 2);
+                        barrier_expect_cluster(bar, boxes_a * (S::kAMn ? kBoxBytes : kHalfBytes) + max(parts_b, 0) * kBlockK * 2);
                         if (kStage == kUp && boxes_a > 0) tma_load_5d(a, &map_a, bar, policy_a, k * kBlockK, 0, 0, m0 / 16, w.expert);
                         if (kStage == kDown && boxes_a > 0) tma_load_3d(a, &map_a, bar, policy_a, k * kBlockK, m0, w.expert);
                         if (S::kAMn) {
@@ -484,17 +491,20 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             }
         }
         if (!ok) {
-            // the copies in flight have to land before this CTA's shared memory is given back
+            // the copies in flight have to land before the pair's shared memory is given back: the leading CTA waits for
+            // its last blocks, which the other CTA's copies count on too, and once more for a block that will not be
+            // complete, for those of the other CTA that are further ahead (and for blocks with a slot's end)
             if (lane == 0) flag_error(p.err_word, COBALT_DEVERR_WAIT_TIMEOUT);
-            for (int64_t i = issued > S::kRing ? issued - S::kRing : 0; i < issued; ++i)
-                (void)barrier_wait(full + 8 * static_cast<int>(i % S::kRing), static_cast<uint32_t>(i / S::kRing) & 1);
+            if (rank == 0)
+                for (int64_t i = issued > S::kRing ? issued - S::kRing : 0; i <= issued; ++i)
+                    (void)barrier_wait(ready + 8 * static_cast<int>(i % S::kRing), static_cast<uint32_t>(i / S::kRing) & 1);
         }
         __syncwarp();
     } else if (warp == 1) {
-        // ---- products (leading CTA); in a row stage the other CTA passes on that its loads have landed -----------
+        // ---- products (leading CTA) ------------------------------------------------------------------------------
         Ring ring;
         int turn = 0;                            // accumulators used so far
-        const bool part = rank == 0 || !S::kWeightsStage;
+        const bool part = rank == 0;
         Tile next = {};
         if (part && first < tiles) next = get_tile<kStage>(p, first);
         for (int t = first; t < tiles && ok && part; t += step) {
@@ -505,35 +515,27 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             }
             const uint32_t acc = turn & 1, d = tmem + acc * 256;
             const uint32_t idesc = instruction_descriptor(w.n, S::kAMn, S::kWeightsStage);
-            if (rank == 0) {
-                if (!(ok = barrier_wait(acc_empty + 8 * acc, ((turn >> 1) & 1) ^ 1))) break;
-                tmem_fence_after();
-            }
+            if (!(ok = barrier_wait(acc_empty + 8 * acc, ((turn >> 1) & 1) ^ 1))) break;
+            tmem_fence_after();
             for (int k = 0; k < w.blocks; ++k) {
                 if (k == w.blocks / 2 && t + step < tiles) next = get_tile<kStage>(p, t + step);
-                if (!S::kWeightsStage && !(ok = barrier_wait(full + 8 * ring.slot, ring.phase))) break;
                 const uint32_t a = base + ring.slot * kSlotBytes;
-                if (rank != 0) {
-                    if (elect_one()) barrier_arrive_cluster(peer_address(relay + 8 * ring.slot, 0));
-                    __syncwarp();
-                } else {
-                    if (!(ok = barrier_wait(relay + 8 * ring.slot, ring.phase))) break;
-                    tmem_fence_after();
-                    if (elect_one()) {
-                        // K-major: 16 values of k are 32 bytes further in the swizzled row; MN-major: two 8-row groups
-                        const uint64_t da = S::kAMn ? matrix_descriptor(a, kBoxBytes, 1024) : matrix_descriptor(a, 16, 1024);
-                        const uint64_t db = S::kWeightsStage ? matrix_descriptor(a + kHalfBytes, kBoxBytes, 1024)
-                                                             : matrix_descriptor(a + kHalfBytes, 16, 1024);
-                        constexpr uint32_t step_a = (S::kAMn ? 2048 : 32) >> 4, step_b = (S::kWeightsStage ? 2048 : 32) >> 4;
+                if (!(ok = barrier_wait(ready + 8 * ring.slot, ring.phase))) break;
+                tmem_fence_after();
+                if (elect_one()) {
+                    // K-major: 16 values of k are 32 bytes further in the swizzled row; MN-major: two 8-row groups
+                    const uint64_t da = S::kAMn ? matrix_descriptor(a, kBoxBytes, 1024) : matrix_descriptor(a, 16, 1024);
+                    const uint64_t db = S::kWeightsStage ? matrix_descriptor(a + kHalfBytes, kBoxBytes, 1024)
+                                                         : matrix_descriptor(a + kHalfBytes, 16, 1024);
+                    constexpr uint32_t step_a = (S::kAMn ? 2048 : 32) >> 4, step_b = (S::kWeightsStage ? 2048 : 32) >> 4;
 #pragma unroll
-                        for (uint32_t i = 0; i < kBlockK / 16; ++i) mma_pair(d, da + i * step_a, db + i * step_b, idesc, k > 0 || i > 0);
-                        mma_commit_pair(empty + 8 * ring.slot);
-                    }
-                    __syncwarp();
+                    for (uint32_t i = 0; i < kBlockK / 16; ++i) mma_pair(d, da + i * step_a, db + i * step_b, idesc, k > 0 || i > 0);
+                    mma_commit_pair(empty + 8 * ring.slot);
                 }
+                __syncwarp();
                 ring.next<S::kRing>();
             }
-            if (rank == 0 && ok) {
+            if (ok) {
                 if (elect_one()) mma_commit_pair(acc_full + 8 * acc);
                 __syncwarp();
             }
@@ -541,19 +543,18 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         }
         if (!ok) {
             if (lane == 0) flag_error(p.err_word, COBALT_DEVERR_WAIT_TIMEOUT);
-            if (rank == 0) {                     // products in flight end before the tensor memory is freed
-                if (elect_one()) mma_commit_pair(drain);
-                (void)barrier_wait(drain, 0);
-            }
+            if (elect_one()) mma_commit_pair(drain);     // products in flight end before the tensor memory is freed
+            (void)barrier_wait(drain, 0);
         }
         __syncwarp();
     } else if (S::kWeightsStage && warp == 6) {
         // ---- weight gradients: k rows past the end of a slot, which belong to the next one, are cleared here, ahead of
         // the products and off their path; then the leading CTA hears of the block
         Ring ring;
+        uint32_t phases = 0;                     // of `landed`, a bit a slot: only blocks with a slot's end use it
         Tile next = {};
         if (first < tiles) next = get_tile<kStage>(p, first);
-        const uint32_t heard = peer_address(relay, 0);
+        const uint32_t pair_ready = peer_address(ready, 0);
         for (int t = first; t < tiles && ok; t += step) {
             const Tile w = next;
             if (w.blocks == 0 && t + step < tiles) next = get_tile<kStage>(p, t + step);
@@ -561,10 +562,13 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             int seg = w.seg, left = w.head.y;
             for (int k = 0; k < w.blocks; ++k) {
                 if (k == w.blocks / 2 && t + step < tiles) next = get_tile<kStage>(p, t + step);
-                if (!(ok = barrier_wait(full + 8 * ring.slot, ring.phase))) break;
-                if (left < kBlockK) clear_tail(base + ring.slot * kSlotBytes, boxes_b, left, lane);
-                if (elect_one()) barrier_arrive_cluster(heard + 8 * ring.slot);
-                __syncwarp();
+                if (left < kBlockK) {
+                    if (!(ok = barrier_wait(landed + 8 * ring.slot, (phases >> ring.slot) & 1))) break;
+                    phases ^= 1u << ring.slot;
+                    clear_tail(base + ring.slot * kSlotBytes, boxes_b, left, lane);
+                    if (elect_one()) barrier_arrive_cluster(pair_ready + 8 * ring.slot);
+                    __syncwarp();
+                }
                 left -= kBlockK;
                 if (left <= 0 && ++seg < w.seg_end) left = p.plan.segs[seg].y;
                 ring.next<S::kRing>();
@@ -723,7 +727,7 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                             uint32_t r[16] = {};
                             if (w.blocks > 0) {
                                 tmem_load_16x32(lanes + (static_cast<uint32_t>(16 * hl) << 16) + acc * 256 + c + 32 * q, r);
-                                    }
+                            }
 #pragma unroll
                             for (int o = 0; o < 2; ++o) {
                                 uint32_t v[4];
@@ -747,7 +751,7 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             if (w.blocks > 0) {
                 tmem_fence_before();
                 __syncwarp();
-                if (lane == 0) barrier_arrive_cluster(peer_address(acc_empty + 8 * acc, 0));
+                if (lane == 0) barrier_arrive_tmem(peer_address(acc_empty + 8 * acc, 0));
                 ++turn;
             }
         }

@@ -56,22 +56,31 @@ __device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes)
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 
-// `bar` is an address of the cluster's shared memory (peer_address).  The arrival itself orders nothing beyond this
-// CTA: what it stands for is ordered by the loads' own completion and by the tcgen05 fences, and writes of the
-// calling warp need fence_cluster() ahead of it (a release at cluster scope with every arrival stalled the ring).
-__device__ __forceinline__ void barrier_arrive_cluster(uint32_t bar)
+// The same on a barrier of the pair, `bar` an address of the cluster's shared memory (peer_address).  It passes no data on.
+__device__ __forceinline__ void barrier_expect_cluster(uint32_t bar, uint32_t bytes)
 {
-    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 
-__device__ __forceinline__ void fence_cluster() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
+// The same without bytes, behind tmem_fence_before(): accumulators that were read may be overwritten.
+__device__ __forceinline__ void barrier_arrive_tmem(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+// Arrives on a barrier of the pair; what the warp wrote before is visible behind the wait for it.  The release takes about a
+// microsecond: once at the end of a slot, not once a block.
+__device__ __forceinline__ void barrier_arrive_cluster(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
 
 __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity)
 {
     uint32_t done;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
         "selp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(done)
         : "r"(bar), "r"(parity), "r"(1000000u)       // suspended for up to a millisecond instead of polling
@@ -105,10 +114,11 @@ __device__ __forceinline__ uint64_t policy_normal()
     return p;
 }
 
+// Tensor-map loads into this CTA's shared memory; the barrier that counts their bytes may be either CTA's of the pair.
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, uint32_t bar, uint64_t policy, int x, int y)
 {
     asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%4, %5}], [%2], %3;" ::"r"(dst),
+        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2.L2::cache_hint [%0], [%1, {%4, %5}], [%2], %3;" ::"r"(dst),
         "l"(map), "r"(bar), "l"(policy), "r"(x), "r"(y)
         : "memory");
 }
@@ -116,7 +126,7 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint32_t bar, uint64_t policy, int x, int y, int z)
 {
     asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%4, %5, %6}], [%2], %3;" ::"r"(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2.L2::cache_hint [%0], [%1, {%4, %5, %6}], [%2], %3;" ::"r"(
             dst),
         "l"(map), "r"(bar), "l"(policy), "r"(x), "r"(y), "r"(z)
         : "memory");
@@ -126,7 +136,7 @@ __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map
                                             int e)
 {
     asm volatile(
-        "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%4, %5, %6, %7, %8}], [%2], "
+        "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2.L2::cache_hint [%0], [%1, {%4, %5, %6, %7, %8}], [%2], "
         "%3;" ::"r"(dst),
         "l"(map), "r"(bar), "l"(policy), "r"(a), "r"(b), "r"(c), "r"(d), "r"(e)
         : "memory");
