@@ -22,9 +22,9 @@
 // A call of a few rows (a token of generation) is bound by streaming the weights of their experts once; tiles leave SMs
 // without work there, so each warp takes one feature of one row on the fp32 units instead (ffn_few_rows_kernel).
 //
-// Bound by the tensor pipe's energy in long runs (the 1000 W cap; 1209 TFLOP/s at 65 536 rows, H 7168, F 2048, forward and
+// Bound by the tensor pipe's energy in long runs (the 1000 W cap; 1150 to 1209 TFLOP/s at 65 536 rows, H 7168, F 2048, forward and
 // backward, where cuBLAS holds 1340 to 1400 on one product of that shape), by the touched weights' bytes for few rows an
-// expert (384 rows over 105 experts: 635 us, 96 % of copy speed).
+// expert (384 rows over 105 experts: 635 to 670 us, 90 to 96 % of copy speed).
 //
 // Every wait is bounded: when one runs out the kernel sets COBALT_DEVERR_WAIT_TIMEOUT, drains its copies, frees its
 // tensor memory and returns.
