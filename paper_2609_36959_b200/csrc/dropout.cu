@@ -10,7 +10,8 @@
 //
 // A thread owns blocks of eight elements: the generator's 20 wide multiplications serve eight elements (16 bits each
 // decide to 1/65536, finer than any rate in use; a word an element would double them).  Bound by HBM: 32768 x 7168 bf16
-// forward 200 us, backward 168 us one launch at a time, 1410 and 940 MB of which 36 and 47 MB are still in L2 at the end; 375 to 389 us for both in a row, 93 to 96 % of copy speed.
+// forward 200 us, backward 168 us one launch at a time, 1410 and 940 MB of which 36 and 47 MB are still in L2 at the end;
+// 375 to 389 us for both in a row, 93 to 96 % of copy speed.
 #include <math.h>
 
 #include "numeric.cuh"
