@@ -427,6 +427,75 @@ int cobalt_dropout_add(const void* x, const void* residual, int64_t n, int32_t d
 int cobalt_dropout_add_backward(const void* grad_out, int64_t n, int32_t dtype, double p, uint64_t seed,
                                 void* grad_x, uint32_t flags, cobalt_stream_t stream);
 
+/* ==== the dense part of a layer ====================================================================
+ * Operators on the token rows themselves, before and beside the routed experts, with the same conventions. */
+
+/* ---- rows in 8 bits -----------------------------------------------------------------------------------
+ * q holds one-byte codes [T, H], scales fp32 [T, ceil(H / 128)] (group 128: one for each 128 columns) or
+ * [T] (group 0: one for the row).  With `most` a group's largest absolute value and L the code's largest value,
+ *   scale = most / L     code = the one nearest to L x / most, halves to even     value = code * scale
+ *   COBALT_E4M3   8-bit floats of four exponent and three mantissa bits, L = 448 (operands of cobalt_linear)
+ *   COBALT_I8     signed integers, L = 127 (an error of at most scale / 2)
+ * A group of zeros has scale 0; a group that holds a NaN or an infinity has scale NaN and codes 0, and reads back as
+ * NaN.  Groups below 2^-100 may lose bits with the scale's own.  x and out of `dtype`; H a multiple of 8, at most 16384;
+ * T < 2^31; T = 0 is allowed.  The codes of rows given in fp32 or bf16 are exactly those of the definition. */
+#define COBALT_E4M3 2
+#define COBALT_I8 3
+int cobalt_pack_rows(const void* x, int64_t T, int32_t H, int32_t dtype, int32_t code, int32_t group,
+                     void* q, float* scales, cobalt_stream_t stream);
+int cobalt_unpack_rows(const void* q, const float* scales, int64_t T, int32_t H, int32_t code,
+                       int32_t group, int32_t dtype, void* out, cobalt_stream_t stream);
+
+/* ---- root-mean-square norm of a sum ---------------------------------------------------------------------
+ *   s = x + residual, rounded to `dtype`     rstd = 1 / sqrt(sum s^2 / H + eps)     y = s * rstd * gamma
+ * The norm is that of s as it is held.  residual NULL: s is x, and `sum` must be NULL.  sum, y, q and rstd may each be NULL,
+ * but one of y and q must be given; q and q_scales are y in 8 bits (q_code COBALT_E4M3 or COBALT_I8, q_group 128 or 0),
+ * from y before its rounding to `dtype`.  Backward, with g = grad_y * gamma and z = s * rstd:
+ *   grad_x = rstd * (g - z * mean(g * z)) + grad_sum     grad_gamma = sum_t grad_y * z     (overwritten)
+ * grad_x is the gradient of x and of residual alike; grad_sum (may be NULL) is what reaches s past the norm.  rows is
+ * s as rows_type `dtype` (row_scales and group are then not read), or s in 8 bits (rows_type COBALT_I8 or COBALT_E4M3) as
+ * cobalt_pack_rows leaves it.  gamma, grad_gamma fp32 [H]; rstd fp32 [T].  H a multiple of 8, at most 16384; T < 2^31;
+ * T = 0 is allowed (grad_gamma is then 0).  eps >= 0; a row of zeros with eps = 0 gives NaN.  sum and y may each be x or
+ * residual (not both the same buffer), grad_x may be grad_y or grad_sum.  Results do not vary from run to run. */
+int cobalt_rms_norm(const void* x, const void* residual, const float* gamma, int64_t T, int32_t H,
+                    int32_t dtype, float eps, void* sum, void* y, void* q, float* q_scales, int32_t q_code,
+                    int32_t q_group, float* rstd, cobalt_stream_t stream);
+size_t cobalt_rms_norm_workspace_bytes(int64_t T, int32_t H);
+int cobalt_rms_norm_backward(const void* grad_y, const void* grad_sum, const void* rows,
+                             const float* row_scales, int32_t rows_type, int32_t group, const float* gamma,
+                             const float* rstd, int64_t T, int32_t H, int32_t dtype, void* grad_x,
+                             float* grad_gamma, void* workspace, size_t workspace_bytes,
+                             cobalt_stream_t stream);
+
+/* ---- linear: a product with bias, activation and residual ------------------------------------------------
+ *   pre = x w^T + bias     out = act(pre) + residual
+ * x [T, K] and w [N, K] bf16 (operand COBALT_BF16; the scales are not read), or e4m3 codes with one scale a row, fp32 [T] and
+ * [N], as cobalt_pack_rows leaves them with group 0 (operand COBALT_E4M3).  bias bf16 [N] or NULL; residual [T, N] like
+ * out, or NULL; out of out_type COBALT_BF16 or COBALT_F32.  pre, where a backward pass follows an activation: bf16 [T, N]
+ * (pre_type COBALT_BF16), or COBALT_I8 codes [T, N] with pre_scales fp32 [T, ceil(N / 128)]; else NULL.  act:
+ *   COBALT_ACT_NONE   COBALT_ACT_RELU   COBALT_ACT_SILU v / (1 + exp(-v))   COBALT_ACT_GELU v (1 + erf(v / sqrt 2)) / 2
+ * Backward, for bf16 x and w, with grad_out [T, N] of grad_type (COBALT_BF16 or COBALT_F32):
+ *   d = grad_out * act'(pre)     grad_x = d w     grad_w = d^T x     grad_bias = sum_t d     (bf16, overwritten)
+ * grad_pre bf16 [T, N] is scratch for d, needed for grad_x or grad_w if there is an activation or grad_out is fp32 (it may
+ * be grad_out where that is bf16); d is rounded to bf16 once.  pre is not read without an activation.  The residual's gradient is
+ * grad_out itself.  Each of the three results may be NULL, but not all.  Products and sums are fp32.
+ * K and N multiples of 8 (e4m3: K of 16), at most COBALT_LINEAR_MAX_WIDTH; T <= 2^31 - 2^21; T = 0 is allowed (gradients
+ * of w and bias are then 0).  out may be residual.  Results do not vary from run to run. */
+#define COBALT_ACT_NONE 0
+#define COBALT_ACT_RELU 1
+#define COBALT_ACT_SILU 2
+#define COBALT_ACT_GELU 3
+#define COBALT_LINEAR_MAX_WIDTH 65536
+size_t cobalt_linear_workspace_bytes(int64_t T, int32_t K, int32_t N);
+int cobalt_linear(const void* x, const float* x_scales, const void* w, const float* w_scales, const void* bias,
+                  const void* residual, int64_t T, int32_t K, int32_t N, int32_t operand, int32_t act,
+                  int32_t out_type, void* pre, float* pre_scales, int32_t pre_type, void* out, void* workspace,
+                  size_t workspace_bytes, cobalt_stream_t stream);
+int cobalt_linear_backward(const void* grad_out, const void* x, const void* w, const void* pre,
+                           const float* pre_scales, int32_t pre_type, int64_t T, int32_t K, int32_t N,
+                           int32_t act, int32_t grad_type, void* grad_pre, void* grad_x, void* grad_w,
+                           void* grad_bias, void* workspace, size_t workspace_bytes, cobalt_stream_t stream);
+
 /* ---- device error word -------------------------------------------------------------------
  * Waits for `stream`, copies the COBALT_DEVERR_* bits set by kernels on the current device
  * since the last call into *out_bits_host and clears them. */

@@ -19,6 +19,12 @@ int record_cuda_error(cudaError_t err);
             return ::cobalt::record_cuda_error(cobalt_err__);        \
     } while (0)
 
+#define COBALT_TRY(expr)                       \
+    do {                                       \
+        const int cobalt_rc__ = (expr);        \
+        if (cobalt_rc__ != COBALT_OK) return cobalt_rc__; \
+    } while (0)
+
 // Address of the current device's error word (kernels receive it as an argument).
 int device_error_word(uint32_t** out);
 

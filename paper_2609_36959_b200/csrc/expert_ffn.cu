@@ -28,11 +28,10 @@
 //
 // Every wait is bounded: when one runs out the kernel sets COBALT_DEVERR_WAIT_TIMEOUT, drains its copies, frees its
 // tensor memory and returns.
-#include <atomic>
-
 #include "numeric.cuh"
 #include "slot_ranges.h"
 #include "tcgen05.cuh"
+#include "tensor_map.cuh"
 
 namespace cobalt {
 
@@ -316,26 +315,6 @@ __device__ __forceinline__ Tile get_tile(const ProductArgs& p, int t)
     return r;
 }
 
-// Position in the ring: slot and the parity of its present use.
-struct Ring {
-    int slot = 0;
-    uint32_t phase = 0;
-    template <int kRing>
-    __device__ __forceinline__ void next()
-    {
-        if (++slot == kRing) {
-            slot = 0;
-            phase ^= 1;
-        }
-    }
-};
-
-__device__ __forceinline__ uint32_t pack2(float lo, float hi)
-{
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
-}
-
 // The saved pre-activations are 16-bit floats of one sign, six exponent and nine mantissa bits: four times finer than
 // bf16 (whose rounding here alone made the gradients of rows and weights 1.3 times as inexact as the two roundings that
 // they cannot do without: 3.0e-3 against 2.4e-3 in the 2-norm), over 2^-30 .. 2^32, with gradual underflow to 2^-39.
@@ -366,9 +345,6 @@ __device__ __forceinline__ float unpack_pre(uint32_t code)                  // i
     // the largest exponent: fp32's largest, with the mantissa that there is
     return magnitude >= kPreInf << 14 ? __uint_as_float(sign | (0x7F800000u + (magnitude - (kPreInf << 14)))) : v;
 }
-
-// 1 / (1 + exp(-g)): the fast exponential and division are good to a few units of fp32, far below the bf16 results
-__device__ __forceinline__ float sigmoid(float g) { return __fdividef(1.0f, 1.0f + __expf(-g)); }
 
 // Clears k rows valid .. 63 of this CTA's boxes in a ring slot (the loads brought rows of the next slot there).  The
 // release that tells of it comes from one lane, behind the others' fences.
@@ -914,49 +890,9 @@ static int launch_few_rows(const void* x, const void* weights, const uint32_t* o
     return COBALT_OK;
 }
 
-typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-static int encode_function(EncodeTiled* out)
-{
-    static std::atomic<EncodeTiled> cached{nullptr};         // the same for every device
-    EncodeTiled known = cached.load(std::memory_order_relaxed);
-    if (!known) {
-        void* f = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        COBALT_CUDA_TRY(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found));
-        if (found != cudaDriverEntryPointSuccess || !f) return COBALT_ERR_UNSUPPORTED;
-        known = reinterpret_cast<EncodeTiled>(f);
-        cached.store(known, std::memory_order_relaxed);
-    }
-    *out = known;
-    return COBALT_OK;
-}
-
-// A bf16 tensor of up to five dimensions, the first one contiguous; strides of the others in elements.
-static int make_map(CUtensorMap* map, const void* ptr, int rank, const uint64_t (&dim)[5], const uint64_t (&stride)[5], const uint32_t (&box)[5])
-{
-    EncodeTiled encode;
-    const int rc = encode_function(&encode);
-    if (rc != COBALT_OK) return rc;
-    cuuint64_t dims[5], bytes[4];
-    cuuint32_t boxes[5], ones[5] = {1, 1, 1, 1, 1};
-    for (int i = 0; i < rank; ++i) {
-        dims[i] = dim[i];
-        boxes[i] = box[i];
-        if (i > 0) bytes[i - 1] = stride[i] * 2;
-    }
-    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(ptr), dims, bytes, boxes, ones,
-                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? COBALT_OK : record_cuda_error(cudaErrorInvalidValue);
-}
-
 static int rows_map(CUtensorMap* map, const void* ptr, int64_t rows, int64_t columns, uint32_t box_rows)
 {
-    const uint64_t dim[5] = {static_cast<uint64_t>(columns), static_cast<uint64_t>(rows)}, stride[5] = {1, static_cast<uint64_t>(columns)};
-    const uint32_t box[5] = {kBlockK, box_rows};
-    return make_map(map, ptr, 2, dim, stride, box);
+    return matrix_map(map, ptr, rows, columns, kBlockK, box_rows);
 }
 
 static int weights_map(CUtensorMap* map, const void* ptr, int64_t E, int64_t rows, int64_t columns, uint32_t box_rows)
@@ -1026,12 +962,6 @@ static int check_ffn(int64_t P, int32_t D, int32_t E, int32_t H, int32_t F)
         return COBALT_ERR_UNSUPPORTED;
     return COBALT_OK;
 }
-
-#define COBALT_TRY(expr)                       \
-    do {                                       \
-        const int cobalt_rc__ = (expr);        \
-        if (cobalt_rc__ != COBALT_OK) return cobalt_rc__; \
-    } while (0)
 
 }  // namespace cobalt
 

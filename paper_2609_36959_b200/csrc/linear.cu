@@ -1,0 +1,692 @@
+// A dense product with its elementwise part, and its gradients.
+//
+//   pre = x W^T + b      out = act(pre) + residual            x [T, K], W [N, K], bf16, or e4m3 with a scale for each row
+//   d = dout act'(pre)   dx = d W   dW = d^T x   db = sum_t d
+//
+// Three products, one kernel template (tcgen05, fp32 accumulators in tensor memory).  All of them have the form
+//   D[j][i] = sum_k A(i, k) B(j, k)     with i contiguous in the result:
+//   forward  i = feature, j = token, k over K      A = W, B = x
+//   dx       i = column of x, j = token, k over N  A = W transposed, B = d
+//   dW       i = column of x, j = feature, k over T   A = x transposed, B = d transposed
+//
+//   - A CTA pair computes 256 of i (M, 128 a CTA) by n of j (N, a multiple of 32 up to 256).  Warp 0 of each CTA feeds a ring of
+//     128-byte deep blocks by tensor-map loads, warp 1 of the leading CTA issues the products, warps 2 to 5 run the epilogue
+//     under the products of the next tile (two accumulators).
+//   - Persistent pairs deal the tiles round robin.  Where a product has fewer tiles than there are pairs, k is split; the parts
+//     go to the workspace in fp32 and a second kernel adds them in order and runs the epilogue.
+//   - The epilogue passes an accumulator through shared memory, 32 columns of j at a time, so that a thread has eight
+//     neighbouring i of one j: bias, scales, residual and result move in 16-byte vectors, and the 128 i that share a scale when
+//     pre is kept in 8 bits are sixteen neighbouring lanes.
+//
+// Every wait is bounded: when one runs out the kernel sets COBALT_DEVERR_WAIT_TIMEOUT, drains its copies, frees its tensor
+// memory and returns.
+#include "packed.cuh"
+#include "tcgen05.cuh"
+#include "tensor_map.cuh"
+
+namespace cobalt {
+
+typedef __nv_bfloat16 bf16;
+
+constexpr int kTileM = 256;              // i of a pair
+constexpr int kTileN = 256;              // most j of a tile
+constexpr int kDeepBytes = 128;          // depth of one ring slot: one swizzle row
+constexpr int kDeep = kDeepBytes / 2;    // in bf16 values
+constexpr int kHalfBytes = 128 * kDeepBytes;
+constexpr int kSlotBytes = 2 * kHalfBytes;
+constexpr int kBoxBytes = 64 * kDeepBytes;       // MN-major box: 64 values of M or N x 64 of k
+constexpr int kRing = 6;
+constexpr int kPitch = 528;              // epilogue staging: 128 fp32 values of a j, an odd number of 16-byte units
+constexpr int kStaging = 2 * 32 * kPitch;
+constexpr int kLinearSmem = kRing * kSlotBytes + kStaging + 256;
+constexpr int kLinearThreads = 192;
+constexpr int kBand = 8;                 // tiles of j that run together for every tile of i
+
+enum Product { kForward, kForwardE4M3, kGradRows, kGradWeights };
+
+// The elementwise part of the forward call.
+struct Finish {
+    const bf16* bias;                    // or null
+    const void* residual;                // or null, of the result's type
+    const float* x_scales;               // e4m3 only
+    const float* w_scales;
+    int act;
+    int f32;                             // the result's type
+    void* pre;                           // or null
+    float* pre_scales;                   // pre in 8 bits
+};
+
+struct LinearArgs {
+    int I, J;
+    int n, m_tiles, j_tiles, splits, blocks, per_split;      // blocks of k: all, and those of a split
+    void* out;
+    float* partial;                      // [splits][J][I] where splits > 1
+    Finish finish;
+    uint32_t* err_word;
+};
+
+__device__ __forceinline__ float act_value(int act, float v)
+{
+    if (act == COBALT_ACT_RELU) return v < 0.0f ? 0.0f : v;                          // a NaN stays
+    if (act == COBALT_ACT_SILU) return v * sigmoid(v);
+    if (act == COBALT_ACT_GELU) return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
+    return v;
+}
+
+__device__ __forceinline__ float act_slope(int act, float v)
+{
+    if (act == COBALT_ACT_RELU) return v > 0.0f ? 1.0f : 0.0f;
+    if (act == COBALT_ACT_SILU) {
+        const float s = sigmoid(v);
+        return s * (1.0f + v * (1.0f - s));
+    }
+    if (act == COBALT_ACT_GELU)
+        return 0.5f * (1.0f + erff(v * 0.70710678118654752f)) + v * 0.39894228040143268f * __expf(-0.5f * v * v);
+    return 1.0f;
+}
+
+// Eight neighbouring values as fp32, from bf16 or fp32 memory, and back.
+__device__ __forceinline__ void load8(const void* p, int64_t at, bool f32, float (&v)[8])
+{
+    if (f32) {
+        float a[4], b[4];
+        Vec16<float>::unpack(ld_once16(static_cast<const float*>(p) + at), a);
+        Vec16<float>::unpack(ld_once16(static_cast<const float*>(p) + at + 4), b);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = a[k], v[4 + k] = b[k];
+    } else {
+        Vec16<bf16>::unpack(ld_once16(static_cast<const bf16*>(p) + at), v);
+    }
+}
+
+__device__ __forceinline__ void store8(void* p, int64_t at, bool f32, const float (&v)[8])
+{
+    if (f32) {
+        const float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
+        *reinterpret_cast<uint4*>(static_cast<float*>(p) + at) = Vec16<float>::pack(a);
+        *reinterpret_cast<uint4*>(static_cast<float*>(p) + at + 4) = Vec16<float>::pack(b);
+    } else {
+        *reinterpret_cast<uint4*>(static_cast<bf16*>(p) + at) = Vec16<bf16>::pack(v);
+    }
+}
+
+// What the epilogue needs of eight features, whatever the token.
+struct FeatureConstants {
+    float bias[8], scale[8];
+    __device__ __forceinline__ void load(const Finish& f, int i0, bool mine)
+    {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) bias[k] = 0.0f, scale[k] = 1.0f;
+        if (mine && f.bias) Vec16<bf16>::unpack(__ldg(reinterpret_cast<const uint4*>(f.bias + i0)), bias);
+        if (mine && f.w_scales) {
+            const float4 a = __ldg(reinterpret_cast<const float4*>(f.w_scales + i0)), b = __ldg(reinterpret_cast<const float4*>(f.w_scales + i0 + 4));
+            scale[0] = a.x, scale[1] = a.y, scale[2] = a.z, scale[3] = a.w;
+            scale[4] = b.x, scale[5] = b.y, scale[6] = b.z, scale[7] = b.w;
+        }
+    }
+};
+
+// The result for features i0 .. i0 + 7 of token j from their sums.  All sixteen lanes of 128 features are here together
+// (`mine` says which of them have a result).
+template <int kProduct>
+__device__ __forceinline__ void finish8(const LinearArgs& p, int64_t j, int i0, bool mine, const FeatureConstants& c, float (&v)[8])
+{
+    const Finish& f = p.finish;
+    const int64_t at = j * p.I + i0;
+    if (kProduct == kForward || kProduct == kForwardE4M3) {
+        if (kProduct == kForwardE4M3) {
+            const float sx = mine ? __ldg(f.x_scales + j) : 0.0f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] *= sx * c.scale[k];
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] += c.bias[k];
+        if (f.pre_scales) {
+            uint32_t most = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) most = abs_max(most, v[k]);
+            if (!mine) most = 0;
+#pragma unroll
+            for (int off = 1; off < 16; off <<= 1) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, off));
+            const GroupScale g = GroupScale::of<CodeI8>(most);
+            if (mine) {
+                float t[2][4];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) t[k / 4][k % 4] = g.factor > 0.0f ? v[k] * g.factor : 0.0f;
+                *reinterpret_cast<uint2*>(static_cast<uint8_t*>(f.pre) + at) = make_uint2(CodeI8::encode4(t[0]), CodeI8::encode4(t[1]));
+                if (i0 % kPackGroup == 0) f.pre_scales[j * ((p.I + kPackGroup - 1) / kPackGroup) + i0 / kPackGroup] = g.scale;
+            }
+        } else if (f.pre && mine) {
+            store8(f.pre, at, false, v);
+        }
+        if (f.act != COBALT_ACT_NONE) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = act_value(f.act, v[k]);
+        }
+        if (f.residual && mine) {
+            float r[8];
+            load8(f.residual, at, f.f32, r);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] += r[k];
+        }
+        if (mine) store8(p.out, at, f.f32, v);
+    } else if (mine) {
+        store8(p.out, at, false, v);
+    }
+}
+
+struct LinearTile {
+    int i0, j0, split, first, blocks;    // first block of k, and how many
+};
+
+__device__ __forceinline__ LinearTile linear_tile(const LinearArgs& p, int t)
+{
+    LinearTile r;
+    const int each = p.m_tiles * p.j_tiles;
+    r.split = t / each;
+    const int in = t - r.split * each, band = in / (kBand * p.m_tiles), high = min(kBand, p.j_tiles - band * kBand), at = in - band * kBand * p.m_tiles;
+    r.j0 = (band * kBand + at % high) * p.n;
+    r.i0 = at / high * kTileM;
+    r.first = r.split * p.per_split;
+    r.blocks = min(p.per_split, p.blocks - r.first);
+    return r;
+}
+
+template <int kProduct>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinearThreads, 1)
+linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ LinearArgs p)
+{
+    constexpr bool kAMn = kProduct == kGradRows || kProduct == kGradWeights, kBMn = kProduct == kGradWeights;
+    constexpr int kStepK = kProduct == kForwardE4M3 ? kDeepBytes : kDeep;                // values of k in a block
+    extern __shared__ __align__(1024) uint8_t smem[];                    // the swizzle counts from 1024-byte boundaries
+    const uint32_t base = smem_u32(smem), staging = base + kRing * kSlotBytes, bars = staging + kStaging;
+    const uint32_t ready = bars, empty = bars + 8 * kRing, acc_full = bars + 16 * kRing, acc_empty = acc_full + 16, drain = acc_full + 32,
+                   tmem_slot = acc_full + 40;
+    const int warp = __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kRing; ++i) {
+            barrier_init(ready + 8 * i, 2);      // leading CTA: both CTAs' loads of the slot
+            barrier_init(empty + 8 * i, 1);      // the products that read the slot are done
+        }
+        for (int i = 0; i < 2; ++i) {
+            barrier_init(acc_full + 8 * i, 1);
+            barrier_init(acc_empty + 8 * i, 8);  // leading CTA: four epilogue warps of each CTA
+        }
+        barrier_init(drain, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        prefetch_map(&map_a);
+        prefetch_map(&map_b);
+    }
+    if (warp == 1) tmem_alloc_pair(tmem_slot, 512);
+    tmem_fence_before();
+    cluster_sync();
+    tmem_fence_after();
+    wait_for_prior_kernel();
+    launch_dependents();
+    uint32_t tmem;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot) : "memory");
+
+    const int tiles = p.m_tiles * p.j_tiles * p.splits, first = blockIdx.x >> 1, step = gridDim.x >> 1;
+    bool ok = true;                              // no wait has run out
+
+    if (warp == 0) {
+        // ---- loads of this CTA's halves --------------------------------------------------------------------
+        const uint32_t pair_ready = peer_address(ready, 0);
+        const uint64_t policy = policy_normal();
+        const int half = p.n / 2;
+        Ring ring;
+        int64_t issued = 0;
+        for (int t = first; t < tiles && ok; t += step) {
+            const LinearTile w = linear_tile(p, t);
+            // boxes wholly outside their tensor are left out: what is in the slot then only reaches results that are not stored
+            const int i0 = w.i0 + static_cast<int>(rank) * 128, j0 = w.j0 + static_cast<int>(rank) * half;
+            const int boxes_a = i0 >= p.I ? 0 : !kAMn || i0 + 64 >= p.I ? 1 : 2;
+            const int boxes_b = j0 >= p.J ? 0 : kBMn ? min((half + 63) / 64, (p.J - j0 + 63) / 64) : 1;
+            const uint32_t bytes = boxes_a * (kAMn ? kBoxBytes : kHalfBytes) + boxes_b * (kBMn ? kBoxBytes : half * kDeepBytes);
+            for (int k = w.first; k < w.first + w.blocks; ++k) {
+                if (!(ok = barrier_wait(empty + 8 * ring.slot, ring.phase ^ 1))) break;
+                const uint32_t bar = pair_ready + 8 * ring.slot, a = base + ring.slot * kSlotBytes, b = a + kHalfBytes;
+                if (elect_one()) {
+                    barrier_expect_cluster(bar, bytes);
+                    if (kAMn) {
+                        if (boxes_a > 0) tma_load_2d(a, &map_a, bar, policy, i0, k * kStepK);
+                        if (boxes_a > 1) tma_load_2d(a + kBoxBytes, &map_a, bar, policy, i0 + 64, k * kStepK);
+                    } else if (boxes_a > 0) {
+                        tma_load_2d(a, &map_a, bar, policy, k * kStepK, i0);
+                    }
+                    if (kBMn) {
+                        if (boxes_b > 0) tma_load_2d(b, &map_b, bar, policy, j0, k * kStepK);
+                        if (boxes_b > 1) tma_load_2d(b + kBoxBytes, &map_b, bar, policy, j0 + 64, k * kStepK);
+                    } else if (boxes_b > 0) {
+                        tma_load_2d(b, &map_b, bar, policy, k * kStepK, j0);
+                    }
+                }
+                __syncwarp();
+                ring.next<kRing>();
+                ++issued;
+            }
+        }
+        if (!ok) {
+            // the copies in flight have to land before the pair's shared memory is given back: the leading CTA waits for
+            // its last blocks, which the other CTA's copies count on too, and once more for a block that will not be
+            // complete, for those of the other CTA that are further ahead
+            if (lane == 0) flag_error(p.err_word, COBALT_DEVERR_WAIT_TIMEOUT);
+            if (rank == 0)
+                for (int64_t i = issued > kRing ? issued - kRing : 0; i <= issued; ++i)
+                    (void)barrier_wait(ready + 8 * static_cast<int>(i % kRing), static_cast<uint32_t>(i / kRing) & 1);
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        // ---- products (leading CTA) ------------------------------------------------------------------------------
+        Ring ring;
+        int turn = 0;                            // accumulators used so far
+        const uint32_t idesc = kProduct == kForwardE4M3 ? instruction_descriptor_e4m3(p.n) : instruction_descriptor(p.n, kAMn, kBMn);
+        for (int t = first; t < tiles && ok && rank == 0; t += step) {
+            const LinearTile w = linear_tile(p, t);
+            const uint32_t acc = turn & 1, d = tmem + acc * 256;
+            if (!(ok = barrier_wait(acc_empty + 8 * acc, ((turn >> 1) & 1) ^ 1))) break;
+            tmem_fence_after();
+            for (int k = 0; k < w.blocks; ++k) {
+                const uint32_t a = base + ring.slot * kSlotBytes;
+                if (!(ok = barrier_wait(ready + 8 * ring.slot, ring.phase))) break;
+                tmem_fence_after();
+                if (elect_one()) {
+                    // K-major: 32 bytes further in the swizzled row; MN-major: two 8-row groups
+                    const uint64_t da = matrix_descriptor(a, kAMn ? kBoxBytes : 16, 1024), db = matrix_descriptor(a + kHalfBytes, kBMn ? kBoxBytes : 16, 1024);
+                    constexpr uint32_t step_a = (kAMn ? 2048 : 32) >> 4, step_b = (kBMn ? 2048 : 32) >> 4;
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i) {
+                        if (kProduct == kForwardE4M3) mma_pair_e4m3(d, da + i * step_a, db + i * step_b, idesc, k > 0 || i > 0);
+                        else mma_pair(d, da + i * step_a, db + i * step_b, idesc, k > 0 || i > 0);
+                    }
+                    mma_commit_pair(empty + 8 * ring.slot);
+                }
+                __syncwarp();
+                ring.next<kRing>();
+            }
+            if (ok) {
+                if (elect_one()) mma_commit_pair(acc_full + 8 * acc);
+                __syncwarp();
+            }
+            ++turn;
+        }
+        if (!ok) {
+            if (lane == 0) flag_error(p.err_word, COBALT_DEVERR_WAIT_TIMEOUT);
+            if (elect_one()) mma_commit_pair(drain);     // products in flight end before the tensor memory is freed
+            (void)barrier_wait(drain, 0);
+        }
+        __syncwarp();
+    } else {
+        // ---- epilogue: quarter of the tensor memory lanes by warp, 32 accumulator columns at a time ---------------
+        const int quarter = warp & 3, tid = threadIdx.x - 64;
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(32 * quarter) << 16);
+        int turn = 0, chunk_turn = 0;
+        for (int t = first; t < tiles; t += step, ++turn) {
+            const LinearTile w = linear_tile(p, t);
+            const uint32_t acc = turn & 1;
+            const int i_cta = w.i0 + static_cast<int>(rank) * 128, i8 = i_cta + 8 * (tid & 15), columns = min(p.n, p.J - w.j0);
+            FeatureConstants constants;
+            if ((kProduct == kForward || kProduct == kForwardE4M3) && p.splits == 1) constants.load(p.finish, i8, i8 < p.I);
+            // one verdict for the four warps: none is left alone at the barriers below
+            ok = named_barrier_and(1, 128, barrier_wait(acc_full + 8 * acc, (turn >> 1) & 1));
+            if (!ok) break;
+            tmem_fence_after();
+            for (int c = 0; c < columns; c += 32, ++chunk_turn) {
+                uint32_t r[32];
+                tmem_load_32x32(lanes + acc * 256 + c, r);
+                if (p.splits > 1) {
+                    const int i = i_cta + 32 * quarter + lane;
+                    if (i < p.I) {
+                        float* out = p.partial + (static_cast<int64_t>(w.split) * p.J + w.j0 + c) * p.I + i;
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            if (c + k < columns) out[static_cast<int64_t>(k) * p.I] = __uint_as_float(r[k]);
+                    }
+                    continue;
+                }
+                const uint32_t buf = staging + (chunk_turn & 1) * (32 * kPitch), at = buf + (32 * quarter + lane) * 4;
+#pragma unroll
+                for (int k = 0; k < 32; ++k) asm volatile("st.shared.u32 [%0], %1;" ::"r"(at + k * kPitch), "r"(r[k]) : "memory");
+                named_barrier(1, 128);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int col = 8 * i + (tid >> 4);
+                    const uint4 lo = load_shared16(buf + col * kPitch + (tid & 15) * 32), hi = load_shared16(buf + col * kPitch + (tid & 15) * 32 + 16);
+                    float v[8] = {__uint_as_float(lo.x), __uint_as_float(lo.y), __uint_as_float(lo.z), __uint_as_float(lo.w),
+                                  __uint_as_float(hi.x), __uint_as_float(hi.y), __uint_as_float(hi.z), __uint_as_float(hi.w)};
+                    finish8<kProduct>(p, w.j0 + c + col, i8, c + col < columns && i8 < p.I, constants, v);
+                }
+            }
+            tmem_fence_before();
+            __syncwarp();
+            if (lane == 0) barrier_arrive_tmem(peer_address(acc_empty + 8 * acc, 0));
+        }
+        if (!ok && lane == 0) flag_error(p.err_word, COBALT_DEVERR_WAIT_TIMEOUT);
+        __syncwarp();
+    }
+    tmem_fence_before();
+    cluster_sync();                              // no CTA leaves while the other may still reach its barriers
+    tmem_fence_after();
+    if (warp == 1) tmem_free_pair(tmem, 512);
+}
+
+// Adds the parts of a split product in order and finishes: eight neighbouring i of one j a thread, sixteen lanes 128 of i.
+template <int kProduct>
+__global__ void __launch_bounds__(256)
+linear_join_kernel(const __grid_constant__ LinearArgs p)
+{
+    wait_for_prior_kernel();
+    launch_dependents();
+    const int per_row = (p.I + 127) / 128 * 16;
+    const int64_t index = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, j = index / per_row;
+    const int i8 = static_cast<int>(index - j * per_row) * 8;
+    const bool mine = j < p.J && i8 < p.I;
+    FeatureConstants constants;
+    if (kProduct == kForward || kProduct == kForwardE4M3) constants.load(p.finish, i8, mine);
+    float v[8] = {};
+    if (mine) {
+        const float* from = p.partial + j * p.I + i8;
+        const int64_t stride = static_cast<int64_t>(p.J) * p.I;
+#pragma unroll 4
+        for (int s = 0; s < p.splits; ++s) {
+            float a[4], b[4];
+            Vec16<float>::unpack(ld_once16(from + s * stride), a);
+            Vec16<float>::unpack(ld_once16(from + s * stride + 4), b);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] += a[k], v[4 + k] += b[k];
+        }
+    }
+    finish8<kProduct>(p, j, i8, mine, constants, v);
+}
+
+// d = dout act'(pre) in bf16 (where the products need it) and its column sums: a CTA has 128 features and a slice of the
+// tokens, sixteen at a time; the sums of its sixteen token rows are added in order and written to partial [gridDim.y][N].
+struct GradPreArgs {
+    const void* grad_out;
+    const void* pre;                     // or null
+    const float* pre_scales;             // pre in 8 bits
+    int64_t T;
+    int N, act, f32;
+    bf16* grad_pre;                      // or null
+    float* partial;                      // or null
+};
+
+__global__ void __launch_bounds__(256)
+linear_grad_pre_kernel(const GradPreArgs p)
+{
+    __shared__ float sums[16][128];
+    wait_for_prior_kernel();
+    launch_dependents();
+    const int i8 = (blockIdx.x * 16 + (threadIdx.x & 15)) * 8, own = threadIdx.x >> 4, groups = (p.N + kPackGroup - 1) / kPackGroup;
+    const int64_t step = static_cast<int64_t>(gridDim.y) * 16;
+    float total[8] = {};
+    if (i8 < p.N) {
+        for (int64_t t = static_cast<int64_t>(blockIdx.y) * 16 + own; t < p.T; t += step) {
+            const int64_t at = t * p.N + i8;
+            float d[8];
+            load8(p.grad_out, at, p.f32, d);
+            if (p.act != COBALT_ACT_NONE) {
+                float v[8];
+                if (p.pre_scales) {
+                    const uint2 codes = __ldcs(reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(p.pre) + at));
+                    const float scale = __ldg(p.pre_scales + t * groups + blockIdx.x);
+                    float a[4], b[4];
+                    CodeI8::decode4(codes.x, a);
+                    CodeI8::decode4(codes.y, b);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] = a[k] * scale, v[4 + k] = b[k] * scale;
+                } else {
+                    load8(p.pre, at, false, v);
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) d[k] *= act_slope(p.act, v[k]);
+            }
+            if (p.grad_pre) store8(p.grad_pre, at, false, d);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) total[k] += d[k];
+        }
+    }
+    if (!p.partial) return;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sums[own][8 * (threadIdx.x & 15) + k] = total[k];
+    __syncthreads();
+    const int i = blockIdx.x * 128 + threadIdx.x;
+    if (threadIdx.x < 128 && i < p.N) {
+        float s = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s += sums[r][threadIdx.x];
+        p.partial[static_cast<int64_t>(blockIdx.y) * p.N + i] = s;
+    }
+}
+
+// grad_bias: the parts' sums, eight threads a feature.
+__global__ void __launch_bounds__(256)
+linear_bias_kernel(const float* partial, int parts, int N, bf16* __restrict__ grad_bias)
+{
+    __shared__ float slice[8][33];
+    wait_for_prior_kernel();
+    launch_dependents();
+    const int lane = threadIdx.x & 31, own = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;
+    float s = 0.0f;
+    if (i < N)
+        for (int k = own; k < parts; k += 8) s += partial[static_cast<int64_t>(k) * N + i];
+    slice[own][lane] = s;
+    __syncthreads();
+    if (own == 0 && i < N) {
+        float total = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) total += slice[k][lane];
+        grad_bias[i] = __float2bfloat16_rn(total);
+    }
+}
+
+// ---- host side ----------------------------------------------------------------------------------------------------
+
+constexpr int kPlanPairs = 74;           // the plan is the same on every device: it counts with the pairs of 148 SMs
+
+struct LinearPlan {
+    int n, splits, per_split;
+};
+
+constexpr int kMostSplits = 32;
+constexpr int kMostParts = 4 * kPlanPairs;       // tiles of all splits together, where k is split
+
+// n and the number of splits with the least estimated cycles: waves of tiles, a block of k taking 2n cycles on the tensor cores (at least
+// what its loads take), a fixed part for filling and emptying a tile, and the parts' way through L2 where k is split.
+static LinearPlan linear_plan(int64_t I, int64_t J, int64_t blocks)
+{
+    static const int kSplits[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32};
+    LinearPlan best = {32, 1, static_cast<int>(blocks)};
+    double least = 1e300;
+    const int64_t m_tiles = (I + kTileM - 1) / kTileM;
+    for (int n = 32; n <= kTileN; n += 32) {
+        if (n > 32 && n - 32 >= J) break;
+        const int64_t tiles = m_tiles * ((J + n - 1) / n);
+        const double block = 2.0 * n + 64.0 > 400.0 ? 2.0 * n + 64.0 : 400.0;
+        for (int s : kSplits) {
+            if (s > 1 && (s > blocks || tiles * s > kMostParts || tiles >= 2 * kPlanPairs)) break;
+            const int64_t per = (blocks + s - 1) / s, waves = (tiles * s + kPlanPairs - 1) / kPlanPairs;
+            if (per * (s - 1) >= blocks) continue;                 // a split without blocks
+            double cycles = static_cast<double>(waves) * (per * block + 800.0) + 2500.0;
+            if (s > 1) cycles += 4000.0 + static_cast<double>(s) * I * J * 8.0 / 2500.0;
+            if (cycles < least) {
+                least = cycles;
+                best = {n, s, static_cast<int>(per)};
+            }
+        }
+    }
+    return best;
+}
+
+// At least what the plan's parts take.
+static size_t part_bytes(int64_t I, int64_t J)
+{
+    const int64_t tiles = ((I + kTileM - 1) / kTileM) * ((J + kTileN - 1) / kTileN);
+    if (tiles >= 2 * kPlanPairs) return 0;
+    const int64_t by_splits = kMostSplits * I * J, by_tiles = static_cast<int64_t>(kMostParts) * kTileM * kTileN;
+    return static_cast<size_t>(by_splits < by_tiles ? by_splits : by_tiles) * sizeof(float);
+}
+
+static int64_t deep_blocks(int64_t k, int deep) { return (k + deep - 1) / deep; }
+
+// Slices of the tokens in the pass over the output's gradient: about four CTAs an SM.
+static int bias_parts(int64_t T, int N)
+{
+    const int64_t groups = (N + 127) / 128, rows = (T + 15) / 16;
+    int64_t parts = (4 * 2 * kPlanPairs + groups - 1) / groups;
+    if (parts > rows) parts = rows;
+    return static_cast<int>(parts < 1 ? 1 : parts);
+}
+
+static int check_linear(int64_t T, int32_t K, int32_t N, int deep_unit)
+{
+    if (T < 0 || K < 1 || N < 1) return COBALT_ERR_INVALID_ARG;
+    if (T > (1ll << 31) - (1ll << 21) || K % deep_unit != 0 || N % 8 != 0 || K > COBALT_LINEAR_MAX_WIDTH || N > COBALT_LINEAR_MAX_WIDTH)
+        return COBALT_ERR_UNSUPPORTED;
+    return COBALT_OK;
+}
+
+static size_t linear_workspace(int64_t T, int32_t K, int32_t N)
+{
+    if (T == 0) return 256;
+    size_t most = static_cast<size_t>(bias_parts(T, N)) * N * sizeof(float);
+    const size_t all[3] = {part_bytes(N, T), part_bytes(K, T), part_bytes(K, N)};
+    for (size_t b : all) most = b > most ? b : most;
+    return round_up(most > 0 ? most : 1, 256);
+}
+
+// May start while the kernel before it is at its end; every kernel here waits for that one before it touches memory.
+template <typename... Params, typename... Args>
+static int launch_after(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, Args... args)
+{
+    cudaLaunchAttribute attr;
+    set_programmatic_launch(&attr, true);
+    cudaLaunchConfig_t config = {};
+    config.gridDim = grid;
+    config.blockDim = block;
+    config.dynamicSmemBytes = smem;
+    config.stream = s;
+    config.attrs = &attr;
+    config.numAttrs = 1;
+    COBALT_CUDA_TRY(cudaLaunchKernelEx(&config, kernel, args...));
+    return COBALT_OK;
+}
+
+// a: [I, k] or, transposed, [k, I]; b: [J, k] or [k, J].
+template <int kProduct>
+static int launch_product(const void* a, const void* b, int64_t I, int64_t J, int64_t k, LinearArgs p, void* workspace, cudaStream_t s)
+{
+    constexpr bool kAMn = kProduct == kGradRows || kProduct == kGradWeights, kBMn = kProduct == kGradWeights;
+    constexpr int kBytes = kProduct == kForwardE4M3 ? 1 : 2, kStepK = kDeepBytes / kBytes;
+    const int64_t blocks = deep_blocks(k, kStepK);
+    const LinearPlan plan = linear_plan(I, J, blocks);
+    p.I = static_cast<int>(I);
+    p.J = static_cast<int>(J);
+    p.n = plan.n;
+    p.m_tiles = static_cast<int>((I + kTileM - 1) / kTileM);
+    p.j_tiles = static_cast<int>((J + plan.n - 1) / plan.n);
+    p.splits = plan.splits;
+    p.blocks = static_cast<int>(blocks);
+    p.per_split = plan.per_split;
+    p.partial = static_cast<float*>(workspace);
+    CUtensorMap map_a, map_b;
+    COBALT_TRY(kAMn ? matrix_map(&map_a, a, k, I, 64, kDeep) : matrix_map(&map_a, a, I, k, kStepK, 128, kBytes));
+    COBALT_TRY(kBMn ? matrix_map(&map_b, b, k, J, 64, kDeep) : matrix_map(&map_b, b, J, k, kStepK, plan.n / 2, kBytes));
+    COBALT_TRY(ensure_kernel_attributes(reinterpret_cast<const void*>(linear_kernel<kProduct>), kLinearSmem, false));
+    int sms = 0;
+    COBALT_TRY(sm_count(&sms));
+    const int64_t tiles = static_cast<int64_t>(p.m_tiles) * p.j_tiles * p.splits, pairs = tiles < sms / 2 ? tiles : sms / 2;
+    if (tiles >= (1ll << 31) - (1 << 16)) return COBALT_ERR_UNSUPPORTED;
+    COBALT_TRY(launch_after(linear_kernel<kProduct>, dim3(static_cast<unsigned>(2 * (pairs < 1 ? 1 : pairs))), dim3(kLinearThreads), kLinearSmem, s,
+                            map_a, map_b, p));
+    if (p.splits == 1) return COBALT_OK;
+    const int64_t threads = J * ((I + 127) / 128 * 16);
+    return launch_after(linear_join_kernel<kProduct>, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, s, p);
+}
+
+}  // namespace cobalt
+
+using namespace cobalt;
+
+extern "C" {
+
+size_t cobalt_linear_workspace_bytes(int64_t T, int32_t K, int32_t N)
+{
+    if (check_linear(T, K, N, 8) != COBALT_OK) return 0;
+    return linear_workspace(T, K, N);
+}
+
+int cobalt_linear(const void* x, const float* x_scales, const void* w, const float* w_scales, const void* bias, const void* residual, int64_t T,
+                  int32_t K, int32_t N, int32_t operand, int32_t act, int32_t out_type, void* pre, float* pre_scales, int32_t pre_type, void* out,
+                  void* workspace, size_t workspace_bytes, cobalt_stream_t stream)
+{
+    if ((operand != COBALT_BF16 && operand != COBALT_E4M3) || (out_type != COBALT_BF16 && out_type != COBALT_F32) || act < COBALT_ACT_NONE ||
+        act > COBALT_ACT_GELU || (pre && pre_type != COBALT_BF16 && pre_type != COBALT_I8))
+        return COBALT_ERR_INVALID_ARG;
+    const bool e4m3 = operand == COBALT_E4M3, pre8 = pre && pre_type == COBALT_I8;
+    COBALT_TRY(check_linear(T, K, N, e4m3 ? 16 : 8));
+    if (T == 0) return COBALT_OK;
+    if (!x || !w || !out || (e4m3 && (!x_scales || !w_scales)) || (pre8 && !pre_scales)) return COBALT_ERR_INVALID_ARG;
+    if (!aligned16(x) || !aligned16(x_scales) || !aligned16(w) || !aligned16(w_scales) || !aligned16(bias) || !aligned16(residual) ||
+        !aligned16(pre) || !aligned16(pre_scales) || !aligned16(out) || !aligned16(workspace))
+        return COBALT_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < linear_workspace(T, K, N)) return COBALT_ERR_WORKSPACE_TOO_SMALL;
+    LinearArgs p = {};
+    COBALT_TRY(device_error_word(&p.err_word));
+    p.out = out;
+    p.finish = {static_cast<const bf16*>(bias), residual, e4m3 ? x_scales : nullptr, e4m3 ? w_scales : nullptr, act, out_type == COBALT_F32, pre,
+                pre8 ? pre_scales : nullptr};
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return e4m3 ? launch_product<kForwardE4M3>(w, x, N, T, K, p, workspace, s) : launch_product<kForward>(w, x, N, T, K, p, workspace, s);
+}
+
+int cobalt_linear_backward(const void* grad_out, const void* x, const void* w, const void* pre, const float* pre_scales, int32_t pre_type,
+                           int64_t T, int32_t K, int32_t N, int32_t act, int32_t grad_type, void* grad_pre, void* grad_x, void* grad_w,
+                           void* grad_bias, void* workspace, size_t workspace_bytes, cobalt_stream_t stream)
+{
+    if ((grad_type != COBALT_BF16 && grad_type != COBALT_F32) || act < COBALT_ACT_NONE || act > COBALT_ACT_GELU ||
+        (act != COBALT_ACT_NONE && pre_type != COBALT_BF16 && pre_type != COBALT_I8))
+        return COBALT_ERR_INVALID_ARG;
+    COBALT_TRY(check_linear(T, K, N, 8));
+    const bool none = act == COBALT_ACT_NONE, pre8 = !none && pre_type == COBALT_I8, converts = !none || grad_type == COBALT_F32;
+    const bool products = grad_x || grad_w;
+    if (T > 0 && (!products && !grad_bias)) return COBALT_ERR_INVALID_ARG;
+    if (T > 0 && (!grad_out || (grad_x && !w) || (grad_w && !x) || (!none && !pre) || (pre8 && !pre_scales) || (products && converts && !grad_pre)))
+        return COBALT_ERR_INVALID_ARG;
+    if (!aligned16(grad_out) || !aligned16(x) || !aligned16(w) || !aligned16(pre) || !aligned16(pre_scales) || !aligned16(grad_pre) ||
+        !aligned16(grad_x) || !aligned16(grad_w) || !aligned16(grad_bias) || !aligned16(workspace))
+        return COBALT_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < linear_workspace(T, K, N)) return COBALT_ERR_WORKSPACE_TOO_SMALL;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (T == 0) {                                // no rows: the weights' gradients are 0
+        if (grad_w) COBALT_CUDA_TRY(cudaMemsetAsync(grad_w, 0, static_cast<size_t>(N) * K * sizeof(bf16), s));
+        if (grad_bias) COBALT_CUDA_TRY(cudaMemsetAsync(grad_bias, 0, static_cast<size_t>(N) * sizeof(bf16), s));
+        return COBALT_OK;
+    }
+    LinearArgs p = {};
+    COBALT_TRY(device_error_word(&p.err_word));
+    const void* d = grad_out;
+    if (grad_bias || (products && converts)) {
+        GradPreArgs g = {grad_out, pre, pre8 ? pre_scales : nullptr, T, N, act, grad_type == COBALT_F32,
+                         products && converts ? static_cast<bf16*>(grad_pre) : nullptr, grad_bias ? static_cast<float*>(workspace) : nullptr};
+        const int parts = bias_parts(T, N);
+        COBALT_TRY(launch_after(linear_grad_pre_kernel, dim3((N + 127) / 128, parts), dim3(256), 0, s, g));
+        if (grad_bias)
+            COBALT_TRY(launch_after(linear_bias_kernel, dim3((N + 31) / 32), dim3(256), 0, s, static_cast<const float*>(g.partial), parts, N,
+                                    static_cast<bf16*>(grad_bias)));
+        if (converts) d = grad_pre;
+    }
+    if (grad_x) {
+        p.out = grad_x;
+        COBALT_TRY(launch_product<kGradRows>(w, d, K, T, N, p, workspace, s));
+    }
+    if (grad_w) {
+        p.out = grad_w;
+        COBALT_TRY(launch_product<kGradWeights>(x, d, K, N, T, p, workspace, s));
+    }
+    return COBALT_OK;
+}
+
+}  // extern "C"

@@ -1,4 +1,4 @@
-// sm_100a building blocks of the expert feed-forward products: mbarriers with bounded waits, tensor-map loads, the
+// sm_100a building blocks of the products on the tensor cores: mbarriers with bounded waits, tensor-map loads, the
 // tensor-core instructions of a CTA pair and the register/shared-memory moves of their epilogues (PTX ISA 8.7).
 #pragma once
 
@@ -187,6 +187,18 @@ __device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uin
         : "memory");
 }
 
+// The same for e4m3 operands, 32 values of k (formats 0 in the instruction descriptor).
+__device__ __forceinline__ constexpr uint32_t instruction_descriptor_e4m3(uint32_t n) { return (1u << 4) | ((n >> 3) << 17) | ((256u >> 4) << 24); }
+
+__device__ __forceinline__ void mma_pair_e4m3(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(accumulate))
+        : "memory");
+}
+
 // Arrives at the barrier at this offset in both CTAs once the products issued so far are done.
 __device__ __forceinline__ void mma_commit_pair(uint32_t bar)
 {
@@ -204,6 +216,21 @@ __device__ __forceinline__ void tmem_load_16x32(uint32_t addr, uint32_t (&r)[16]
         "tcgen05.wait::ld.sync.aligned;"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
           "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr)
+        : "memory");
+}
+
+// 32 lanes x 32 columns of tensor memory, waited for: r[c] is column c of TMEM lane `lane`.
+__device__ __forceinline__ void tmem_load_32x32(uint32_t addr, uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
+          "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]),
+          "=r"(r[30]), "=r"(r[31])
         : "r"(addr)
         : "memory");
 }
@@ -253,6 +280,20 @@ __device__ __forceinline__ bool named_barrier_and(int id, int threads, bool ok)
         : "memory");
     return all != 0;
 }
+
+// Position in the ring: slot and the parity of its present use.
+struct Ring {
+    int slot = 0;
+    uint32_t phase = 0;
+    template <int kRing>
+    __device__ __forceinline__ void next()
+    {
+        if (++slot == kRing) {
+            slot = 0;
+            phase ^= 1;
+        }
+    }
+};
 
 #endif  // __CUDACC__
 
