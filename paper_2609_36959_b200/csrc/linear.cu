@@ -10,7 +10,7 @@
 //   dW       i = column of x, j = feature, k over T   A = x transposed, B = d transposed
 //
 //   - A CTA pair computes 256 of i (M, 128 a CTA) by n of j (N, a multiple of 32 up to 256).  Warp 0 of each CTA feeds a ring of
-//     128-byte deep blocks by tensor-map loads, warp 1 of the leading CTA issues the products, warps 2 to 5 run the epilogue
+//     128-byte deep blocks by tensor-map loads, warp 1 of the leading CTA issues the products, warps 2 to 9 run the epilogue
 //     under the products of the next tile (two accumulators).
 //   - Persistent pairs deal the tiles round robin.  Where a product has fewer tiles than there are pairs, k is split; the parts
 //     go to the workspace in fp32 and a second kernel adds them in order and runs the epilogue.
@@ -36,13 +36,22 @@ constexpr int kHalfBytes = 128 * kDeepBytes;
 constexpr int kSlotBytes = 2 * kHalfBytes;
 constexpr int kBoxBytes = 64 * kDeepBytes;       // MN-major box: 64 values of M or N x 64 of k
 constexpr int kRing = 6;
-constexpr int kPitch = 528;              // epilogue staging: 128 fp32 values of a j, an odd number of 16-byte units
-constexpr int kStaging = 2 * 32 * kPitch;
+// Epilogue staging of a j's 128 values, an odd number of 16-byte units: 32 j in bf16, or 16 in fp32; two buffers for each of two
+// groups of four warps.
+constexpr int kPitch16 = 272, kPitch32 = 528;
+constexpr int kBuffer16 = 32 * kPitch16, kBuffer32 = 16 * kPitch32;
+constexpr int kStaging = 4 * (kBuffer16 > kBuffer32 ? kBuffer16 : kBuffer32);
 constexpr int kLinearSmem = kRing * kSlotBytes + kStaging + 256;
-constexpr int kLinearThreads = 192;
+constexpr int kLinearThreads = 320;
+constexpr int kLongBlocks = 8;           // blocks of k (512 values) that the tensor cores add up before fp32 registers take over
 constexpr int kBand = 8;                 // tiles of j that run together for every tile of i
 
 enum Product { kForward, kForwardE4M3, kGradRows, kGradWeights };
+
+// kPlain: bf16 results of bias, scales and activation alone.  kFull: any.  kLong: fp32 results; the tensor cores cut every addition (a sum
+// of 7168 products is 6.9e-6 too small, in proportion to their number), so 512 values are added there and the sums of those, rounded,
+// in registers (4.7e-7).
+enum Form { kPlain, kFull, kLong };
 
 // The elementwise part of the forward call.
 struct Finish {
@@ -65,11 +74,23 @@ struct LinearArgs {
     uint32_t* err_word;
 };
 
+// The normal distribution's cumulative function at v and exp(-v^2 / 2), by the rational approximation 7.1.26 of Abramowitz and
+// Stegun's Handbook (erf to 1.5e-7): no branch, a third of the instructions of erff and exp, and the epilogue is bound by them.
+__device__ __forceinline__ float2 normal_cdf(float v)
+{
+    const float a = fabsf(v) * 0.70710678118654752f, t = __fdividef(1.0f, fmaf(0.3275911f, a, 1.0f)), e = __expf(-0.5f * v * v);
+    float q = fmaf(t, 1.061405429f, -1.453152027f);
+    q = fmaf(t, q, 1.421413741f);
+    q = fmaf(t, q, -0.284496736f);
+    q = fmaf(t, q, 0.254829592f) * t * e * 0.5f;
+    return make_float2(v > 0.0f ? 1.0f - q : q, e);
+}
+
 __device__ __forceinline__ float act_value(int act, float v)
 {
     if (act == COBALT_ACT_RELU) return v < 0.0f ? 0.0f : v;                          // a NaN stays
     if (act == COBALT_ACT_SILU) return v * sigmoid(v);
-    if (act == COBALT_ACT_GELU) return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
+    if (act == COBALT_ACT_GELU) return v * normal_cdf(v).x;
     return v;
 }
 
@@ -80,8 +101,10 @@ __device__ __forceinline__ float act_slope(int act, float v)
         const float s = sigmoid(v);
         return s * (1.0f + v * (1.0f - s));
     }
-    if (act == COBALT_ACT_GELU)
-        return 0.5f * (1.0f + erff(v * 0.70710678118654752f)) + v * 0.39894228040143268f * __expf(-0.5f * v * v);
+    if (act == COBALT_ACT_GELU) {
+        const float2 c = normal_cdf(v);
+        return fmaf(v * 0.39894228040143268f, c.y, c.x);
+    }
     return 1.0f;
 }
 
@@ -192,7 +215,7 @@ __device__ __forceinline__ LinearTile linear_tile(const LinearArgs& p, int t)
     return r;
 }
 
-template <int kProduct>
+template <int kProduct, int kForm>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinearThreads, 1)
 linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ LinearArgs p)
 {
@@ -212,7 +235,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
         }
         for (int i = 0; i < 2; ++i) {
             barrier_init(acc_full + 8 * i, 1);
-            barrier_init(acc_empty + 8 * i, 8);  // leading CTA: four epilogue warps of each CTA
+            barrier_init(acc_empty + 8 * i, 16);  // leading CTA: eight epilogue warps of each CTA
         }
         barrier_init(drain, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -285,32 +308,34 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
         const uint32_t idesc = kProduct == kForwardE4M3 ? instruction_descriptor_e4m3(p.n) : instruction_descriptor(p.n, kAMn, kBMn);
         for (int t = first; t < tiles && ok && rank == 0; t += step) {
             const LinearTile w = linear_tile(p, t);
-            const uint32_t acc = turn & 1, d = tmem + acc * 256;
-            if (!(ok = barrier_wait(acc_empty + 8 * acc, ((turn >> 1) & 1) ^ 1))) break;
-            tmem_fence_after();
-            for (int k = 0; k < w.blocks; ++k) {
-                const uint32_t a = base + ring.slot * kSlotBytes;
-                if (!(ok = barrier_wait(ready + 8 * ring.slot, ring.phase))) break;
+            for (int k = 0; k < w.blocks && ok; ++turn) {
+                const uint32_t acc = turn & 1, d = tmem + acc * 256;
+                const int first_k = k, end = kForm == kLong ? min(w.blocks, k + kLongBlocks) : w.blocks;
+                if (!(ok = barrier_wait(acc_empty + 8 * acc, ((turn >> 1) & 1) ^ 1))) break;
                 tmem_fence_after();
-                if (elect_one()) {
-                    // K-major: 32 bytes further in the swizzled row; MN-major: two 8-row groups
-                    const uint64_t da = matrix_descriptor(a, kAMn ? kBoxBytes : 16, 1024), db = matrix_descriptor(a + kHalfBytes, kBMn ? kBoxBytes : 16, 1024);
-                    constexpr uint32_t step_a = (kAMn ? 2048 : 32) >> 4, step_b = (kBMn ? 2048 : 32) >> 4;
+                for (; k < end; ++k) {
+                    const uint32_t a = base + ring.slot * kSlotBytes;
+                    if (!(ok = barrier_wait(ready + 8 * ring.slot, ring.phase))) break;
+                    tmem_fence_after();
+                    if (elect_one()) {
+                        // K-major: 32 bytes further in the swizzled row; MN-major: two 8-row groups
+                        const uint64_t da = matrix_descriptor(a, kAMn ? kBoxBytes : 16, 1024), db = matrix_descriptor(a + kHalfBytes, kBMn ? kBoxBytes : 16, 1024);
+                        constexpr uint32_t step_a = (kAMn ? 2048 : 32) >> 4, step_b = (kBMn ? 2048 : 32) >> 4;
 #pragma unroll
-                    for (uint32_t i = 0; i < 4; ++i) {
-                        if (kProduct == kForwardE4M3) mma_pair_e4m3(d, da + i * step_a, db + i * step_b, idesc, k > 0 || i > 0);
-                        else mma_pair(d, da + i * step_a, db + i * step_b, idesc, k > 0 || i > 0);
+                        for (uint32_t i = 0; i < 4; ++i) {
+                            if (kProduct == kForwardE4M3) mma_pair_e4m3(d, da + i * step_a, db + i * step_b, idesc, k > first_k || i > 0);
+                            else mma_pair(d, da + i * step_a, db + i * step_b, idesc, k > first_k || i > 0);
+                        }
+                        mma_commit_pair(empty + 8 * ring.slot);
                     }
-                    mma_commit_pair(empty + 8 * ring.slot);
+                    __syncwarp();
+                    ring.next<kRing>();
                 }
-                __syncwarp();
-                ring.next<kRing>();
+                if (ok) {
+                    if (elect_one()) mma_commit_pair(acc_full + 8 * acc);
+                    __syncwarp();
+                }
             }
-            if (ok) {
-                if (elect_one()) mma_commit_pair(acc_full + 8 * acc);
-                __syncwarp();
-            }
-            ++turn;
         }
         if (!ok) {
             if (lane == 0) flag_error(p.err_word, COBALT_DEVERR_WAIT_TIMEOUT);
@@ -319,49 +344,148 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
         }
         __syncwarp();
     } else {
-        // ---- epilogue: quarter of the tensor memory lanes by warp, 32 accumulator columns at a time ---------------
-        const int quarter = warp & 3, tid = threadIdx.x - 64;
+        // ---- epilogue: two groups of four warps, each a quarter of the tensor memory lanes a warp, take 32 columns in turn ----------
+        const int quarter = warp & 3, group = (warp - 2) >> 2, tid = (threadIdx.x - 64) & 127;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(32 * quarter) << 16);
         int turn = 0, chunk_turn = 0;
-        for (int t = first; t < tiles; t += step, ++turn) {
-            const LinearTile w = linear_tile(p, t);
-            const uint32_t acc = turn & 1;
-            const int i_cta = w.i0 + static_cast<int>(rank) * 128, i8 = i_cta + 8 * (tid & 15), columns = min(p.n, p.J - w.j0);
-            FeatureConstants constants;
-            if ((kProduct == kForward || kProduct == kForwardE4M3) && p.splits == 1) constants.load(p.finish, i8, i8 < p.I);
-            // one verdict for the four warps: none is left alone at the barriers below
-            ok = named_barrier_and(1, 128, barrier_wait(acc_full + 8 * acc, (turn >> 1) & 1));
-            if (!ok) break;
-            tmem_fence_after();
-            for (int c = 0; c < columns; c += 32, ++chunk_turn) {
-                uint32_t r[32];
-                tmem_load_32x32(lanes + acc * 256 + c, r);
-                if (p.splits > 1) {
-                    const int i = i_cta + 32 * quarter + lane;
-                    if (i < p.I) {
-                        float* out = p.partial + (static_cast<int64_t>(w.split) * p.J + w.j0 + c) * p.I + i;
-#pragma unroll
-                        for (int k = 0; k < 32; ++k)
-                            if (c + k < columns) out[static_cast<int64_t>(k) * p.I] = __uint_as_float(r[k]);
-                    }
-                    continue;
-                }
-                const uint32_t buf = staging + (chunk_turn & 1) * (32 * kPitch), at = buf + (32 * quarter + lane) * 4;
-#pragma unroll
-                for (int k = 0; k < 32; ++k) asm volatile("st.shared.u32 [%0], %1;" ::"r"(at + k * kPitch), "r"(r[k]) : "memory");
-                named_barrier(1, 128);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int col = 8 * i + (tid >> 4);
-                    const uint4 lo = load_shared16(buf + col * kPitch + (tid & 15) * 32), hi = load_shared16(buf + col * kPitch + (tid & 15) * 32 + 16);
-                    float v[8] = {__uint_as_float(lo.x), __uint_as_float(lo.y), __uint_as_float(lo.z), __uint_as_float(lo.w),
-                                  __uint_as_float(hi.x), __uint_as_float(hi.y), __uint_as_float(hi.z), __uint_as_float(hi.w)};
-                    finish8<kProduct>(p, w.j0 + c + col, i8, c + col < columns && i8 < p.I, constants, v);
-                }
-            }
+        // one verdict for the eight warps: none is left alone at the barriers below
+        auto accumulator = [&]() {
+            ok = named_barrier_and(1, 256, barrier_wait(acc_full + 8 * (turn & 1), (turn >> 1) & 1));
+            if (ok) tmem_fence_after();
+            return ok;
+        };
+        auto release = [&]() {
             tmem_fence_before();
             __syncwarp();
-            if (lane == 0) barrier_arrive_tmem(peer_address(acc_empty + 8 * acc, 0));
+            if (lane == 0) barrier_arrive_tmem(peer_address(acc_empty + 8 * (turn & 1), 0));
+            ++turn;
+        };
+        for (int t = first; t < tiles; t += step) {
+            const LinearTile w = linear_tile(p, t);
+            const int i_cta = w.i0 + static_cast<int>(rank) * 128, i8 = i_cta + 8 * (tid & 15), columns = min(p.n, p.J - w.j0);
+            const bool split = p.splits > 1;
+            // 32 sums of one i: a split's part
+            auto store_part = [&](int c, const float (&r)[32]) {
+                const int i = i_cta + 32 * quarter + lane;
+                if (i >= p.I) return;
+                float* out = p.partial + (static_cast<int64_t>(w.split) * p.J + w.j0 + c) * p.I + i;
+#pragma unroll
+                for (int k = 0; k < 32; ++k)
+                    if (c + k < columns) out[static_cast<int64_t>(k) * p.I] = r[k];
+            };
+            FeatureConstants constants;
+            auto finish = [&](int c, const float (&r)[32]) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t buf = staging + (2 * group + h) * kBuffer32, at = buf + (32 * quarter + lane) * 4;
+#pragma unroll
+                    for (int k = 0; k < 16; ++k)
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + k * kPitch32), "f"(r[16 * h + k]) : "memory");
+                    named_barrier(2 + group, 128);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int col = 8 * i + (tid >> 4);
+                        const uint4 lo = load_shared16(buf + col * kPitch32 + (tid & 15) * 32), hi = load_shared16(buf + col * kPitch32 + (tid & 15) * 32 + 16);
+                        float v[8] = {__uint_as_float(lo.x), __uint_as_float(lo.y), __uint_as_float(lo.z), __uint_as_float(lo.w),
+                                      __uint_as_float(hi.x), __uint_as_float(hi.y), __uint_as_float(hi.z), __uint_as_float(hi.w)};
+                        const int j = c + 16 * h + col;
+                        finish8<kProduct>(p, w.j0 + j, i8, j < columns && i8 < p.I, constants, v);
+                    }
+                }
+            };
+            if constexpr (kForm == kLong) {
+                float sum[4][32] = {};
+                for (int k = 0; k < w.blocks; k += kLongBlocks) {
+                    if (!accumulator()) break;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int c = 64 * q + 32 * group;
+                        if (c >= columns) break;
+                        uint32_t r[32];
+                        tmem_load_32x32(lanes + (turn & 1) * 256 + c, r);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) sum[q][i] += __uint_as_float(r[i]);
+                    }
+                    release();
+                }
+                if (!ok) break;
+                if (!split) constants.load(p.finish, i8, i8 < p.I);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int c = 64 * q + 32 * group;
+                    if (c >= columns) break;
+                    if (split) store_part(c, sum[q]);
+                    else finish(c, sum[q]);
+                }
+            } else if (kForm == kFull || split) {
+                if (!split) constants.load(p.finish, i8, i8 < p.I);
+                if (!accumulator()) break;
+                for (int c = 32 * group; c < columns; c += 64) {
+                    uint32_t raw[32];
+                    float r[32];
+                    tmem_load_32x32(lanes + (turn & 1) * 256 + c, raw);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) r[i] = __uint_as_float(raw[i]);
+                    if (split) store_part(c, r);
+                    else if (kForm == kFull) finish(c, r);
+                }
+                release();
+            } else {
+                // the elementwise part on the accumulators where they are: a lane has four i (16 hl + 8 o + lane / 4) and pairs of j
+                constexpr bool kElementwise = kProduct == kForward || kProduct == kForwardE4M3;
+                float bias[4] = {}, scale[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+                if (kElementwise) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int i = i_cta + 32 * quarter + 8 * q + (lane >> 2);
+                        if (p.finish.bias && i < p.I) bias[q] = __bfloat162float(p.finish.bias[i]);
+                        if (kProduct == kForwardE4M3 && i < p.I) scale[q] = __ldg(p.finish.w_scales + i);
+                    }
+                }
+                if (!accumulator()) break;
+                for (int c = 32 * group; c < columns; c += 64, ++chunk_turn) {
+                    const uint32_t buf = staging + (2 * group + (chunk_turn & 1)) * kBuffer16;
+                    float sx[8];
+                    if (kProduct == kForwardE4M3) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int j = c + 8 * (i >> 1) + 2 * (lane & 3) + (i & 1);
+                            sx[i] = j < columns ? __ldg(p.finish.x_scales + w.j0 + j) : 0.0f;
+                        }
+                    }
+#pragma unroll
+                    for (int hl = 0; hl < 2; ++hl) {
+                        uint32_t r[16];
+                        tmem_load_16x32(lanes + (static_cast<uint32_t>(16 * hl) << 16) + (turn & 1) * 256 + c, r);
+#pragma unroll
+                        for (int o = 0; o < 2; ++o) {
+                            uint32_t v[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                float e[2] = {__uint_as_float(r[4 * i + 2 * o]), __uint_as_float(r[4 * i + 2 * o + 1])};
+                                if (kElementwise) {
+#pragma unroll
+                                    for (int k = 0; k < 2; ++k) {
+                                        if (kProduct == kForwardE4M3) e[k] *= sx[2 * i + k] * scale[2 * hl + o];
+                                        e[k] = act_value(p.finish.act, e[k] + bias[2 * hl + o]);
+                                    }
+                                }
+                                v[i] = pack2(e[0], e[1]);
+                            }
+                            stmatrix_x4_trans(buf + lane * kPitch16 + (32 * quarter + 16 * hl + 8 * o) * 2, v[0], v[1], v[2], v[3]);
+                        }
+                    }
+                    named_barrier(2 + group, 128);
+                    bf16* out = static_cast<bf16*>(p.out);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int col = i * 8 + (tid >> 4);
+                        if (c + col < columns && i8 < p.I)
+                            *reinterpret_cast<uint4*>(out + static_cast<int64_t>(w.j0 + c + col) * p.I + i8) = load_shared16(buf + col * kPitch16 + (tid & 15) * 16);
+                    }
+                }
+                release();
+            }
         }
         if (!ok && lane == 0) flag_error(p.err_word, COBALT_DEVERR_WAIT_TIMEOUT);
         __syncwarp();
@@ -402,7 +526,7 @@ linear_join_kernel(const __grid_constant__ LinearArgs p)
 }
 
 // d = dout act'(pre) in bf16 (where the products need it) and its column sums: a CTA has 128 features and a slice of the
-// tokens, sixteen at a time; the sums of its sixteen token rows are added in order and written to partial [gridDim.y][N].
+// tokens, 64 at a time; the sums of its sixteen token rows are added in order and written to partial [gridDim.y][N].
 struct GradPreArgs {
     const void* grad_out;
     const void* pre;                     // or null
@@ -416,36 +540,66 @@ struct GradPreArgs {
 __global__ void __launch_bounds__(256)
 linear_grad_pre_kernel(const GradPreArgs p)
 {
+    constexpr int kAhead = 4;            // tokens that a thread has in flight
     __shared__ float sums[16][128];
     wait_for_prior_kernel();
     launch_dependents();
     const int i8 = (blockIdx.x * 16 + (threadIdx.x & 15)) * 8, own = threadIdx.x >> 4, groups = (p.N + kPackGroup - 1) / kPackGroup;
-    const int64_t step = static_cast<int64_t>(gridDim.y) * 16;
+    const int64_t step = static_cast<int64_t>(gridDim.y) * 16 * kAhead;
     float total[8] = {};
     if (i8 < p.N) {
-        for (int64_t t = static_cast<int64_t>(blockIdx.y) * 16 + own; t < p.T; t += step) {
-            const int64_t at = t * p.N + i8;
-            float d[8];
-            load8(p.grad_out, at, p.f32, d);
-            if (p.act != COBALT_ACT_NONE) {
-                float v[8];
+        for (int64_t t0 = static_cast<int64_t>(blockIdx.y) * 16 * kAhead + own; t0 < p.T; t0 += step) {
+            uint4 d16[kAhead], d32[kAhead], v16[kAhead];
+            float scale[kAhead];
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) {
+                const int64_t t = t0 + 16 * a, at = t * p.N + i8;
+                d16[a] = d32[a] = v16[a] = make_uint4(0, 0, 0, 0);
+                scale[a] = 0.0f;
+                if (t >= p.T) continue;
+                d16[a] = ld_once16(static_cast<const uint8_t*>(p.grad_out) + at * (p.f32 ? 4 : 2));
+                if (p.f32) d32[a] = ld_once16(static_cast<const float*>(p.grad_out) + at + 4);
+                if (p.act == COBALT_ACT_NONE) continue;
                 if (p.pre_scales) {
                     const uint2 codes = __ldcs(reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(p.pre) + at));
-                    const float scale = __ldg(p.pre_scales + t * groups + blockIdx.x);
-                    float a[4], b[4];
-                    CodeI8::decode4(codes.x, a);
-                    CodeI8::decode4(codes.y, b);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) v[k] = a[k] * scale, v[4 + k] = b[k] * scale;
+                    v16[a].x = codes.x, v16[a].y = codes.y;
+                    scale[a] = __ldg(p.pre_scales + t * groups + blockIdx.x);
                 } else {
-                    load8(p.pre, at, false, v);
+                    v16[a] = ld_once16(static_cast<const bf16*>(p.pre) + at);
                 }
-#pragma unroll
-                for (int k = 0; k < 8; ++k) d[k] *= act_slope(p.act, v[k]);
             }
-            if (p.grad_pre) store8(p.grad_pre, at, false, d);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) total[k] += d[k];
+            for (int a = 0; a < kAhead; ++a) {
+                const int64_t t = t0 + 16 * a;
+                if (t >= p.T) break;
+                float d[8];
+                if (p.f32) {
+                    float x[4], y[4];
+                    Vec16<float>::unpack(d16[a], x);
+                    Vec16<float>::unpack(d32[a], y);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) d[k] = x[k], d[4 + k] = y[k];
+                } else {
+                    Vec16<bf16>::unpack(d16[a], d);
+                }
+                if (p.act != COBALT_ACT_NONE) {
+                    float v[8];
+                    if (p.pre_scales) {
+                        float x[4], y[4];
+                        CodeI8::decode4(v16[a].x, x);
+                        CodeI8::decode4(v16[a].y, y);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) v[k] = x[k] * scale[a], v[4 + k] = y[k] * scale[a];
+                    } else {
+                        Vec16<bf16>::unpack(v16[a], v);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) d[k] *= act_slope(p.act, v[k]);
+                }
+                if (p.grad_pre) store8(p.grad_pre, t * p.N + i8, false, d);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) total[k] += d[k];
+            }
         }
     }
     if (!p.partial) return;
@@ -531,11 +685,11 @@ static size_t part_bytes(int64_t I, int64_t J)
 
 static int64_t deep_blocks(int64_t k, int deep) { return (k + deep - 1) / deep; }
 
-// Slices of the tokens in the pass over the output's gradient: about four CTAs an SM.
+// Slices of the tokens in the pass over the output's gradient: about six CTAs an SM.
 static int bias_parts(int64_t T, int N)
 {
-    const int64_t groups = (N + 127) / 128, rows = (T + 15) / 16;
-    int64_t parts = (4 * 2 * kPlanPairs + groups - 1) / groups;
+    const int64_t groups = (N + 127) / 128, rows = (T + 63) / 64;
+    int64_t parts = (6 * 2 * kPlanPairs + groups - 1) / groups;
     if (parts > rows) parts = rows;
     return static_cast<int>(parts < 1 ? 1 : parts);
 }
@@ -575,7 +729,7 @@ static int launch_after(void (*kernel)(Params...), dim3 grid, dim3 block, size_t
 }
 
 // a: [I, k] or, transposed, [k, I]; b: [J, k] or [k, J].
-template <int kProduct>
+template <int kProduct, int kForm>
 static int launch_product(const void* a, const void* b, int64_t I, int64_t J, int64_t k, LinearArgs p, void* workspace, cudaStream_t s)
 {
     constexpr bool kAMn = kProduct == kGradRows || kProduct == kGradWeights, kBMn = kProduct == kGradWeights;
@@ -594,13 +748,14 @@ static int launch_product(const void* a, const void* b, int64_t I, int64_t J, in
     CUtensorMap map_a, map_b;
     COBALT_TRY(kAMn ? matrix_map(&map_a, a, k, I, 64, kDeep) : matrix_map(&map_a, a, I, k, kStepK, 128, kBytes));
     COBALT_TRY(kBMn ? matrix_map(&map_b, b, k, J, 64, kDeep) : matrix_map(&map_b, b, J, k, kStepK, plan.n / 2, kBytes));
-    COBALT_TRY(ensure_kernel_attributes(reinterpret_cast<const void*>(linear_kernel<kProduct>), kLinearSmem, false));
+    const void* kernel = reinterpret_cast<const void*>(&linear_kernel<kProduct, kForm>);
+    COBALT_TRY(ensure_kernel_attributes(kernel, kLinearSmem, false));
     int sms = 0;
     COBALT_TRY(sm_count(&sms));
     const int64_t tiles = static_cast<int64_t>(p.m_tiles) * p.j_tiles * p.splits, pairs = tiles < sms / 2 ? tiles : sms / 2;
     if (tiles >= (1ll << 31) - (1 << 16)) return COBALT_ERR_UNSUPPORTED;
-    COBALT_TRY(launch_after(linear_kernel<kProduct>, dim3(static_cast<unsigned>(2 * (pairs < 1 ? 1 : pairs))), dim3(kLinearThreads), kLinearSmem, s,
-                            map_a, map_b, p));
+    const dim3 grid(static_cast<unsigned>(2 * (pairs < 1 ? 1 : pairs)));
+    COBALT_TRY((launch_after(linear_kernel<kProduct, kForm>, grid, dim3(kLinearThreads), kLinearSmem, s, map_a, map_b, p)));
     if (p.splits == 1) return COBALT_OK;
     const int64_t threads = J * ((I + 127) / 128 * 16);
     return launch_after(linear_join_kernel<kProduct>, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, s, p);
@@ -639,7 +794,11 @@ int cobalt_linear(const void* x, const float* x_scales, const void* w, const flo
     p.finish = {static_cast<const bf16*>(bias), residual, e4m3 ? x_scales : nullptr, e4m3 ? w_scales : nullptr, act, out_type == COBALT_F32, pre,
                 pre8 ? pre_scales : nullptr};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return e4m3 ? launch_product<kForwardE4M3>(w, x, N, T, K, p, workspace, s) : launch_product<kForward>(w, x, N, T, K, p, workspace, s);
+    const int form = out_type == COBALT_F32 ? kLong : residual || pre ? kFull : kPlain;
+#define COBALT_LINEAR(FORM) \
+    (e4m3 ? launch_product<kForwardE4M3, FORM>(w, x, N, T, K, p, workspace, s) : launch_product<kForward, FORM>(w, x, N, T, K, p, workspace, s))
+    return form == kLong ? COBALT_LINEAR(kLong) : form == kFull ? COBALT_LINEAR(kFull) : COBALT_LINEAR(kPlain);
+#undef COBALT_LINEAR
 }
 
 int cobalt_linear_backward(const void* grad_out, const void* x, const void* w, const void* pre, const float* pre_scales, int32_t pre_type,
@@ -680,11 +839,11 @@ int cobalt_linear_backward(const void* grad_out, const void* x, const void* w, c
     }
     if (grad_x) {
         p.out = grad_x;
-        COBALT_TRY(launch_product<kGradRows>(w, d, K, T, N, p, workspace, s));
+        COBALT_TRY((launch_product<kGradRows, kPlain>(w, d, K, T, N, p, workspace, s)));
     }
     if (grad_w) {
         p.out = grad_w;
-        COBALT_TRY(launch_product<kGradWeights>(x, d, K, N, T, p, workspace, s));
+        COBALT_TRY((launch_product<kGradWeights, kPlain>(x, d, K, N, T, p, workspace, s)));
     }
     return COBALT_OK;
 }
