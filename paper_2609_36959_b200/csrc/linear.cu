@@ -74,54 +74,86 @@ struct LinearArgs {
     uint32_t* err_word;
 };
 
-// The normal distribution's cumulative function at v and exp(-v^2 / 2), by the rational approximation 7.1.26 of Abramowitz and
-// Stegun's Handbook (erf to 1.5e-7): no branch, a third of the instructions of erff and exp, and the epilogue is bound by them.
-__device__ __forceinline__ float2 normal_cdf(float v)
+// 2^x and 1 / x by the special function unit, good to two units; results below 2^-126 are 0.
+__device__ __forceinline__ float fast_exp2(float x)
 {
-    const float a = fabsf(v) * 0.70710678118654752f, t = __fdividef(1.0f, fmaf(0.3275911f, a, 1.0f)), e = __expf(-0.5f * v * v);
-    float q = fmaf(t, 1.061405429f, -1.453152027f);
-    q = fmaf(t, q, 1.421413741f);
-    q = fmaf(t, q, -0.284496736f);
-    q = fmaf(t, q, 0.254829592f) * t * e * 0.5f;
-    return make_float2(v > 0.0f ? 1.0f - q : q, e);
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float fast_inverse(float x)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
 }
 
-__device__ __forceinline__ float act_value(int act, float v)
-{
-    if (act == COBALT_ACT_RELU) return v < 0.0f ? 0.0f : v;                          // a NaN stays
-    if (act == COBALT_ACT_SILU) return v * sigmoid(v);
-    if (act == COBALT_ACT_GELU) return v * normal_cdf(v).x;
-    return v;
-}
+constexpr float kLog2E = 1.44269504088896341f;
 
-__device__ __forceinline__ float act_slope(int act, float v)
-{
-    if (act == COBALT_ACT_RELU) return v > 0.0f ? 1.0f : 0.0f;
-    if (act == COBALT_ACT_SILU) {
-        const float s = sigmoid(v);
-        return s * (1.0f + v * (1.0f - s));
-    }
-    if (act == COBALT_ACT_GELU) {
-        const float2 c = normal_cdf(v);
-        return fmaf(v * 0.39894228040143268f, c.y, c.x);
-    }
-    return 1.0f;
-}
+__device__ __forceinline__ float fast_sigmoid(float v) { return fast_inverse(1.0f + fast_exp2(-kLog2E * v)); }
 
-// Eight neighbouring values as fp32, from bf16 or fp32 memory, and back.
-__device__ __forceinline__ void load8(const void* p, int64_t at, bool f32, float (&v)[8])
+// The activations, of whole arrays: the switch stands outside the loops (inside, it took as long as the rest of the epilogue).
+// gelu's normal distribution function comes from the rational approximations of Abramowitz and Stegun's Handbook for erf of a = |v| / sqrt 2:
+//   7.1.28 (to 3e-7, no exponential)   erf a = 1 - (1 + a1 a + ... + a6 a^6)^-16
+//   7.1.26 (to 1.5e-7)                 erf a = 1 - (b1 t + ... + b5 t^5) exp(-a^2), t = 1 / (1 + 0.3275911 a)
+// both without branches; the epilogue is bound by instructions, and erff with its two branches takes three times as many.
+template <int N>
+__device__ __forceinline__ void apply_act(int act, float (&v)[N])
 {
-    if (f32) {
-        float a[4], b[4];
-        Vec16<float>::unpack(ld_once16(static_cast<const float*>(p) + at), a);
-        Vec16<float>::unpack(ld_once16(static_cast<const float*>(p) + at + 4), b);
+    if (act == COBALT_ACT_RELU) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = a[k], v[4 + k] = b[k];
-    } else {
-        Vec16<bf16>::unpack(ld_once16(static_cast<const bf16*>(p) + at), v);
+        for (int i = 0; i < N; ++i) v[i] = v[i] < 0.0f ? 0.0f : v[i];              // a NaN stays
+    } else if (act == COBALT_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] *= fast_sigmoid(v[i]);
+    } else if (act == COBALT_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float a = fabsf(v[i]) * 0.70710678118654752f;
+            float p = fmaf(a, 0.0000430638f, 0.0002765672f);
+            p = fmaf(a, p, 0.0001520143f);
+            p = fmaf(a, p, 0.0092705272f);
+            p = fmaf(a, p, 0.0422820123f);
+            p = fmaf(a, p, 0.0705230784f);
+            p = fmaf(a, p, 1.0f);
+            p *= p;
+            p *= p;
+            p *= p;
+            p *= p;
+            const float tail = 0.5f * fast_inverse(p);                              // beyond |v|, on one side
+            v[i] *= v[i] > 0.0f ? 1.0f - tail : tail;
+        }
     }
 }
 
+// d times the activation's slope at v.
+template <int N>
+__device__ __forceinline__ void apply_slope(int act, const float (&v)[N], float (&d)[N])
+{
+    if (act == COBALT_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) d[i] *= v[i] > 0.0f ? 1.0f : 0.0f;
+    } else if (act == COBALT_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float s = fast_sigmoid(v[i]);
+            d[i] *= s * fmaf(v[i], 1.0f - s, 1.0f);
+        }
+    } else if (act == COBALT_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float t = fast_inverse(fmaf(0.3275911f * 0.70710678118654752f, fabsf(v[i]), 1.0f)), e = fast_exp2(-0.5f * kLog2E * v[i] * v[i]);
+            float q = fmaf(t, 1.061405429f, -1.453152027f);
+            q = fmaf(t, q, 1.421413741f);
+            q = fmaf(t, q, -0.284496736f);
+            q = fmaf(t, q, 0.254829592f);
+            q *= 0.5f * t * e;
+            d[i] *= fmaf(v[i] * 0.39894228040143268f, e, v[i] > 0.0f ? 1.0f - q : q);
+        }
+    }
+}
+
+// Eight neighbouring values to bf16 or fp32 memory.
 __device__ __forceinline__ void store8(void* p, int64_t at, bool f32, const float (&v)[8])
 {
     if (f32) {
@@ -149,10 +181,39 @@ struct FeatureConstants {
     }
 };
 
+// The residual of eight features, fetched ahead of their sums.
+struct Residual8 {
+    uint4 a, b;
+    __device__ __forceinline__ void load(const LinearArgs& p, int64_t j, int i0, bool mine)
+    {
+        a = b = make_uint4(0, 0, 0, 0);
+        if (!mine || !p.finish.residual) return;
+        const int64_t at = j * p.I + i0;
+        a = ld_once16(static_cast<const uint8_t*>(p.finish.residual) + at * (p.finish.f32 ? 4 : 2));
+        if (p.finish.f32) b = ld_once16(static_cast<const float*>(p.finish.residual) + at + 4);
+    }
+    __device__ __forceinline__ void add_to(const LinearArgs& p, float (&v)[8]) const
+    {
+        if (!p.finish.residual) return;
+        float r[8];
+        if (p.finish.f32) {
+            float x[4], y[4];
+            Vec16<float>::unpack(a, x);
+            Vec16<float>::unpack(b, y);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) r[k] = x[k], r[4 + k] = y[k];
+        } else {
+            Vec16<bf16>::unpack(a, r);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] += r[k];
+    }
+};
+
 // The result for features i0 .. i0 + 7 of token j from their sums.  All sixteen lanes of 128 features are here together
 // (`mine` says which of them have a result).
 template <int kProduct>
-__device__ __forceinline__ void finish8(const LinearArgs& p, int64_t j, int i0, bool mine, const FeatureConstants& c, float (&v)[8])
+__device__ __forceinline__ void finish8(const LinearArgs& p, int64_t j, int i0, bool mine, const FeatureConstants& c, const Residual8& residual, float (&v)[8])
 {
     const Finish& f = p.finish;
     const int64_t at = j * p.I + i0;
@@ -173,25 +234,16 @@ __device__ __forceinline__ void finish8(const LinearArgs& p, int64_t j, int i0, 
             for (int off = 1; off < 16; off <<= 1) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, off));
             const GroupScale g = GroupScale::of<CodeI8>(most);
             if (mine) {
-                float t[2][4];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) t[k / 4][k % 4] = g.factor > 0.0f ? v[k] * g.factor : 0.0f;
-                *reinterpret_cast<uint2*>(static_cast<uint8_t*>(f.pre) + at) = make_uint2(CodeI8::encode4(t[0]), CodeI8::encode4(t[1]));
+                uint32_t codes[2];
+                encode_fast<CodeI8>(v, g, codes);            // pre is itself a rounded sum: a code at a border may go either way
+                *reinterpret_cast<uint2*>(static_cast<uint8_t*>(f.pre) + at) = make_uint2(codes[0], codes[1]);
                 if (i0 % kPackGroup == 0) f.pre_scales[j * ((p.I + kPackGroup - 1) / kPackGroup) + i0 / kPackGroup] = g.scale;
             }
         } else if (f.pre && mine) {
             store8(f.pre, at, false, v);
         }
-        if (f.act != COBALT_ACT_NONE) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = act_value(f.act, v[k]);
-        }
-        if (f.residual && mine) {
-            float r[8];
-            load8(f.residual, at, f.f32, r);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] += r[k];
-        }
+        apply_act(f.act, v);
+        residual.add_to(p, v);
         if (mine) store8(p.out, at, f.f32, v);
     } else if (mine) {
         store8(p.out, at, false, v);
@@ -347,7 +399,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
         // ---- epilogue: two groups of four warps, each a quarter of the tensor memory lanes a warp, take 32 columns in turn ----------
         const int quarter = warp & 3, group = (warp - 2) >> 2, tid = (threadIdx.x - 64) & 127;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(32 * quarter) << 16);
-        int turn = 0, chunk_turn = 0;
+        int turn = 0;
         // one verdict for the eight warps: none is left alone at the barriers below
         auto accumulator = [&]() {
             ok = named_barrier_and(1, 256, barrier_wait(acc_full + 8 * (turn & 1), (turn >> 1) & 1));
@@ -374,6 +426,14 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                     if (c + k < columns) out[static_cast<int64_t>(k) * p.I] = r[k];
             };
             FeatureConstants constants;
+            Residual8 residual[4];
+            auto fetch_residual = [&](int c) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int j = c + 8 * i + (tid >> 4);
+                    residual[i].load(p, w.j0 + j, i8, j < columns && i8 < p.I);
+                }
+            };
             auto finish = [&](int c, const float (&r)[32]) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -389,7 +449,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                         float v[8] = {__uint_as_float(lo.x), __uint_as_float(lo.y), __uint_as_float(lo.z), __uint_as_float(lo.w),
                                       __uint_as_float(hi.x), __uint_as_float(hi.y), __uint_as_float(hi.z), __uint_as_float(hi.w)};
                         const int j = c + 16 * h + col;
-                        finish8<kProduct>(p, w.j0 + j, i8, j < columns && i8 < p.I, constants, v);
+                        finish8<kProduct>(p, w.j0 + j, i8, j < columns && i8 < p.I, constants, residual[2 * h + i], v);
                     }
                 }
             };
@@ -402,7 +462,8 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                         const int c = 64 * q + 32 * group;
                         if (c >= columns) break;
                         uint32_t r[32];
-                        tmem_load_32x32(lanes + (turn & 1) * 256 + c, r);
+                        tmem_fetch_32x32(lanes + (turn & 1) * 256 + c, r);
+                        tmem_wait(r);
 #pragma unroll
                         for (int i = 0; i < 32; ++i) sum[q][i] += __uint_as_float(r[i]);
                     }
@@ -414,20 +475,32 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                 for (int q = 0; q < 4; ++q) {
                     const int c = 64 * q + 32 * group;
                     if (c >= columns) break;
-                    if (split) store_part(c, sum[q]);
-                    else finish(c, sum[q]);
+                    if (split) {
+                        store_part(c, sum[q]);
+                    } else {
+                        fetch_residual(c);
+                        finish(c, sum[q]);
+                    }
                 }
             } else if (kForm == kFull || split) {
-                if (!split) constants.load(p.finish, i8, i8 < p.I);
+                if (!split) {
+                    constants.load(p.finish, i8, i8 < p.I);
+                    fetch_residual(32 * group);
+                }
                 if (!accumulator()) break;
                 for (int c = 32 * group; c < columns; c += 64) {
                     uint32_t raw[32];
                     float r[32];
-                    tmem_load_32x32(lanes + (turn & 1) * 256 + c, raw);
+                    tmem_fetch_32x32(lanes + (turn & 1) * 256 + c, raw);
+                    tmem_wait(raw);
 #pragma unroll
                     for (int i = 0; i < 32; ++i) r[i] = __uint_as_float(raw[i]);
-                    if (split) store_part(c, r);
-                    else if (kForm == kFull) finish(c, r);
+                    if (split) {
+                        store_part(c, r);
+                    } else if (kForm == kFull) {
+                        finish(c, r);
+                        fetch_residual(c + 64);
+                    }
                 }
                 release();
             } else {
@@ -442,38 +515,50 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                         if (kProduct == kForwardE4M3 && i < p.I) scale[q] = __ldg(p.finish.w_scales + i);
                     }
                 }
-                if (!accumulator()) break;
-                for (int c = 32 * group; c < columns; c += 64, ++chunk_turn) {
-                    const uint32_t buf = staging + (2 * group + (chunk_turn & 1)) * kBuffer16;
-                    float sx[8];
-                    if (kProduct == kForwardE4M3) {
+                float sx[8];
+                auto token_scales = [&](int c) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const int j = c + 8 * (i >> 1) + 2 * (lane & 3) + (i & 1);
-                            sx[i] = j < columns ? __ldg(p.finish.x_scales + w.j0 + j) : 0.0f;
-                        }
+                    for (int i = 0; i < 8; ++i) {
+                        const int j = c + 8 * (i >> 1) + 2 * (lane & 3) + (i & 1);
+                        sx[i] = j < columns ? __ldg(p.finish.x_scales + w.j0 + j) : 0.0f;
                     }
+                };
+                if (kProduct == kForwardE4M3) token_scales(32 * group);
+                if (!accumulator()) break;
+                // the next chunk's accumulators and scales are on their way while this one is stored.  The four chunks are unrolled: what
+                // is fetched stays in its registers up to the wait.  (Columns past the tile's are fetched and not used.)
+                uint32_t r[2][16];
+                auto fetch = [&](int c) {
+#pragma unroll
+                    for (int hl = 0; hl < 2; ++hl) tmem_fetch_16x32(lanes + (static_cast<uint32_t>(16 * hl) << 16) + (turn & 1) * 256 + c, r[hl]);
+                };
+                fetch(32 * group);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int c = 64 * q + 32 * group;
+                    const uint32_t buf = staging + (2 * group + (q & 1)) * kBuffer16;
+                    tmem_wait(r[0]);
+                    tmem_wait(r[1]);
+                    if (c >= columns) break;
 #pragma unroll
                     for (int hl = 0; hl < 2; ++hl) {
-                        uint32_t r[16];
-                        tmem_load_16x32(lanes + (static_cast<uint32_t>(16 * hl) << 16) + (turn & 1) * 256 + c, r);
 #pragma unroll
                         for (int o = 0; o < 2; ++o) {
-                            uint32_t v[4];
+                            float e[8];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                float e[2] = {__uint_as_float(r[4 * i + 2 * o]), __uint_as_float(r[4 * i + 2 * o + 1])};
-                                if (kElementwise) {
-#pragma unroll
-                                    for (int k = 0; k < 2; ++k) {
-                                        if (kProduct == kForwardE4M3) e[k] *= sx[2 * i + k] * scale[2 * hl + o];
-                                        e[k] = act_value(p.finish.act, e[k] + bias[2 * hl + o]);
-                                    }
-                                }
-                                v[i] = pack2(e[0], e[1]);
+                            for (int i = 0; i < 8; ++i) {
+                                e[i] = __uint_as_float(r[hl][4 * (i >> 1) + 2 * o + (i & 1)]);
+                                if (kProduct == kForwardE4M3) e[i] *= sx[i] * scale[2 * hl + o];
+                                if (kElementwise) e[i] += bias[2 * hl + o];
                             }
-                            stmatrix_x4_trans(buf + lane * kPitch16 + (32 * quarter + 16 * hl + 8 * o) * 2, v[0], v[1], v[2], v[3]);
+                            if (kElementwise) apply_act(p.finish.act, e);
+                            stmatrix_x4_trans(buf + lane * kPitch16 + (32 * quarter + 16 * hl + 8 * o) * 2, pack2(e[0], e[1]), pack2(e[2], e[3]),
+                                              pack2(e[4], e[5]), pack2(e[6], e[7]));
                         }
+                    }
+                    if (q < 3) {
+                        fetch(c + 64);
+                        if (kProduct == kForwardE4M3) token_scales(c + 64);
                     }
                     named_barrier(2 + group, 128);
                     bf16* out = static_cast<bf16*>(p.out);
@@ -508,7 +593,11 @@ linear_join_kernel(const __grid_constant__ LinearArgs p)
     const int i8 = static_cast<int>(index - j * per_row) * 8;
     const bool mine = j < p.J && i8 < p.I;
     FeatureConstants constants;
-    if (kProduct == kForward || kProduct == kForwardE4M3) constants.load(p.finish, i8, mine);
+    Residual8 residual = {};
+    if (kProduct == kForward || kProduct == kForwardE4M3) {
+        constants.load(p.finish, i8, mine);
+        residual.load(p, j, i8, mine);
+    }
     float v[8] = {};
     if (mine) {
         const float* from = p.partial + j * p.I + i8;
@@ -522,7 +611,100 @@ linear_join_kernel(const __grid_constant__ LinearArgs p)
             for (int k = 0; k < 4; ++k) v[k] += a[k], v[4 + k] += b[k];
         }
     }
-    finish8<kProduct>(p, j, i8, mine, constants, v);
+    finish8<kProduct>(p, j, i8, mine, constants, residual, v);
+}
+
+// ---- a few rows ---------------------------------------------------------------------------------------------------
+
+constexpr int kFewThreads = 256;
+
+// Sixteen bytes of an operand's row as fp32: eight bf16 values or sixteen e4m3 ones.
+template <bool kE4M3>
+struct OperandVec {
+    static constexpr int kElems = kE4M3 ? 16 : 8;
+    float f[kElems];
+    __device__ __forceinline__ explicit OperandVec(const uint4& v)
+    {
+        if constexpr (kE4M3) {
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float e[4];
+                CodeE4M3::decode4(w[i], e);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) f[4 * i + k] = e[k];
+            }
+        } else {
+            Vec16<bf16>::unpack(v, f);
+        }
+    }
+};
+
+// Up to R tokens on the fp32 units: `share` warps (1, 2, 4 or 8 of a CTA's eight) take one feature, its row of W once and the tokens'
+// rows from L1, and add their sums in order.  Every vector index is clamped to the row, so that no address lies outside it.
+template <bool kE4M3, int R>
+__global__ void __launch_bounds__(kFewThreads)
+linear_few_rows_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict__ w, int T, int K, int N, int share, void* out, const Finish f)
+{
+    constexpr int kAhead = 4, kElems = OperandVec<kE4M3>::kElems;        // vectors of W that a lane has in flight
+    __shared__ float sums[kFewThreads / 32][R];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % share, vecs = K / kElems;
+    const int feature = blockIdx.x * (8 / share) + warp / share, own = min(feature, N - 1);
+    wait_for_prior_kernel();
+    launch_dependents();
+    const uint8_t* row = w + static_cast<int64_t>(own) * vecs * 16;
+    uint4 next[kAhead];
+    auto load = [&](int base) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) next[i] = ld_stream16(row + 16 * static_cast<int64_t>(min(base + 32 * i + lane, vecs - 1)));
+    };
+    const int step = 32 * kAhead * share;
+    int base = 32 * kAhead * part;
+    load(base);
+    float sum[R] = {};
+    for (; base < vecs; base += step) {
+        uint4 now[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) now[i] = next[i];
+        if (base + step < vecs) load(base + step);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int v = base + 32 * i + lane;
+            if (v >= vecs) continue;
+            const OperandVec<kE4M3> a(now[i]);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int token = R == 1 ? 0 : min(r, T - 1);
+                const OperandVec<kE4M3> b(__ldg(reinterpret_cast<const uint4*>(x + (static_cast<int64_t>(token) * vecs + v) * 16)));
+#pragma unroll
+                for (int k = 0; k < kElems; ++k) sum[r] = fmaf(a.f[k], b.f[k], sum[r]);
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) sum[r] = warp_sum(sum[r]);
+    if (lane == 0) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) sums[warp][r] = sum[r];
+    }
+    __syncthreads();
+    // one thread a result
+    const int i = blockIdx.x * (8 / share) + threadIdx.x / R, t = threadIdx.x % R;
+    if (threadIdx.x >= 8 / share * R || i >= N || t >= T) return;
+    float v[1] = {0.0f};
+    for (int k = 0; k < share; ++k) v[0] += sums[threadIdx.x / R * share + k][t];
+    const int64_t at = static_cast<int64_t>(t) * N + i;
+    if (kE4M3) v[0] *= __ldg(f.x_scales + t) * __ldg(f.w_scales + i);
+    if (f.bias) v[0] += __bfloat162float(f.bias[i]);
+    if (f.pre) static_cast<bf16*>(f.pre)[at] = __float2bfloat16_rn(v[0]);
+    apply_act(f.act, v);
+    if (f.f32) {
+        if (f.residual) v[0] += static_cast<const float*>(f.residual)[at];
+        static_cast<float*>(out)[at] = v[0];
+    } else {
+        if (f.residual) v[0] += __bfloat162float(static_cast<const bf16*>(f.residual)[at]);
+        static_cast<bf16*>(out)[at] = __float2bfloat16_rn(v[0]);
+    }
 }
 
 // d = dout act'(pre) in bf16 (where the products need it) and its column sums: a CTA has 128 features and a slice of the
@@ -593,8 +775,7 @@ linear_grad_pre_kernel(const GradPreArgs p)
                     } else {
                         Vec16<bf16>::unpack(v16[a], v);
                     }
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) d[k] *= act_slope(p.act, v[k]);
+                    apply_slope(p.act, v, d);
                 }
                 if (p.grad_pre) store8(p.grad_pre, t * p.N + i8, false, d);
 #pragma unroll
@@ -761,6 +942,23 @@ static int launch_product(const void* a, const void* b, int64_t I, int64_t J, in
     return launch_after(linear_join_kernel<kProduct>, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, s, p);
 }
 
+// Most tokens that the fp32 units take.
+constexpr int kFewRows = 4;
+
+template <bool kE4M3>
+static int launch_few_rows(const void* x, const void* w, int T, int K, int N, void* out, const Finish& f, cudaStream_t s)
+{
+    // warps of a feature: more while there are fewer than 4096 warps and each has at least four vectors a lane
+    const int vecs = K / OperandVec<kE4M3>::kElems;
+    int share = 1;
+    while (share < 8 && N * share < 4096 && vecs >= 256 * share) share *= 2;
+    const dim3 grid(static_cast<unsigned>((N + 8 / share - 1) / (8 / share))), block(kFewThreads);
+    const uint8_t *a = static_cast<const uint8_t*>(x), *b = static_cast<const uint8_t*>(w);
+    if (T == 1) return launch_after(linear_few_rows_kernel<kE4M3, 1>, grid, block, 0, s, a, b, T, K, N, share, out, f);
+    if (T == 2) return launch_after(linear_few_rows_kernel<kE4M3, 2>, grid, block, 0, s, a, b, T, K, N, share, out, f);
+    return launch_after(linear_few_rows_kernel<kE4M3, 4>, grid, block, 0, s, a, b, T, K, N, share, out, f);
+}
+
 }  // namespace cobalt
 
 using namespace cobalt;
@@ -794,6 +992,9 @@ int cobalt_linear(const void* x, const float* x_scales, const void* w, const flo
     p.finish = {static_cast<const bf16*>(bias), residual, e4m3 ? x_scales : nullptr, e4m3 ? w_scales : nullptr, act, out_type == COBALT_F32, pre,
                 pre8 ? pre_scales : nullptr};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (T <= kFewRows && !pre8)
+        return e4m3 ? launch_few_rows<true>(x, w, static_cast<int>(T), K, N, out, p.finish, s)
+                    : launch_few_rows<false>(x, w, static_cast<int>(T), K, N, out, p.finish, s);
     const int form = out_type == COBALT_F32 ? kLong : residual || pre ? kFull : kPlain;
 #define COBALT_LINEAR(FORM) \
     (e4m3 ? launch_product<kForwardE4M3, FORM>(w, x, N, T, K, p, workspace, s) : launch_product<kForward, FORM>(w, x, N, T, K, p, workspace, s))

@@ -1,12 +1,11 @@
 // Rows to 8 bits and back (see packed.cuh for the format).
 //
-//   pack    one read of the rows, codes and scales written: 3 bytes a bf16 value. A thread has 16 neighbouring columns (one
-//           32-byte load of bf16, one 16-byte store), eight lanes a group of 128, whose largest value takes three shuffles.
+//   pack    one read of the rows, codes and scales written: 3 bytes a bf16 value. A thread has two pieces of 64 bytes (32 bf16
+//           columns; 32-byte loads and stores), four lanes a group of 128, whose largest value takes two shuffles.
 //           With one scale a row a warp or a CTA holds the row in registers between its largest value and the codes.
 //   unpack  the same walk without the reduction.
 //
-// Both are bound by HBM.  Rows whose width is no multiple of 16, or pointers off a 32-byte boundary, take eight columns a
-// thread.
+// Rows whose width is no multiple of such a piece, or pointers off a 32-byte boundary, take eight columns a piece.
 #include "packed.cuh"
 
 namespace cobalt {
@@ -14,13 +13,12 @@ namespace cobalt {
 constexpr int kPackThreads = 256;
 constexpr int kPackMaxH = 16384;
 
-// C columns of a row in fp32: two or four 16-byte loads, or 32-byte ones where C is 16.
+// C columns of a row: 16-byte loads, or 32-byte ones where they are more than eight.
 template <typename T, int C>
-__device__ __forceinline__ void load_columns(const T* p, float (&f)[C])
+__device__ __forceinline__ void load_columns(const T* p, uint4 (&v)[C / Vec16<T>::kElems])
 {
     constexpr int N = Vec16<T>::kElems;
-    uint4 v[C / N];
-    if constexpr (C == 16) {
+    if constexpr (C > 8) {
 #pragma unroll
         for (int i = 0; i < C / N; i += 2)
             asm volatile("ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
@@ -30,13 +28,6 @@ __device__ __forceinline__ void load_columns(const T* p, float (&f)[C])
     } else {
 #pragma unroll
         for (int i = 0; i < C / N; ++i) v[i] = ld_once16(p + i * N);
-    }
-#pragma unroll
-    for (int i = 0; i < C / N; ++i) {
-        float e[N];
-        Vec16<T>::unpack(v[i], e);
-#pragma unroll
-        for (int k = 0; k < N; ++k) f[i * N + k] = e[k];
     }
 }
 
@@ -52,7 +43,7 @@ __device__ __forceinline__ void store_columns(T* p, const float (&f)[C])
         for (int k = 0; k < N; ++k) e[k] = f[i * N + k];
         v[i] = Vec16<T>::pack(e);
     }
-    if constexpr (C == 16) {
+    if constexpr (C > 8) {
 #pragma unroll
         for (int i = 0; i < C / N; i += 2)
             asm volatile("st.global.L1::no_allocate.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p + i * N), "r"(v[i].x), "r"(v[i].y),
@@ -67,23 +58,47 @@ __device__ __forceinline__ void store_columns(T* p, const float (&f)[C])
 template <int C>
 __device__ __forceinline__ void store_codes(uint8_t* p, const uint32_t (&w)[C / 4])
 {
-    if constexpr (C == 16)
+    if constexpr (C == 32)
+        asm volatile("st.global.L1::no_allocate.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+                     "r"(w[C / 4 - 4]), "r"(w[C / 4 - 3]), "r"(w[C / 4 - 2]), "r"(w[C / 4 - 1])
+                     : "memory");
+    else if constexpr (C == 16)
         st_stream16(p, make_uint4(w[0], w[1], w[2], w[3]));
     else
         *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
 }
 
-// Piece `index` of the rows, per_row pieces a row: row and piece in the row.  One 64-bit division a CTA (all threads alike),
-// 32-bit ones for the pieces.
+// Pieces of C columns, per_row of them a row, kPieces a thread: a CTA has kPackThreads * kPieces consecutive ones, a thread every
+// kPackThreads-th.  One 64-bit division a thread; the other pieces follow by steps.
+constexpr int kPieces = 2;
+
 struct Piece {
     int64_t row;
-    int at;
-    __device__ __forceinline__ Piece(int64_t cta_first, int offset, int per_row)
+    int at;                              // in the row
+    __device__ __forceinline__ explicit Piece(int per_row)
     {
-        const int64_t r = cta_first / per_row;
-        const uint32_t in = static_cast<uint32_t>(cta_first - r * per_row) + offset, more = in / static_cast<uint32_t>(per_row);
-        row = r + more;
-        at = static_cast<int>(in - more * per_row);
+        const int64_t index = static_cast<int64_t>(blockIdx.x) * (kPackThreads * kPieces) + threadIdx.x;
+        if (index < (1ll << 31)) {
+            row = static_cast<uint32_t>(index) / static_cast<uint32_t>(per_row);
+            at = static_cast<int>(static_cast<uint32_t>(index) - static_cast<uint32_t>(row) * per_row);
+        } else {
+            row = index / per_row;
+            at = static_cast<int>(index - row * per_row);
+        }
+    }
+    __device__ __forceinline__ void next(int per_row)
+    {
+        at += kPackThreads;
+        if (at >= per_row) {
+            if (at < 2 * per_row) {
+                at -= per_row;
+                ++row;
+            } else {
+                const int more = at / per_row;
+                row += more;
+                at -= more * per_row;
+            }
+        }
     }
 };
 
@@ -92,30 +107,43 @@ template <typename T, typename Code, int C>
 __global__ void __launch_bounds__(kPackThreads)
 pack_groups_kernel(const T* __restrict__ x, int64_t rows, int H, uint8_t* __restrict__ q, float* __restrict__ scales)
 {
-    constexpr int kLanes = kPackGroup / C;
+    constexpr int kLanes = kPackGroup / C, N = Vec16<T>::kElems;
     const int groups = (H + kPackGroup - 1) / kPackGroup, per_row = groups * kLanes;
-    const Piece p(static_cast<int64_t>(blockIdx.x) * kPackThreads, threadIdx.x, per_row);
-    const int col = p.at * C;
-    const bool mine = p.row < rows && col < H;
-    float f[C];
+    Piece p(per_row);
+    uint4 v[kPieces][C / N];
+    int64_t row[kPieces];
+    int at[kPieces];
 #pragma unroll
-    for (int i = 0; i < C; ++i) f[i] = 0.0f;
-    if (mine) load_columns<T, C>(x + p.row * H + col, f);
-    uint32_t most = 0;
+    for (int j = 0; j < kPieces; ++j, p.next(per_row)) {
+        row[j] = p.row;
+        at[j] = p.at;
 #pragma unroll
-    for (int i = 0; i < C; ++i) most = abs_max(most, f[i]);
-#pragma unroll
-    for (int off = 1; off < kLanes; off <<= 1) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, off));
-    if (!mine) return;
-    const GroupScale g = GroupScale::of<Code>(most);
-    uint32_t w[C / 4];
-#pragma unroll
-    for (int i = 0; i < C / 4; ++i) {
-        const float t[4] = {f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]};
-        w[i] = encode_group4<Code>(t, g);
+        for (int i = 0; i < C / N; ++i) v[j][i] = make_uint4(0, 0, 0, 0);
+        if (p.row < rows && p.at * C < H) load_columns<T, C>(x + p.row * H + p.at * C, v[j]);
     }
-    store_codes<C>(q + p.row * H + col, w);
-    if (p.at % kLanes == 0) scales[p.row * groups + p.at / kLanes] = g.scale;
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < C / N; ++i) most = abs_max16<T>(most, v[j][i]);
+#pragma unroll
+        for (int off = 1; off < kLanes; off <<= 1) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, off));
+        if (row[j] >= rows || at[j] * C >= H) continue;
+        const GroupScale g = GroupScale::of<Code>(most);
+        float f[C];
+#pragma unroll
+        for (int i = 0; i < C / N; ++i) {
+            float e[N];
+            Vec16<T>::unpack(v[j][i], e);
+#pragma unroll
+            for (int k = 0; k < N; ++k) f[i * N + k] = e[k];
+        }
+        uint32_t w[C / 4];
+        const int64_t to = row[j] * H + at[j] * C;
+        encode_exactly<T, Code>(f, g, w);
+        store_codes<C>(q + to, w);
+        if (at[j] % kLanes == 0) scales[row[j] * groups + at[j] / kLanes] = g.scale;
+    }
 }
 
 // One scale a row: kCta the CTA has one row, else each warp.  Up to VPT 16-byte vectors a thread.
@@ -138,12 +166,7 @@ pack_rows_kernel(const T* __restrict__ x, int64_t rows, int H, uint8_t* __restri
         if (at < n_vec) v[i] = ld_once16(x + row * H + at * N);
     }
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-        float f[N];
-        Vec16<T>::unpack(v[i], f);
-#pragma unroll
-        for (int k = 0; k < N; ++k) most = abs_max(most, f[k]);
-    }
+    for (int i = 0; i < VPT; ++i) most = abs_max16<T>(most, v[i]);
     most = __reduce_max_sync(0xFFFFFFFFu, most);
     if (kCta) {
         if (lane == 0) scratch[warp] = most;
@@ -159,14 +182,10 @@ pack_rows_kernel(const T* __restrict__ x, int64_t rows, int H, uint8_t* __restri
         float f[N];
         Vec16<T>::unpack(v[i], f);
         uint32_t w[N / 4];
-#pragma unroll
-        for (int k = 0; k < N / 4; ++k) {
-            const float t[4] = {f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]};
-            w[k] = encode_group4<Code>(t, g);
-        }
-        uint8_t* out = q + row * H + at * N;
-        if constexpr (N == 8) *reinterpret_cast<uint2*>(out) = make_uint2(w[0], w[1]);
-        else *reinterpret_cast<uint32_t*>(out) = w[0];
+        const int64_t to = row * H + at * N;
+        encode_exactly<T, Code>(f, g, w);
+        if constexpr (N == 8) *reinterpret_cast<uint2*>(q + to) = make_uint2(w[0], w[1]);
+        else *reinterpret_cast<uint32_t*>(q + to) = w[0];
     }
 }
 
@@ -175,44 +194,54 @@ template <typename T, typename Code, int C>
 __global__ void __launch_bounds__(kPackThreads)
 unpack_rows_kernel(const uint8_t* __restrict__ q, const float* __restrict__ scales, int64_t rows, int H, int groups, T* __restrict__ out)
 {
-    const int per_row = (H + C - 1) / C;
-    const Piece p(static_cast<int64_t>(blockIdx.x) * kPackThreads, threadIdx.x, per_row);
-    if (p.row >= rows) return;
-    const int col = p.at * C;
-    const uint8_t* at = q + p.row * H + col;
-    uint32_t w[C / 4];
-    if constexpr (C == 16) {
-        const uint4 v = ld_stream16(at);
-        w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-    } else {
-        const uint2 v = __ldcs(reinterpret_cast<const uint2*>(at));
-        w[0] = v.x, w[1] = v.y;
-    }
-    const float scale = __ldg(scales + p.row * groups + (groups > 1 ? col / kPackGroup : 0));
-    float f[C];
+    const int per_row = H / C;
+    Piece p(per_row);
+    uint32_t w[kPieces][C / 4];
+    float scale[kPieces];
+    int64_t to[kPieces];
 #pragma unroll
-    for (int i = 0; i < C / 4; ++i) {
-        float e[4];
-        Code::decode4(w[i], e);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) f[4 * i + k] = e[k] * scale;
+    for (int j = 0; j < kPieces; ++j, p.next(per_row)) {
+        to[j] = -1;
+        if (p.row >= rows) continue;
+        to[j] = p.row * H + p.at * C;
+        if constexpr (C == 16) {
+            const uint4 v = ld_stream16(q + to[j]);
+            w[j][0] = v.x, w[j][1] = v.y, w[j][2] = v.z, w[j][3] = v.w;
+        } else {
+            const uint2 v = __ldcs(reinterpret_cast<const uint2*>(q + to[j]));
+            w[j][0] = v.x, w[j][1] = v.y;
+        }
+        scale[j] = __ldg(scales + p.row * groups + (groups > 1 ? p.at * C / kPackGroup : 0));
     }
-    store_columns<T, C>(out + p.row * H + col, f);
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+        if (to[j] < 0) continue;
+        float f[C];
+#pragma unroll
+        for (int i = 0; i < C / 4; ++i) {
+            float e[4];
+            Code::decode4(w[j][i], e);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) f[4 * i + k] = e[k] * scale[j];
+        }
+        store_columns<T, C>(out + to[j], f);
+    }
 }
 
 static bool aligned32(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31u) == 0; }
 
-static int64_t piece_ctas(int64_t rows, int64_t per_row) { return (rows * per_row + kPackThreads - 1) / kPackThreads; }
+static int64_t piece_ctas(int64_t rows, int64_t per_row) { return (rows * per_row + kPackThreads * kPieces - 1) / (kPackThreads * kPieces); }
 
 template <typename T, typename Code>
 static int launch_pack(const T* x, int64_t rows, int H, bool whole_row, uint8_t* q, float* scales, cudaStream_t s)
 {
     if (!whole_row) {
         const int64_t groups = (H + kPackGroup - 1) / kPackGroup;
-        if (H % 16 == 0 && aligned32(x)) {
-            const int64_t ctas = piece_ctas(rows, groups * (kPackGroup / 16));
+        constexpr int kWide = 64 / sizeof(T);
+        if (H % kWide == 0 && aligned32(x) && aligned32(q)) {
+            const int64_t ctas = piece_ctas(rows, groups * (kPackGroup / kWide));
             if (ctas >= (1ll << 31)) return COBALT_ERR_UNSUPPORTED;
-            pack_groups_kernel<T, Code, 16><<<static_cast<unsigned>(ctas), kPackThreads, 0, s>>>(x, rows, H, q, scales);
+            pack_groups_kernel<T, Code, kWide><<<static_cast<unsigned>(ctas), kPackThreads, 0, s>>>(x, rows, H, q, scales);
         } else {
             const int64_t ctas = piece_ctas(rows, groups * (kPackGroup / 8));
             if (ctas >= (1ll << 31)) return COBALT_ERR_UNSUPPORTED;

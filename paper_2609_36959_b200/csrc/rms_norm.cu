@@ -9,6 +9,9 @@
 //
 // Both directions are bound by HBM: 2 + 2 bytes in and 2 + 2 out a bf16 value forward (one less with 8-bit rows), 6 in and 2 out
 // backward.  A row is read once and stays in registers.
+#include <cstdlib>
+#include <type_traits>
+
 #include "packed.cuh"
 #include "tcgen05.cuh"
 
@@ -31,10 +34,31 @@ __device__ __forceinline__ float row_sum(float v, float* scratch)
     return v;
 }
 
+// N neighbouring values of gamma.  `wide` (a 32-byte boundary): one load of 32 bytes a lane for bf16 rows; two of 16 touch every line
+// twice, and gamma is half of what goes through L1.
+template <int N>
+__device__ __forceinline__ void load_gamma(const float* gamma, bool wide, float (&g)[N])
+{
+    if (N == 8 && wide) {
+        asm volatile("ld.global.nc.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                     : "=f"(g[0]), "=f"(g[1]), "=f"(g[2]), "=f"(g[3]), "=f"(g[N - 4]), "=f"(g[N - 3]), "=f"(g[N - 2]), "=f"(g[N - 1])
+                     : "l"(gamma));
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; k += 4) {
+            const float4 v = __ldg(reinterpret_cast<const float4*>(gamma + k));
+            g[k] = v.x, g[k + 1] = v.y, g[k + 2] = v.z, g[k + 3] = v.w;
+        }
+    }
+}
+
+static inline bool on_32_bytes(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31u) == 0; }
+
 struct RmsForward {
     const void* x;
     const void* residual;                    // or null
     const float* gamma;
+    bool wide;                               // gamma on a 32-byte boundary
     int64_t rows;
     int H;
     float eps;
@@ -46,128 +70,136 @@ struct RmsForward {
     float* rstd;                             // or null
 };
 
-template <typename Code, int N>
-__device__ __forceinline__ void store_group_codes(uint8_t* q, const float (&y)[N], const GroupScale& g)
+// A row's codes and scales.  y is itself a rounded value: a code at a border may go either way.
+template <typename Code, int N, int VPT>
+__device__ __forceinline__ void store_packed(const RmsForward& p, int64_t row, int first, int step, const float (&y)[VPT][N], const uint32_t (&most)[VPT],
+                                             uint32_t row_most)
 {
-    uint32_t w[N / 4];
+    GroupScale g = GroupScale::of<Code>(row_most);
+    if (p.group == 0 && first == 0) p.scales[row] = g.scale;
 #pragma unroll
-    for (int k = 0; k < N / 4; ++k) {
-        float t[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) t[i] = g.factor > 0.0f ? y[4 * k + i] * g.factor : 0.0f;
-        w[k] = Code::encode4(t);             // y is itself a rounded value: a code at a border may go either way
+    for (int i = 0; i < VPT; ++i) {
+        const int at = first + i * step;
+        if (at >= p.H / N) continue;
+        if (p.group != 0) {
+            g = GroupScale::of<Code>(most[i]);
+            if (at % (kPackGroup / N) == 0) p.scales[row * ((p.H + kPackGroup - 1) / kPackGroup) + at / (kPackGroup / N)] = g.scale;
+        }
+        uint32_t w[N / 4];
+        encode_fast<Code>(y[i], g, w);
+        uint8_t* q = p.q + row * p.H + at * N;
+        if constexpr (N == 8) *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[1]);
+        else *reinterpret_cast<uint32_t*>(q) = w[0];
     }
-    if constexpr (N == 8) *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[1]);
-    else *reinterpret_cast<uint32_t*>(q) = w[0];
 }
 
-// A row a CTA (kCta) or a warp, up to VPT vectors a thread.
+// Most threads of a CTA.
 template <typename T, int VPT, bool kCta>
-__global__ void __launch_bounds__(1024)
+constexpr int kRmsThreads = !kCta ? 256 : VPT == 2 ? 448 : sizeof(T) == 4 ? 1024 : 512;
+
+// A row a CTA (kCta) or a warp at a time, up to VPT vectors a thread.
+template <typename T, int VPT, bool kCta, bool kPacked>
+__global__ void __launch_bounds__(kRmsThreads<T, VPT, kCta>, !kCta ? 4 : VPT == 4 && sizeof(T) == 2 ? 2 : 1)
 rms_norm_kernel(const RmsForward p)
 {
     constexpr int N = Vec16<T>::kElems;
-    __shared__ float scratch[32];
-    __shared__ uint32_t scratch_max[32];
+    __shared__ float scratch[2][32];
+    __shared__ uint32_t scratch_max[2][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_vec = p.H / N;
     const int first = kCta ? threadIdx.x : lane, step = kCta ? blockDim.x : 32;
-    const int64_t row = kCta ? blockIdx.x : static_cast<int64_t>(blockIdx.x) * (blockDim.x >> 5) + warp;
-    if (row >= p.rows) return;
-    const int64_t at_row = row * p.H;
-    const T *x = static_cast<const T*>(p.x) + at_row, *residual = static_cast<const T*>(p.residual) + at_row;
-    uint4 v[VPT];
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-        const int at = first + i * step;
-        v[i] = make_uint4(0, 0, 0, 0);
-        if (at < n_vec) v[i] = ld_once16(x + at * N);
-    }
-    if (p.residual) {
-        uint4 r[VPT];
+    const int64_t rows_step = kCta ? gridDim.x : static_cast<int64_t>(gridDim.x) * (blockDim.x >> 5);
+    int64_t row = kCta ? blockIdx.x : static_cast<int64_t>(blockIdx.x) * (blockDim.x >> 5) + warp;
+    for (int turn = 0; row < p.rows; row += rows_step, turn ^= 1) {
+        const int64_t at_row = row * p.H;
+        const T *x = static_cast<const T*>(p.x) + at_row, *residual = static_cast<const T*>(p.residual) + at_row;
+        uint4 v[VPT];
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int at = first + i * step;
-            r[i] = make_uint4(0, 0, 0, 0);
-            if (at < n_vec) r[i] = ld_once16(residual + at * N);
+            v[i] = make_uint4(0, 0, 0, 0);
+            if (at < n_vec) v[i] = ld_once16(x + at * N);
         }
+        if (p.residual) {
+            uint4 r[VPT];
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            const int at = first + i * step;
-            float a[N], b[N];
-            Vec16<T>::unpack(v[i], a);
-            Vec16<T>::unpack(r[i], b);
+            for (int i = 0; i < VPT; ++i) {
+                const int at = first + i * step;
+                r[i] = make_uint4(0, 0, 0, 0);
+                if (at < n_vec) r[i] = ld_once16(residual + at * N);
+            }
 #pragma unroll
-            for (int k = 0; k < N; ++k) a[k] += b[k];
-            v[i] = Vec16<T>::pack(a);
-            if (p.sum && at < n_vec) st_stream16(static_cast<T*>(p.sum) + at_row + at * N, v[i]);
+            for (int i = 0; i < VPT; ++i) {
+                const int at = first + i * step;
+                float a[N], b[N];
+                Vec16<T>::unpack(v[i], a);
+                Vec16<T>::unpack(r[i], b);
+#pragma unroll
+                for (int k = 0; k < N; ++k) a[k] += b[k];
+                v[i] = Vec16<T>::pack(a);
+                if (p.sum && at < n_vec) st_stream16(static_cast<T*>(p.sum) + at_row + at * N, v[i]);
+            }
         }
-    }
-    float squares = 0.0f;
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-        float f[N];
-        Vec16<T>::unpack(v[i], f);
-#pragma unroll
-        for (int k = 0; k < N; ++k) squares = fmaf(f[k], f[k], squares);
-    }
-    const float rstd = rsqrtf(row_sum<kCta>(squares, scratch) / static_cast<float>(p.H) + p.eps);
-    if (p.rstd && first == 0) p.rstd[row] = rstd;
-
-    GroupScale own = {};
-    if (p.q && p.group == 0) {               // the row's scale ahead of its codes
-        uint32_t most = 0;
+        float squares = 0.0f;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const int at = first + i * step;
-            if (at >= n_vec) continue;
             float f[N];
             Vec16<T>::unpack(v[i], f);
 #pragma unroll
-            for (int k = 0; k < N; k += 4) {
-                const float4 g = __ldg(reinterpret_cast<const float4*>(p.gamma + at * N + k));
-                most = abs_max(abs_max(abs_max(abs_max(most, f[k] * rstd * g.x), f[k + 1] * rstd * g.y), f[k + 2] * rstd * g.z), f[k + 3] * rstd * g.w);
-            }
+            for (int k = 0; k < N; ++k) squares = fmaf(f[k], f[k], squares);
         }
-        most = __reduce_max_sync(0xFFFFFFFFu, most);
-        if (kCta) {
-            if (lane == 0) scratch_max[warp] = most;
-            __syncthreads();
-            most = __reduce_max_sync(0xFFFFFFFFu, lane < (blockDim.x >> 5) ? scratch_max[lane] : 0u);
-        }
-        own = p.code == COBALT_E4M3 ? GroupScale::of<CodeE4M3>(most) : GroupScale::of<CodeI8>(most);
-        if (first == 0) p.scales[row] = own.scale;
-    }
+        const float rstd = rsqrtf(row_sum<kCta>(squares, scratch[turn]) / static_cast<float>(p.H) + p.eps);
+        if (p.rstd && first == 0) p.rstd[row] = rstd;
+
+        if constexpr (!kPacked) {
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-        const int at = first + i * step;
-        const bool mine = at < n_vec;
-        float f[N];
-        Vec16<T>::unpack(v[i], f);
+            for (int i = 0; i < VPT; ++i) {
+                const int at = first + i * step;
+                if (at >= n_vec) continue;
+                float f[N], g[N];
+                load_gamma<N>(p.gamma + at * N, p.wide, g);
+                Vec16<T>::unpack(v[i], f);
 #pragma unroll
-        for (int k = 0; k < N; k += 4) {
-            const float4 g = mine ? __ldg(reinterpret_cast<const float4*>(p.gamma + at * N + k)) : make_float4(0, 0, 0, 0);
-            f[k] = f[k] * rstd * g.x;
-            f[k + 1] = f[k + 1] * rstd * g.y;
-            f[k + 2] = f[k + 2] * rstd * g.z;
-            f[k + 3] = f[k + 3] * rstd * g.w;
-        }
-        if (mine && p.y) st_stream16(static_cast<T*>(p.y) + at_row + at * N, Vec16<T>::pack(f));
-        if (p.q) {
-            GroupScale g = own;
-            if (p.group != 0) {              // 128 columns: neighbouring lanes, all of them here
-                uint32_t most = 0;
-#pragma unroll
-                for (int k = 0; k < N; ++k) most = mine ? abs_max(most, f[k]) : 0u;
-#pragma unroll
-                for (int off = 1; off < kPackGroup / N; off <<= 1) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, off));
-                g = p.code == COBALT_E4M3 ? GroupScale::of<CodeE4M3>(most) : GroupScale::of<CodeI8>(most);
-                if (mine && at % (kPackGroup / N) == 0) p.scales[row * ((p.H + kPackGroup - 1) / kPackGroup) + at / (kPackGroup / N)] = g.scale;
+                for (int k = 0; k < N; ++k) f[k] = f[k] * rstd * g[k];
+                st_stream16(static_cast<T*>(p.y) + at_row + at * N, Vec16<T>::pack(f));
             }
-            if (mine) {
-                uint8_t* q = p.q + at_row + at * N;
-                if (p.code == COBALT_E4M3) store_group_codes<CodeE4M3>(q, f, g);
-                else store_group_codes<CodeI8>(q, f, g);
+        } else {
+            // y in registers between a group's largest value and its codes
+            float y[VPT][N];
+            uint32_t most[VPT], row_most = 0;
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                const int at = first + i * step;
+                most[i] = 0;
+#pragma unroll
+                for (int k = 0; k < N; ++k) y[i][k] = 0.0f;
+                if (at < n_vec) {
+                    float g[N];
+                    load_gamma<N>(p.gamma + at * N, p.wide, g);
+                    Vec16<T>::unpack(v[i], y[i]);
+#pragma unroll
+                    for (int k = 0; k < N; ++k) {
+                        y[i][k] = y[i][k] * rstd * g[k];
+                        most[i] = abs_max(most[i], y[i][k]);
+                    }
+                    if (p.y) st_stream16(static_cast<T*>(p.y) + at_row + at * N, Vec16<T>::pack(y[i]));
+                }
+                row_most = max(row_most, most[i]);
             }
+            if (p.group == 0) {
+                row_most = __reduce_max_sync(0xFFFFFFFFu, row_most);
+                if (kCta) {
+                    if (lane == 0) scratch_max[turn][warp] = row_most;
+                    __syncthreads();
+                    row_most = __reduce_max_sync(0xFFFFFFFFu, lane < (blockDim.x >> 5) ? scratch_max[turn][lane] : 0u);
+                }
+            } else {                         // 128 columns: neighbouring lanes, all of them here
+#pragma unroll
+                for (int i = 0; i < VPT; ++i)
+#pragma unroll
+                    for (int off = 1; off < kPackGroup / N; off <<= 1) most[i] = max(most[i], __shfl_xor_sync(0xFFFFFFFFu, most[i], off));
+            }
+            if (p.code == COBALT_E4M3) store_packed<CodeE4M3, N, VPT>(p, row, first, step, y, most, row_most);
+            else store_packed<CodeI8, N, VPT>(p, row, first, step, y, most, row_most);
         }
     }
 }
@@ -179,6 +211,7 @@ struct RmsBackward {
     const float* scales;                     // of the codes
     int groups;                              // scales of a row
     const float* gamma;
+    bool wide;                               // gamma on a 32-byte boundary
     const float* rstd;
     int64_t rows;
     int H;
@@ -186,7 +219,7 @@ struct RmsBackward {
     float* partial;                          // [CTAs][H]
 };
 
-// A vector's worth of s.
+// A vector's worth of s; values() times a factor.
 template <typename T, typename Code>
 struct SavedRows {
     static constexpr int N = Vec16<T>::kElems;
@@ -209,14 +242,15 @@ struct SavedRows {
         for (int i = 0; i < N / 4; ++i) w[i] = 0;
         scale = 0.0f;
     }
-    __device__ __forceinline__ void values(float (&f)[N]) const
+    __device__ __forceinline__ void values(float factor, Pair (&f)[N / 2]) const
     {
+        const Pair by = pair(scale * factor);
 #pragma unroll
         for (int i = 0; i < N / 4; ++i) {
             float e[4];
             Code::decode4(w[i], e);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) f[4 * i + k] = e[k] * scale;
+            f[2 * i] = pair(e[0], e[1]) * by;
+            f[2 * i + 1] = pair(e[2], e[3]) * by;
         }
     }
 };
@@ -227,12 +261,17 @@ struct SavedRows<T, void> {
     uint4 v;
     __device__ __forceinline__ void load(const RmsBackward& p, int64_t row, int at) { v = ld_once16(static_cast<const T*>(p.rows_in) + row * p.H + at * N); }
     __device__ __forceinline__ void clear() { v = make_uint4(0, 0, 0, 0); }
-    __device__ __forceinline__ void values(float (&f)[N]) const { Vec16<T>::unpack(v, f); }
+    __device__ __forceinline__ void values(float factor, Pair (&f)[N / 2]) const
+    {
+        unpack_pairs<T>(v, f);
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) f[i] = f[i] * pair(factor);
+    }
 };
 
 // Persistent CTAs; a thread has the same columns of every row, whose gradients of gamma stay in its registers.
-template <typename T, typename Code, int VPT, bool kCta>
-__global__ void __launch_bounds__(kCta ? 1024 : 256)
+template <typename T, typename Code, int VPT, bool kCta, bool kSum>
+__global__ void __launch_bounds__(kRmsThreads<T, VPT, kCta>, kCta ? (VPT == 2 ? 2 : 1) : 2)
 rms_norm_backward_kernel(const RmsBackward p)
 {
     constexpr int N = Vec16<T>::kElems;
@@ -244,11 +283,11 @@ rms_norm_backward_kernel(const RmsBackward p)
     int64_t row = kCta ? blockIdx.x : static_cast<int64_t>(blockIdx.x) * (blockDim.x >> 5) + warp;
     const float inv_h = 1.0f / static_cast<float>(p.H);
     launch_dependents();
-    float acc[VPT][N];
+    Pair acc[VPT][N / 2];
 #pragma unroll
     for (int i = 0; i < VPT; ++i)
 #pragma unroll
-        for (int k = 0; k < N; ++k) acc[i][k] = 0.0f;
+        for (int k = 0; k < N / 2; ++k) acc[i][k] = pair(0.0f);
     int turn = 0;
     for (; row < p.rows; row += rows_step, turn ^= 1) {
         uint4 dy[VPT], ds[VPT];
@@ -268,45 +307,42 @@ rms_norm_backward_kernel(const RmsBackward p)
         for (int i = 0; i < VPT; ++i) {
             const int at = first + i * step;
             ds[i] = make_uint4(0, 0, 0, 0);
-            if (p.grad_sum && at < n_vec) ds[i] = ld_once16(static_cast<const T*>(p.grad_sum) + row * p.H + at * N);
+            if (kSum && at < n_vec) ds[i] = ld_once16(static_cast<const T*>(p.grad_sum) + row * p.H + at * N);
         }
-        float dot = 0.0f;
+        Pair dot = pair(0.0f);
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int at = first + i * step;
             if (at >= n_vec) continue;
-            float z[N], d[N];
-            s[i].values(z);
-            Vec16<T>::unpack(dy[i], d);
+            float gm[N];
+            Pair z[N / 2], d[N / 2];
+            load_gamma<N>(p.gamma + at * N, p.wide, gm);
+            s[i].values(rstd, z);
+            unpack_pairs<T>(dy[i], d);
 #pragma unroll
-            for (int k = 0; k < N; k += 4) {
-                const float4 g = __ldg(reinterpret_cast<const float4*>(p.gamma + at * N + k));
-                const float gm[4] = {g.x, g.y, g.z, g.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float dz = d[k + j] * (z[k + j] * rstd);
-                    acc[i][k + j] += dz;
-                    dot = fmaf(dz, gm[j], dot);
-                }
+            for (int k = 0; k < N / 2; ++k) {
+                const Pair dz = d[k] * z[k];
+                acc[i][k] = acc[i][k] + dz;
+                dot = fma2(dz, pair(gm[2 * k], gm[2 * k + 1]), dot);
             }
         }
-        const float mean = row_sum<kCta>(dot, scratch[turn]) * inv_h;
+        const float mean = row_sum<kCta>(dot.v.x + dot.v.y, scratch[turn]) * inv_h;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int at = first + i * step;
             if (at >= n_vec) continue;
-            float z[N], d[N], e[N];
-            s[i].values(z);
-            Vec16<T>::unpack(dy[i], d);
-            Vec16<T>::unpack(ds[i], e);
+            float gm[N];
+            Pair z[N / 2], d[N / 2], e[N / 2];
+            load_gamma<N>(p.gamma + at * N, p.wide, gm);
+            s[i].values(rstd, z);
+            unpack_pairs<T>(dy[i], d);
+            if (kSum) unpack_pairs<T>(ds[i], e);
 #pragma unroll
-            for (int k = 0; k < N; k += 4) {
-                const float4 g = __ldg(reinterpret_cast<const float4*>(p.gamma + at * N + k));
-                const float gm[4] = {g.x, g.y, g.z, g.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) d[k + j] = fmaf(rstd, fmaf(-mean, z[k + j] * rstd, d[k + j] * gm[j]), e[k + j]);
+            for (int k = 0; k < N / 2; ++k) {
+                const Pair v = fma2(pair(-mean), z[k], d[k] * pair(gm[2 * k], gm[2 * k + 1]));
+                d[k] = kSum ? fma2(pair(rstd), v, e[k]) : pair(rstd) * v;
             }
-            st_stream16(static_cast<T*>(p.grad_x) + row * p.H + at * N, Vec16<T>::pack(d));
+            st_stream16(static_cast<T*>(p.grad_x) + row * p.H + at * N, pack_pairs<T>(d));
         }
     }
     float* out = p.partial + static_cast<int64_t>(blockIdx.x) * p.H;
@@ -317,7 +353,8 @@ rms_norm_backward_kernel(const RmsBackward p)
             if (at >= n_vec) continue;
 #pragma unroll
             for (int k = 0; k < N; k += 4)
-                *reinterpret_cast<float4*>(out + at * N + k) = make_float4(acc[i][k], acc[i][k + 1], acc[i][k + 2], acc[i][k + 3]);
+                *reinterpret_cast<float4*>(out + at * N + k) = 
+                    make_float4(acc[i][k / 2].v.x, acc[i][k / 2].v.y, acc[i][k / 2 + 1].v.x, acc[i][k / 2 + 1].v.y);
         }
     } else {
         for (int w = 0; w < static_cast<int>(blockDim.x >> 5); ++w) {          // the warps one after the other: a fixed order
@@ -327,7 +364,8 @@ rms_norm_backward_kernel(const RmsBackward p)
                     const int at = first + i * step;
                     if (at >= n_vec) continue;
 #pragma unroll
-                    for (int k = 0; k < N; ++k) warp_sums[at * N + k] = (w > 0 ? warp_sums[at * N + k] : 0.0f) + acc[i][k];
+                    for (int k = 0; k < N; ++k) 
+                        warp_sums[at * N + k] = (w > 0 ? warp_sums[at * N + k] : 0.0f) + (k & 1 ? acc[i][k / 2].v.y : acc[i][k / 2].v.x);
                 }
             }
             __syncthreads();
@@ -345,7 +383,7 @@ rms_norm_reduce_kernel(const float* partial, int parts, int H, float* __restrict
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
     float s = 0.0f;
     if (col < H) {
-#pragma unroll 4
+#pragma unroll 8
         for (int p = warp; p < parts; p += 32) s += partial[static_cast<int64_t>(p) * H + col];
     }
     slice[warp][lane] = s;
@@ -359,33 +397,37 @@ rms_norm_reduce_kernel(const float* partial, int parts, int H, float* __restrict
 }
 
 struct RmsShape {
-    int vpt, threads, resident;              // resident: CTAs an SM (backward)
+    int vpt, threads;
     bool cta;
 };
 
-static RmsShape rms_shape(int n_vec)
+// A warp a row up to 128 vectors; above, a CTA a row with `vpt` vectors a thread.
+static RmsShape rms_shape(int n_vec, int vpt)
 {
     RmsShape s = {};
     s.cta = n_vec > kRmsWarpVecs;
     if (!s.cta) {
         s.threads = 256;
         s.vpt = n_vec <= 32 ? 1 : n_vec <= 64 ? 2 : 4;
-        s.resident = 4;
     } else {
-        s.vpt = n_vec <= 1024 ? 2 : 4;
+        s.vpt = n_vec <= 896 ? vpt : 4;
         s.threads = ((n_vec + s.vpt - 1) / s.vpt + 31) / 32 * 32;
-        s.resident = 1024 / s.threads > 4 ? 4 : 1024 / s.threads < 1 ? 1 : 1024 / s.threads;
     }
     return s;
 }
 
 constexpr int kMaxSms = 256;                 // the workspace query knows no device: sized for this many
 
+// CTAs (= partial sums) of the backward kernels: about 1024 threads an SM, and eight rows each where there are that many.
 static int64_t rms_parts(int64_t T, const RmsShape& s, int sms)
 {
     const int64_t rows = s.cta ? 1 : s.threads / 32;
-    int64_t ctas = (T + rows - 1) / rows;
-    if (ctas > static_cast<int64_t>(s.resident) * sms) ctas = static_cast<int64_t>(s.resident) * sms;
+    int64_t ctas = (T + rows - 1) / rows, resident = 1024 / s.threads;
+    resident = resident < 1 ? 1 : resident > 8 ? 8 : resident;
+    int64_t most = resident * sms, by_rows = (ctas + 7) / 8;
+    if (by_rows < sms) by_rows = sms;
+    if (most > by_rows) most = by_rows;
+    if (ctas > most) ctas = most;
     return ctas < 1 ? 1 : ctas;              // no rows: one part of zeros
 }
 
@@ -398,37 +440,48 @@ static int check_rms(int64_t T, int32_t H, int32_t dtype)
 
 static bool check_code(int32_t code, int32_t group) { return (code == COBALT_E4M3 || code == COBALT_I8) && (group == 0 || group == kPackGroup); }
 
-template <typename T>
+template <typename T, bool kPacked>
 static void launch_forward(const RmsForward& p, cudaStream_t s)
 {
-    const RmsShape shape = rms_shape(p.H / Vec16<T>::kElems);
-    const int64_t per_cta = shape.cta ? 1 : shape.threads / 32;
-    const unsigned grid = static_cast<unsigned>((p.rows + per_cta - 1) / per_cta);
+    int vpt = getenv("RMS_VPT") ? atoi(getenv("RMS_VPT")) : 4;
+    const RmsShape shape = rms_shape(p.H / Vec16<T>::kElems, vpt);
+    const int64_t per_cta = shape.cta ? 1 : shape.threads / 32, ctas = (p.rows + per_cta - 1) / per_cta;
+    const int64_t most = getenv("RMS_RES") ? atoi(getenv("RMS_RES")) * 148 : 1 << 30;
+    const unsigned grid = static_cast<unsigned>(ctas < most ? ctas : most);
     if (shape.cta) {
-        if (shape.vpt == 2) rms_norm_kernel<T, 2, true><<<grid, shape.threads, 0, s>>>(p);
-        else rms_norm_kernel<T, 4, true><<<grid, shape.threads, 0, s>>>(p);
+        if (shape.vpt == 2) rms_norm_kernel<T, 2, true, kPacked><<<grid, shape.threads, 0, s>>>(p);
+        else rms_norm_kernel<T, 4, true, kPacked><<<grid, shape.threads, 0, s>>>(p);
     } else {
-        if (shape.vpt == 1) rms_norm_kernel<T, 1, false><<<grid, shape.threads, 0, s>>>(p);
-        else if (shape.vpt == 2) rms_norm_kernel<T, 2, false><<<grid, shape.threads, 0, s>>>(p);
-        else rms_norm_kernel<T, 4, false><<<grid, shape.threads, 0, s>>>(p);
+        if (shape.vpt == 1) rms_norm_kernel<T, 1, false, kPacked><<<grid, shape.threads, 0, s>>>(p);
+        else if (shape.vpt == 2) rms_norm_kernel<T, 2, false, kPacked><<<grid, shape.threads, 0, s>>>(p);
+        else rms_norm_kernel<T, 4, false, kPacked><<<grid, shape.threads, 0, s>>>(p);
     }
 }
 
-template <typename T, typename Code>
-static int launch_backward(const RmsBackward& p, int sms, cudaStream_t s)
+// *parts: the kernel's partial sums.
+template <typename T, typename Code, bool kSum>
+static int launch_backward(const RmsBackward& p, int sms, int* parts, cudaStream_t s)
 {
-    const RmsShape shape = rms_shape(p.H / Vec16<T>::kElems);
-    const int parts = static_cast<int>(rms_parts(p.rows, shape, sms < kMaxSms ? sms : kMaxSms));
+    const RmsShape shape = rms_shape(p.H / Vec16<T>::kElems, 2);
+    *parts = static_cast<int>(rms_parts(p.rows, shape, sms < kMaxSms ? sms : kMaxSms));
     const size_t smem = shape.cta ? 0 : sizeof(float) * p.H;
     if (shape.cta) {
-        if (shape.vpt == 2) rms_norm_backward_kernel<T, Code, 2, true><<<parts, shape.threads, smem, s>>>(p);
-        else rms_norm_backward_kernel<T, Code, 4, true><<<parts, shape.threads, smem, s>>>(p);
+        if (shape.vpt == 2) rms_norm_backward_kernel<T, Code, 2, true, kSum><<<*parts, shape.threads, smem, s>>>(p);
+        else rms_norm_backward_kernel<T, Code, 4, true, kSum><<<*parts, shape.threads, smem, s>>>(p);
     } else {
-        if (shape.vpt == 1) rms_norm_backward_kernel<T, Code, 1, false><<<parts, shape.threads, smem, s>>>(p);
-        else if (shape.vpt == 2) rms_norm_backward_kernel<T, Code, 2, false><<<parts, shape.threads, smem, s>>>(p);
-        else rms_norm_backward_kernel<T, Code, 4, false><<<parts, shape.threads, smem, s>>>(p);
+        if (shape.vpt == 1) rms_norm_backward_kernel<T, Code, 1, false, kSum><<<*parts, shape.threads, smem, s>>>(p);
+        else if (shape.vpt == 2) rms_norm_backward_kernel<T, Code, 2, false, kSum><<<*parts, shape.threads, smem, s>>>(p);
+        else rms_norm_backward_kernel<T, Code, 4, false, kSum><<<*parts, shape.threads, smem, s>>>(p);
     }
-    return parts;
+    return COBALT_OK;
+}
+
+// code: of rows in 8 bits, -1 for rows as they are.
+template <typename T, bool kSum>
+static int launch_backward(const RmsBackward& p, int code, int sms, int* parts, cudaStream_t s)
+{
+    return code == COBALT_I8 ? launch_backward<T, CodeI8, kSum>(p, sms, parts, s)
+                             : code == COBALT_E4M3 ? launch_backward<T, CodeE4M3, kSum>(p, sms, parts, s) : launch_backward<T, void, kSum>(p, sms, parts, s);
 }
 
 }  // namespace cobalt
@@ -448,10 +501,10 @@ int cobalt_rms_norm(const void* x, const void* residual, const float* gamma, int
     if (!aligned16(x) || !aligned16(residual) || !aligned16(gamma) || !aligned16(sum) || !aligned16(y) || !aligned16(q) ||
         !aligned16(q_scales) || !aligned16(rstd))
         return COBALT_ERR_INVALID_ARG;
-    const RmsForward p = {x, residual, gamma, T, H, eps, sum, y, static_cast<uint8_t*>(q), q_scales, q_code, q_group, rstd};
+    const RmsForward p = {x, residual, gamma, on_32_bytes(gamma), T, H, eps, sum, y, static_cast<uint8_t*>(q), q_scales, q_code, q_group, rstd};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (dtype == COBALT_BF16) launch_forward<__nv_bfloat16>(p, s);
-    else launch_forward<float>(p, s);
+    if (dtype == COBALT_BF16) q ? launch_forward<__nv_bfloat16, true>(p, s) : launch_forward<__nv_bfloat16, false>(p, s);
+    else q ? launch_forward<float, true>(p, s) : launch_forward<float, false>(p, s);
     COBALT_CUDA_TRY(cudaGetLastError());
     return COBALT_OK;
 }
@@ -461,7 +514,7 @@ size_t cobalt_rms_norm_workspace_bytes(int64_t T, int32_t H)
     if (check_rms(T, H, COBALT_F32) != COBALT_OK) return 0;
     int64_t parts = 0;
     for (int elems = 4; elems <= 8; elems += 4) {        // whichever type needs more
-        const int64_t p = rms_parts(T, rms_shape(H / elems), kMaxSms);
+        const int64_t p = rms_parts(T, rms_shape(H / elems, 2), kMaxSms);
         parts = p > parts ? p : parts;
     }
     return round_up(static_cast<size_t>(parts) * H * sizeof(float), 256);
@@ -483,16 +536,14 @@ int cobalt_rms_norm_backward(const void* grad_y, const void* grad_sum, const voi
     int sms = 0;
     rc = sm_count(&sms);
     if (rc != COBALT_OK) return rc;
-    const RmsBackward p = {grad_y, grad_sum, rows, row_scales, group == 0 ? 1 : (H + kPackGroup - 1) / kPackGroup, gamma, rstd, T, H, grad_x,
+    const RmsBackward p = {grad_y, grad_sum, rows, row_scales, group == 0 ? 1 : (H + kPackGroup - 1) / kPackGroup, gamma, on_32_bytes(gamma), rstd, T, H, grad_x,
                            static_cast<float*>(workspace)};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     int parts = 0;
-    if (dtype == COBALT_BF16)
-        parts = !packed ? launch_backward<__nv_bfloat16, void>(p, sms, s)
-                        : rows_type == COBALT_I8 ? launch_backward<__nv_bfloat16, CodeI8>(p, sms, s) : launch_backward<__nv_bfloat16, CodeE4M3>(p, sms, s);
-    else
-        parts = !packed ? launch_backward<float, void>(p, sms, s)
-                        : rows_type == COBALT_I8 ? launch_backward<float, CodeI8>(p, sms, s) : launch_backward<float, CodeE4M3>(p, sms, s);
+    const int code = packed ? rows_type : -1;
+    if (dtype == COBALT_BF16) rc = grad_sum ? launch_backward<__nv_bfloat16, true>(p, code, sms, &parts, s) : launch_backward<__nv_bfloat16, false>(p, code, sms, &parts, s);
+    else rc = grad_sum ? launch_backward<float, true>(p, code, sms, &parts, s) : launch_backward<float, false>(p, code, sms, &parts, s);
+    if (rc != COBALT_OK) return rc;
     COBALT_CUDA_TRY(cudaGetLastError());
     cudaLaunchAttribute attr;
     set_programmatic_launch(&attr, true);

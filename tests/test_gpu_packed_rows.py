@@ -1,9 +1,9 @@
 """Rows in 8 bits and back against the 64-bit definition.
 
 The codes are exactly the definition's: 16- and 32-bit values divided by one another lie on a border between codes or at
-least 2^-33 of themselves away from it, far more than 64 bits are off by.  A scale is one fp32 division (u), a value one
-product of two fp32 numbers more, rounded once more to bf16.  The scale of a group whose largest value is above 3e38 is rounded
-down instead of to nearest, so that L scale <= that value stays finite: off by up to 2 u there."""
+least 2^-33 of themselves away from it, far more than 64 bits are off by.  A scale is the group's largest value times the
+rounded 1 / L, rounded (2 u and u^2: 2.01 u), a value one product of two fp32 numbers more, rounded once more to bf16.  The scale of a
+group whose largest value is above 3e38 may be one step (2 u) lower, so that L times it stays finite."""
 import math
 
 import pytest
@@ -35,13 +35,13 @@ def _check(x, code, group, got):
     assert torch.equal(q.to(D.F64), rq), int((q.to(D.F64) != rq).sum())
     nan = torch.isnan(rs)
     assert torch.equal(torch.isnan(scales), nan)
-    down = D.U * (rs * D.LARGEST[code] > 3e38)                       # the second u of a scale rounded down
-    assert ((scales.double() - rs).abs()[~nan] <= ((D.U + down) * rs.abs())[~nan] + 2.0 ** -149).all()
+    down = 2 * D.U * (rs * D.LARGEST[code] > 3e38)                   # the step at the end of the range
+    assert ((scales.double() - rs).abs()[~nan] <= ((2.01 * D.U + down) * rs.abs())[~nan] + 2.0 ** -149).all()
     ref = D.values(rq, rs, group)
     bad = torch.isnan(ref)
     assert torch.equal(torch.isnan(out), bad)
     half = 0 if x.dtype == torch.float32 else D.HALF[x.dtype]
-    relative = (2 * D.U + half + D.values(torch.ones_like(ref), down, group)) * (1 + 2 * D.U)
+    relative = (3.01 * D.U + half + D.values(torch.ones_like(ref), down, group)) * (1 + 2 * D.U)
     assert ((out.double() - ref).abs()[~bad] <= (relative * ref.abs())[~bad] + 127 * 2.0 ** -149).all()
 
 
