@@ -14,6 +14,8 @@
 //     under the products of the next tile (two accumulators).
 //   - Persistent pairs deal the tiles round robin.  Where a product has fewer tiles than there are pairs, k is split; the parts
 //     go to the workspace in fp32 and a second kernel adds them in order and runs the epilogue.
+//   - Where k is short (four blocks) and i long, a router's dx, a pair keeps its j's operand in shared memory for all tiles of i and only
+//     the other one streams: half of what went through L2, which bounded that product (11 TB/s).
 //   - The epilogue passes an accumulator through shared memory, 32 columns of j at a time, so that a thread has eight
 //     neighbouring i of one j: bias, scales, residual and result move in 16-byte vectors, and the 128 i that share a scale when
 //     pre is kept in 8 bits are sixteen neighbouring lanes.
@@ -36,10 +38,12 @@ constexpr int kHalfBytes = 128 * kDeepBytes;
 constexpr int kSlotBytes = 2 * kHalfBytes;
 constexpr int kBoxBytes = 64 * kDeepBytes;       // MN-major box: 64 values of M or N x 64 of k
 constexpr int kRing = 6;
-// Epilogue staging of a j's 128 values, an odd number of 16-byte units: 32 j in bf16, or 16 in fp32; two buffers for each of two
-// groups of four warps.
-constexpr int kPitch16 = 272, kPitch32 = 528;
-constexpr int kBuffer16 = 32 * kPitch16, kBuffer32 = 16 * kPitch32;
+constexpr int kStayBlocks = 4;           // blocks of k that stay: beside them the ring has eight slots of the other operand
+constexpr int kStayRing = (kRing * kSlotBytes - kStayBlocks * kHalfBytes) / kHalfBytes;
+// Epilogue staging of 128 values of i, two buffers for each of two groups of four warps: 32 j in bf16, as two boxes of 64 values with the
+// 128-byte swizzle, or 16 j in fp32, an odd number of 16-byte units each.
+constexpr int kBox16 = 32 * 128, kBuffer16 = 2 * kBox16;
+constexpr int kPitch32 = 528, kBuffer32 = 16 * kPitch32;
 constexpr int kStaging = 4 * (kBuffer16 > kBuffer32 ? kBuffer16 : kBuffer32);
 constexpr int kLinearSmem = kRing * kSlotBytes + kStaging + 256;
 constexpr int kLinearThreads = 320;
@@ -254,9 +258,17 @@ struct LinearTile {
     int i0, j0, split, first, blocks;    // first block of k, and how many
 };
 
+template <bool kStay>
 __device__ __forceinline__ LinearTile linear_tile(const LinearArgs& p, int t)
 {
     LinearTile r;
+    if (kStay) {                         // all tiles of i for one j
+        r.split = r.first = 0;
+        r.j0 = t / p.m_tiles * p.n;
+        r.i0 = t % p.m_tiles * kTileM;
+        r.blocks = p.blocks;
+        return r;
+    }
     const int each = p.m_tiles * p.j_tiles;
     r.split = t / each;
     const int in = t - r.split * each, band = in / (kBand * p.m_tiles), high = min(kBand, p.j_tiles - band * kBand), at = in - band * kBand * p.m_tiles;
@@ -267,21 +279,24 @@ __device__ __forceinline__ LinearTile linear_tile(const LinearArgs& p, int t)
     return r;
 }
 
-template <int kProduct, int kForm>
+template <int kProduct, int kForm, bool kStay>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinearThreads, 1)
-linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ LinearArgs p)
+linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
+              const __grid_constant__ LinearArgs p)
 {
     constexpr bool kAMn = kProduct == kGradRows || kProduct == kGradWeights, kBMn = kProduct == kGradWeights;
     constexpr int kStepK = kProduct == kForwardE4M3 ? kDeepBytes : kDeep;                // values of k in a block
     extern __shared__ __align__(1024) uint8_t smem[];                    // the swizzle counts from 1024-byte boundaries
     const uint32_t base = smem_u32(smem), staging = base + kRing * kSlotBytes, bars = staging + kStaging;
-    const uint32_t ready = bars, empty = bars + 8 * kRing, acc_full = bars + 16 * kRing, acc_empty = acc_full + 16, drain = acc_full + 32,
-                   tmem_slot = acc_full + 40;
+    constexpr int kSlots = kStay ? kStayRing : kRing, kStride = kStay ? kHalfBytes : kSlotBytes;
+    const uint32_t stay = base + kSlots * kStride;                       // kStay: the blocks of j's operand
+    const uint32_t ready = bars, empty = bars + 8 * kSlots, acc_full = bars + 16 * kSlots, acc_empty = acc_full + 16, drain = acc_full + 32,
+                   tmem_slot = acc_full + 40, stay_ready = acc_full + 48, stay_empty = acc_full + 56;
     const int warp = __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kRing; ++i) {
+        for (int i = 0; i < kSlots; ++i) {
             barrier_init(ready + 8 * i, 2);      // leading CTA: both CTAs' loads of the slot
             barrier_init(empty + 8 * i, 1);      // the products that read the slot are done
         }
@@ -290,6 +305,8 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
             barrier_init(acc_empty + 8 * i, 16);  // leading CTA: eight epilogue warps of each CTA
         }
         barrier_init(drain, 1);
+        barrier_init(stay_ready, 2);
+        barrier_init(stay_empty, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         prefetch_map(&map_a);
         prefetch_map(&map_b);
@@ -303,7 +320,9 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
     uint32_t tmem;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot) : "memory");
 
-    const int tiles = p.m_tiles * p.j_tiles * p.splits, first = blockIdx.x >> 1, step = gridDim.x >> 1;
+    // the tiles (kStay: all those of a j) are dealt round robin
+    const int tiles = p.m_tiles * p.j_tiles * p.splits, pairs = gridDim.x >> 1, unit = kStay ? p.m_tiles : 1, first = (blockIdx.x >> 1) * unit;
+    auto next = [&](int t) { return (t + 1) % unit != 0 ? t + 1 : t + 1 + (pairs - 1) * unit; };
     bool ok = true;                              // no wait has run out
 
     if (warp == 0) {
@@ -313,16 +332,27 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
         const int half = p.n / 2;
         Ring ring;
         int64_t issued = 0;
-        for (int t = first; t < tiles && ok; t += step) {
-            const LinearTile w = linear_tile(p, t);
+        int changes = 0;                         // kStay: how often the operand that stays was loaded
+        for (int t = first; t < tiles && ok; t = next(t)) {
+            const LinearTile w = linear_tile<kStay>(p, t);
             // boxes wholly outside their tensor are left out: what is in the slot then only reaches results that are not stored
             const int i0 = w.i0 + static_cast<int>(rank) * 128, j0 = w.j0 + static_cast<int>(rank) * half;
             const int boxes_a = i0 >= p.I ? 0 : !kAMn || i0 + 64 >= p.I ? 1 : 2;
             const int boxes_b = j0 >= p.J ? 0 : kBMn ? min((half + 63) / 64, (p.J - j0 + 63) / 64) : 1;
-            const uint32_t bytes = boxes_a * (kAMn ? kBoxBytes : kHalfBytes) + boxes_b * (kBMn ? kBoxBytes : half * kDeepBytes);
+            const uint32_t bytes_b = boxes_b * (kBMn ? kBoxBytes : half * kDeepBytes), bytes = boxes_a * (kAMn ? kBoxBytes : kHalfBytes) + (kStay ? 0 : bytes_b);
+            if (kStay && t % unit == 0) {
+                if (!(ok = barrier_wait(stay_empty, (changes & 1) ^ 1))) break;
+                if (elect_one()) {
+                    const uint32_t bar = peer_address(stay_ready, 0);
+                    barrier_expect_cluster(bar, w.blocks * bytes_b);
+                    for (int k = 0; k < w.blocks && boxes_b > 0; ++k) tma_load_2d(stay + k * kHalfBytes, &map_b, bar, policy, k * kStepK, j0);
+                }
+                __syncwarp();
+                ++changes;
+            }
             for (int k = w.first; k < w.first + w.blocks; ++k) {
                 if (!(ok = barrier_wait(empty + 8 * ring.slot, ring.phase ^ 1))) break;
-                const uint32_t bar = pair_ready + 8 * ring.slot, a = base + ring.slot * kSlotBytes, b = a + kHalfBytes;
+                const uint32_t bar = pair_ready + 8 * ring.slot, a = base + ring.slot * kStride, b = a + kHalfBytes;
                 if (elect_one()) {
                     barrier_expect_cluster(bar, bytes);
                     if (kAMn) {
@@ -331,7 +361,8 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                     } else if (boxes_a > 0) {
                         tma_load_2d(a, &map_a, bar, policy, k * kStepK, i0);
                     }
-                    if (kBMn) {
+                    if (kStay) {
+                    } else if (kBMn) {
                         if (boxes_b > 0) tma_load_2d(b, &map_b, bar, policy, j0, k * kStepK);
                         if (boxes_b > 1) tma_load_2d(b + kBoxBytes, &map_b, bar, policy, j0 + 64, k * kStepK);
                     } else if (boxes_b > 0) {
@@ -339,7 +370,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                     }
                 }
                 __syncwarp();
-                ring.next<kRing>();
+                ring.next<kSlots>();
                 ++issued;
             }
         }
@@ -349,29 +380,35 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
             // complete, for those of the other CTA that are further ahead
             if (lane == 0) flag_error(p.err_word, COBALT_DEVERR_WAIT_TIMEOUT);
             if (rank == 0)
-                for (int64_t i = issued > kRing ? issued - kRing : 0; i <= issued; ++i)
-                    (void)barrier_wait(ready + 8 * static_cast<int>(i % kRing), static_cast<uint32_t>(i / kRing) & 1);
+                for (int64_t i = issued > kSlots ? issued - kSlots : 0; i <= issued; ++i)
+                    (void)barrier_wait(ready + 8 * static_cast<int>(i % kSlots), static_cast<uint32_t>(i / kSlots) & 1);
+            if (kStay && rank == 0 && changes > 0) (void)barrier_wait(stay_ready, (changes - 1) & 1);
         }
         __syncwarp();
     } else if (warp == 1) {
         // ---- products (leading CTA) ------------------------------------------------------------------------------
         Ring ring;
         int turn = 0;                            // accumulators used so far
+        int changes = 0;
         const uint32_t idesc = kProduct == kForwardE4M3 ? instruction_descriptor_e4m3(p.n) : instruction_descriptor(p.n, kAMn, kBMn);
-        for (int t = first; t < tiles && ok && rank == 0; t += step) {
-            const LinearTile w = linear_tile(p, t);
+        for (int t = first; t < tiles && ok && rank == 0; t = next(t)) {
+            const LinearTile w = linear_tile<kStay>(p, t);
+            if (kStay && t % unit == 0) {
+                if (!(ok = barrier_wait(stay_ready, changes & 1))) break;
+                ++changes;
+            }
             for (int k = 0; k < w.blocks && ok; ++turn) {
                 const uint32_t acc = turn & 1, d = tmem + acc * 256;
                 const int first_k = k, end = kForm == kLong ? min(w.blocks, k + kLongBlocks) : w.blocks;
                 if (!(ok = barrier_wait(acc_empty + 8 * acc, ((turn >> 1) & 1) ^ 1))) break;
                 tmem_fence_after();
                 for (; k < end; ++k) {
-                    const uint32_t a = base + ring.slot * kSlotBytes;
+                    const uint32_t a = base + ring.slot * kStride;
                     if (!(ok = barrier_wait(ready + 8 * ring.slot, ring.phase))) break;
                     tmem_fence_after();
                     if (elect_one()) {
                         // K-major: 32 bytes further in the swizzled row; MN-major: two 8-row groups
-                        const uint64_t da = matrix_descriptor(a, kAMn ? kBoxBytes : 16, 1024), db = matrix_descriptor(a + kHalfBytes, kBMn ? kBoxBytes : 16, 1024);
+                        const uint64_t da = matrix_descriptor(a, kAMn ? kBoxBytes : 16, 1024), db = matrix_descriptor(kStay ? stay + k * kHalfBytes : a + kHalfBytes, kBMn ? kBoxBytes : 16, 1024);
                         constexpr uint32_t step_a = (kAMn ? 2048 : 32) >> 4, step_b = (kBMn ? 2048 : 32) >> 4;
 #pragma unroll
                         for (uint32_t i = 0; i < 4; ++i) {
@@ -381,10 +418,13 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                         mma_commit_pair(empty + 8 * ring.slot);
                     }
                     __syncwarp();
-                    ring.next<kRing>();
+                    ring.next<kSlots>();
                 }
                 if (ok) {
-                    if (elect_one()) mma_commit_pair(acc_full + 8 * acc);
+                    if (elect_one()) {
+                        mma_commit_pair(acc_full + 8 * acc);
+                        if (kStay && (t + 1) % unit == 0) mma_commit_pair(stay_empty);         // the last tile of this j
+                    }
                     __syncwarp();
                 }
             }
@@ -412,8 +452,8 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
             if (lane == 0) barrier_arrive_tmem(peer_address(acc_empty + 8 * (turn & 1), 0));
             ++turn;
         };
-        for (int t = first; t < tiles; t += step) {
-            const LinearTile w = linear_tile(p, t);
+        for (int t = first; t < tiles; t = next(t)) {
+            const LinearTile w = linear_tile<kStay>(p, t);
             const int i_cta = w.i0 + static_cast<int>(rank) * 128, i8 = i_cta + 8 * (tid & 15), columns = min(p.n, p.J - w.j0);
             const bool split = p.splits > 1;
             // 32 sums of one i: a split's part
@@ -504,7 +544,8 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                 }
                 release();
             } else {
-                // the elementwise part on the accumulators where they are: a lane has four i (16 hl + 8 o + lane / 4) and pairs of j
+                // the elementwise part on the accumulators where they are, and the result leaves by tensor-map stores (stores by the threads
+                // took half of the epilogue's time): a lane has four i (16 hl + 8 o + lane / 4) and pairs of j
                 constexpr bool kElementwise = kProduct == kForward || kProduct == kForwardE4M3;
                 float bias[4] = {}, scale[4] = {1.0f, 1.0f, 1.0f, 1.0f};
                 if (kElementwise) {
@@ -552,26 +593,28 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                                 if (kElementwise) e[i] += bias[2 * hl + o];
                             }
                             if (kElementwise) apply_act(p.finish.act, e);
-                            stmatrix_x4_trans(buf + lane * kPitch16 + (32 * quarter + 16 * hl + 8 * o) * 2, pack2(e[0], e[1]), pack2(e[2], e[3]),
-                                              pack2(e[4], e[5]), pack2(e[6], e[7]));
+                            const uint32_t at = 64 * quarter + 32 * hl + 16 * o;         // bytes into the 128 values
+                            stmatrix_x4_trans(buf + (at >> 7) * kBox16 + lane * 128 + ((at & 127) ^ ((lane & 7) << 4)), pack2(e[0], e[1]),
+                                              pack2(e[2], e[3]), pack2(e[4], e[5]), pack2(e[6], e[7]));
                         }
                     }
                     if (q < 3) {
                         fetch(c + 64);
                         if (kProduct == kForwardE4M3) token_scales(c + 64);
                     }
+                    fence_async_shared();
+                    if (tid == 0) store_groups_read();       // the other buffer, which is written next
                     named_barrier(2 + group, 128);
-                    bf16* out = static_cast<bf16*>(p.out);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int col = i * 8 + (tid >> 4);
-                        if (c + col < columns && i8 < p.I)
-                            *reinterpret_cast<uint4*>(out + static_cast<int64_t>(w.j0 + c + col) * p.I + i8) = load_shared16(buf + col * kPitch16 + (tid & 15) * 16);
+                    if (tid == 0 && i_cta < p.I) {
+                        tma_store_2d(&map_out, buf, i_cta, w.j0 + c);
+                        if (i_cta + 64 < p.I) tma_store_2d(&map_out, buf + kBox16, i_cta + 64, w.j0 + c);
+                        store_group_end();
                     }
                 }
                 release();
             }
         }
+        if (kForm == kPlain && tid == 0) store_groups_done();
         if (!ok && lane == 0) flag_error(p.err_word, COBALT_DEVERR_WAIT_TIMEOUT);
         __syncwarp();
     }
@@ -641,74 +684,81 @@ struct OperandVec {
 };
 
 // Up to R tokens on the fp32 units: `share` warps (1, 2, 4 or 8 of a CTA's eight) take one feature, its row of W once and the tokens'
-// rows from L1, and add their sums in order.  Every vector index is clamped to the row, so that no address lies outside it.
+// rows from L1, and add their sums in order.  Persistent CTAs; the next feature's first vectors are under way while one is summed up.
+// Every vector index is clamped to the row, so that no address lies outside it.
 template <bool kE4M3, int R>
-__global__ void __launch_bounds__(kFewThreads)
+__global__ void __launch_bounds__(kFewThreads, R < 4 ? 4 : 3)
 linear_few_rows_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict__ w, int T, int K, int N, int share, void* out, const Finish f)
 {
     constexpr int kAhead = 4, kElems = OperandVec<kE4M3>::kElems;        // vectors of W that a lane has in flight
-    __shared__ float sums[kFewThreads / 32][R];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % share, vecs = K / kElems;
-    const int feature = blockIdx.x * (8 / share) + warp / share, own = min(feature, N - 1);
+    __shared__ float sums[2][kFewThreads / 32][R];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % share, vecs = K / kElems, each = 8 / share;
+    const int tasks = (N + each - 1) / each, stride = 32 * kAhead * share, start = 32 * kAhead * part;
     wait_for_prior_kernel();
     launch_dependents();
-    const uint8_t* row = w + static_cast<int64_t>(own) * vecs * 16;
     uint4 next[kAhead];
-    auto load = [&](int base) {
+    auto load = [&](int task, int base) {
+        const uint8_t* row = w + static_cast<int64_t>(min(task * each + warp / share, N - 1)) * vecs * 16;
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) next[i] = ld_stream16(row + 16 * static_cast<int64_t>(min(base + 32 * i + lane, vecs - 1)));
     };
-    const int step = 32 * kAhead * share;
-    int base = 32 * kAhead * part;
-    load(base);
-    float sum[R] = {};
-    for (; base < vecs; base += step) {
-        uint4 now[kAhead];
+    load(blockIdx.x, start);
+    for (int task = blockIdx.x, turn = 0; task < tasks; task += gridDim.x, turn ^= 1) {
+        float sum[R] = {};
+        int base = start;
+        do {
+            uint4 now[kAhead];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) now[i] = next[i];
-        if (base + step < vecs) load(base + step);
+            for (int i = 0; i < kAhead; ++i) now[i] = next[i];
+            // the next vectors, or the first ones of the next task
+            const bool last = base + stride >= vecs;
+            if (!last || task + gridDim.x < tasks) load(last ? task + gridDim.x : task, last ? start : base + stride);
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int v = base + 32 * i + lane;
-            if (v >= vecs) continue;
-            const OperandVec<kE4M3> a(now[i]);
+            for (int i = 0; i < kAhead; ++i) {
+                const int v = base + 32 * i + lane;
+                if (v >= vecs) continue;
+                const OperandVec<kE4M3> a(now[i]);
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const int token = R == 1 ? 0 : min(r, T - 1);
-                const OperandVec<kE4M3> b(__ldg(reinterpret_cast<const uint4*>(x + (static_cast<int64_t>(token) * vecs + v) * 16)));
+                for (int r = 0; r < R; ++r) {
+                    const int token = R == 1 ? 0 : min(r, T - 1);
+                    const OperandVec<kE4M3> b(__ldg(reinterpret_cast<const uint4*>(x + (static_cast<int64_t>(token) * vecs + v) * 16)));
 #pragma unroll
-                for (int k = 0; k < kElems; ++k) sum[r] = fmaf(a.f[k], b.f[k], sum[r]);
+                    for (int k = 0; k < kElems; ++k) sum[r] = fmaf(a.f[k], b.f[k], sum[r]);
+                }
             }
+            base += stride;
+        } while (base < vecs);
+#pragma unroll
+        for (int r = 0; r < R; ++r) sum[r] = warp_sum(sum[r]);
+        if (lane == 0) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) sums[turn][warp][r] = sum[r];
         }
-    }
-#pragma unroll
-    for (int r = 0; r < R; ++r) sum[r] = warp_sum(sum[r]);
-    if (lane == 0) {
-#pragma unroll
-        for (int r = 0; r < R; ++r) sums[warp][r] = sum[r];
-    }
-    __syncthreads();
-    // one thread a result
-    const int i = blockIdx.x * (8 / share) + threadIdx.x / R, t = threadIdx.x % R;
-    if (threadIdx.x >= 8 / share * R || i >= N || t >= T) return;
-    float v[1] = {0.0f};
-    for (int k = 0; k < share; ++k) v[0] += sums[threadIdx.x / R * share + k][t];
-    const int64_t at = static_cast<int64_t>(t) * N + i;
-    if (kE4M3) v[0] *= __ldg(f.x_scales + t) * __ldg(f.w_scales + i);
-    if (f.bias) v[0] += __bfloat162float(f.bias[i]);
-    if (f.pre) static_cast<bf16*>(f.pre)[at] = __float2bfloat16_rn(v[0]);
-    apply_act(f.act, v);
-    if (f.f32) {
-        if (f.residual) v[0] += static_cast<const float*>(f.residual)[at];
-        static_cast<float*>(out)[at] = v[0];
-    } else {
-        if (f.residual) v[0] += __bfloat162float(static_cast<const bf16*>(f.residual)[at]);
-        static_cast<bf16*>(out)[at] = __float2bfloat16_rn(v[0]);
+        __syncthreads();
+        // one thread a result
+        const int i = task * each + threadIdx.x / R, t = threadIdx.x % R;
+        if (threadIdx.x >= each * R || i >= N || t >= T) continue;
+        float v[1] = {0.0f};
+        for (int k = 0; k < share; ++k) v[0] += sums[turn][threadIdx.x / R * share + k][t];
+        const int64_t at = static_cast<int64_t>(t) * N + i;
+        if (kE4M3) v[0] *= __ldg(f.x_scales + t) * __ldg(f.w_scales + i);
+        if (f.bias) v[0] += __bfloat162float(f.bias[i]);
+        if (f.pre) static_cast<bf16*>(f.pre)[at] = __float2bfloat16_rn(v[0]);
+        apply_act(f.act, v);
+        if (f.f32) {
+            if (f.residual) v[0] += static_cast<const float*>(f.residual)[at];
+            static_cast<float*>(out)[at] = v[0];
+        } else {
+            if (f.residual) v[0] += __bfloat162float(static_cast<const bf16*>(f.residual)[at]);
+            static_cast<bf16*>(out)[at] = __float2bfloat16_rn(v[0]);
+        }
     }
 }
 
 // d = dout act'(pre) in bf16 (where the products need it) and its column sums: a CTA has 128 features and a slice of the
-// tokens, 64 at a time; the sums of its sixteen token rows are added in order and written to partial [gridDim.y][N].
+// tokens, 32 at a time; the sums of its sixteen token rows are added in order and written to partial [gridDim.y][N].
+constexpr int kGradPreAhead = 2;         // tokens that a thread has in flight
+
 struct GradPreArgs {
     const void* grad_out;
     const void* pre;                     // or null
@@ -719,10 +769,10 @@ struct GradPreArgs {
     float* partial;                      // or null
 };
 
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 4)
 linear_grad_pre_kernel(const GradPreArgs p)
 {
-    constexpr int kAhead = 4;            // tokens that a thread has in flight
+    constexpr int kAhead = kGradPreAhead;
     __shared__ float sums[16][128];
     wait_for_prior_kernel();
     launch_dependents();
@@ -796,23 +846,25 @@ linear_grad_pre_kernel(const GradPreArgs p)
     }
 }
 
-// grad_bias: the parts' sums, eight threads a feature.
-__global__ void __launch_bounds__(256)
+// grad_bias: the parts' sums, 32 features a CTA, every warp a slice of the parts.
+__global__ void __launch_bounds__(1024)
 linear_bias_kernel(const float* partial, int parts, int N, bf16* __restrict__ grad_bias)
 {
-    __shared__ float slice[8][33];
+    __shared__ float slice[32][33];
     wait_for_prior_kernel();
     launch_dependents();
     const int lane = threadIdx.x & 31, own = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;
     float s = 0.0f;
-    if (i < N)
-        for (int k = own; k < parts; k += 8) s += partial[static_cast<int64_t>(k) * N + i];
+    if (i < N) {
+#pragma unroll 8
+        for (int k = own; k < parts; k += 32) s += partial[static_cast<int64_t>(k) * N + i];
+    }
     slice[own][lane] = s;
     __syncthreads();
     if (own == 0 && i < N) {
         float total = 0.0f;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) total += slice[k][lane];
+        for (int k = 0; k < 32; ++k) total += slice[k][lane];
         grad_bias[i] = __float2bfloat16_rn(total);
     }
 }
@@ -845,7 +897,7 @@ static LinearPlan linear_plan(int64_t I, int64_t J, int64_t blocks)
             const int64_t per = (blocks + s - 1) / s, waves = (tiles * s + kPlanPairs - 1) / kPlanPairs;
             if (per * (s - 1) >= blocks) continue;                 // a split without blocks
             double cycles = static_cast<double>(waves) * (per * block + 800.0) + 2500.0;
-            if (s > 1) cycles += 4000.0 + static_cast<double>(s) * I * J * 8.0 / 2500.0;
+            if (s > 1) cycles += 5500.0 + static_cast<double>(s) * I * J * 8.0 / 1000.0;
             if (cycles < least) {
                 least = cycles;
                 best = {n, s, static_cast<int>(per)};
@@ -866,13 +918,15 @@ static size_t part_bytes(int64_t I, int64_t J)
 
 static int64_t deep_blocks(int64_t k, int deep) { return (k + deep - 1) / deep; }
 
-// Slices of the tokens in the pass over the output's gradient: about six CTAs an SM.
+// Slices of the tokens in the pass over the output's gradient: about six CTAs an SM, of as equal a number of steps as can be.
 static int bias_parts(int64_t T, int N)
 {
-    const int64_t groups = (N + 127) / 128, rows = (T + 63) / 64;
+    const int64_t groups = (N + 127) / 128, steps = (T + 16 * kGradPreAhead - 1) / (16 * kGradPreAhead);
     int64_t parts = (6 * 2 * kPlanPairs + groups - 1) / groups;
-    if (parts > rows) parts = rows;
-    return static_cast<int>(parts < 1 ? 1 : parts);
+    if (parts > steps) parts = steps;
+    if (parts < 1) parts = 1;
+    const int64_t each = (steps + parts - 1) / parts;
+    return static_cast<int>((steps + each - 1) / each);
 }
 
 static int check_linear(int64_t T, int32_t K, int32_t N, int deep_unit)
@@ -910,13 +964,14 @@ static int launch_after(void (*kernel)(Params...), dim3 grid, dim3 block, size_t
 }
 
 // a: [I, k] or, transposed, [k, I]; b: [J, k] or [k, J].
-template <int kProduct, int kForm>
+template <int kProduct, int kForm, bool kStay = false>
 static int launch_product(const void* a, const void* b, int64_t I, int64_t J, int64_t k, LinearArgs p, void* workspace, cudaStream_t s)
 {
     constexpr bool kAMn = kProduct == kGradRows || kProduct == kGradWeights, kBMn = kProduct == kGradWeights;
     constexpr int kBytes = kProduct == kForwardE4M3 ? 1 : 2, kStepK = kDeepBytes / kBytes;
     const int64_t blocks = deep_blocks(k, kStepK);
-    const LinearPlan plan = linear_plan(I, J, blocks);
+    LinearPlan plan = linear_plan(I, J, blocks);
+    if (kStay) plan = {kTileN, 1, static_cast<int>(blocks)};
     p.I = static_cast<int>(I);
     p.J = static_cast<int>(J);
     p.n = plan.n;
@@ -926,24 +981,29 @@ static int launch_product(const void* a, const void* b, int64_t I, int64_t J, in
     p.blocks = static_cast<int>(blocks);
     p.per_split = plan.per_split;
     p.partial = static_cast<float*>(workspace);
-    CUtensorMap map_a, map_b;
+    CUtensorMap map_a, map_b, map_out;
     COBALT_TRY(kAMn ? matrix_map(&map_a, a, k, I, 64, kDeep) : matrix_map(&map_a, a, I, k, kStepK, 128, kBytes));
     COBALT_TRY(kBMn ? matrix_map(&map_b, b, k, J, 64, kDeep) : matrix_map(&map_b, b, J, k, kStepK, plan.n / 2, kBytes));
-    const void* kernel = reinterpret_cast<const void*>(&linear_kernel<kProduct, kForm>);
+    if (kForm == kPlain) COBALT_TRY(matrix_map(&map_out, p.out, J, I, 64, 32));
+    else map_out = map_a;                    // not used
+    const void* kernel = reinterpret_cast<const void*>(&linear_kernel<kProduct, kForm, kStay>);
     COBALT_TRY(ensure_kernel_attributes(kernel, kLinearSmem, false));
     int sms = 0;
     COBALT_TRY(sm_count(&sms));
     const int64_t tiles = static_cast<int64_t>(p.m_tiles) * p.j_tiles * p.splits, pairs = tiles < sms / 2 ? tiles : sms / 2;
     if (tiles >= (1ll << 31) - (1 << 16)) return COBALT_ERR_UNSUPPORTED;
     const dim3 grid(static_cast<unsigned>(2 * (pairs < 1 ? 1 : pairs)));
-    COBALT_TRY((launch_after(linear_kernel<kProduct, kForm>, grid, dim3(kLinearThreads), kLinearSmem, s, map_a, map_b, p)));
+    COBALT_TRY((launch_after(linear_kernel<kProduct, kForm, kStay>, grid, dim3(kLinearThreads), kLinearSmem, s, map_a, map_b, map_out, p)));
     if (p.splits == 1) return COBALT_OK;
     const int64_t threads = J * ((I + 127) / 128 * 16);
     return launch_after(linear_join_kernel<kProduct>, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, s, p);
 }
 
-// Most tokens that the fp32 units take.
-constexpr int kFewRows = 4;
+// Calls that the fp32 units take: one token, and up to four while the products are few.  Measured (us, this form / tiles, bf16): 7168 to
+// 2048, two tokens 9.2 / 11.0, three 16.8 / 11.2; 2048 to 1408, four tokens 4.1 / 7.2; 4096 to 8192, two tokens 18.6 / 15.9.
+static bool few_rows(int64_t T, int32_t K, int32_t N) { return T == 1 || (T <= 4 && T * K * N <= (1ll << 25)); }
+
+constexpr int kFewResident = 4;          // CTAs an SM
 
 template <bool kE4M3>
 static int launch_few_rows(const void* x, const void* w, int T, int K, int N, void* out, const Finish& f, cudaStream_t s)
@@ -952,7 +1012,10 @@ static int launch_few_rows(const void* x, const void* w, int T, int K, int N, vo
     const int vecs = K / OperandVec<kE4M3>::kElems;
     int share = 1;
     while (share < 8 && N * share < 4096 && vecs >= 256 * share) share *= 2;
-    const dim3 grid(static_cast<unsigned>((N + 8 / share - 1) / (8 / share))), block(kFewThreads);
+    int sms = 0;
+    COBALT_TRY(sm_count(&sms));
+    const int tasks = (N + 8 / share - 1) / (8 / share), most = kFewResident * sms;
+    const dim3 grid(static_cast<unsigned>(tasks < most ? tasks : most)), block(kFewThreads);
     const uint8_t *a = static_cast<const uint8_t*>(x), *b = static_cast<const uint8_t*>(w);
     if (T == 1) return launch_after(linear_few_rows_kernel<kE4M3, 1>, grid, block, 0, s, a, b, T, K, N, share, out, f);
     if (T == 2) return launch_after(linear_few_rows_kernel<kE4M3, 2>, grid, block, 0, s, a, b, T, K, N, share, out, f);
@@ -992,7 +1055,7 @@ int cobalt_linear(const void* x, const float* x_scales, const void* w, const flo
     p.finish = {static_cast<const bf16*>(bias), residual, e4m3 ? x_scales : nullptr, e4m3 ? w_scales : nullptr, act, out_type == COBALT_F32, pre,
                 pre8 ? pre_scales : nullptr};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (T <= kFewRows && !pre8)
+    if (few_rows(T, K, N) && !pre8)
         return e4m3 ? launch_few_rows<true>(x, w, static_cast<int>(T), K, N, out, p.finish, s)
                     : launch_few_rows<false>(x, w, static_cast<int>(T), K, N, out, p.finish, s);
     const int form = out_type == COBALT_F32 ? kLong : residual || pre ? kFull : kPlain;
@@ -1034,13 +1097,17 @@ int cobalt_linear_backward(const void* grad_out, const void* x, const void* w, c
         const int parts = bias_parts(T, N);
         COBALT_TRY(launch_after(linear_grad_pre_kernel, dim3((N + 127) / 128, parts), dim3(256), 0, s, g));
         if (grad_bias)
-            COBALT_TRY(launch_after(linear_bias_kernel, dim3((N + 31) / 32), dim3(256), 0, s, static_cast<const float*>(g.partial), parts, N,
+            COBALT_TRY(launch_after(linear_bias_kernel, dim3((N + 31) / 32), dim3(1024), 0, s, static_cast<const float*>(g.partial), parts, N,
                                     static_cast<bf16*>(grad_bias)));
         if (converts) d = grad_pre;
     }
     if (grad_x) {
         p.out = grad_x;
-        COBALT_TRY((launch_product<kGradRows, kPlain>(w, d, K, T, N, p, workspace, s)));
+        // the operand that stays is loaded once for all of i: where there are tiles enough for every pair to keep one for a while
+        if (N <= kStayBlocks * kDeep && K >= 4 * kTileM && T >= 4 * kPlanPairs * kTileN)
+            COBALT_TRY((launch_product<kGradRows, kPlain, true>(w, d, K, T, N, p, workspace, s)));
+        else
+            COBALT_TRY((launch_product<kGradRows, kPlain>(w, d, K, T, N, p, workspace, s)));
     }
     if (grad_w) {
         p.out = grad_w;

@@ -138,6 +138,23 @@ def test_linear_gradients_against_plain(T, K, N, act, pre_type):
                 assert torch.equal(one, like)
 
 
+@pytest.mark.parametrize("T,K,N", [(75777, 1032, 136), (80000, 2056, 256), (75800, 1024, 8)])
+def test_linear_gradient_of_many_rows_from_a_few_features(T, K, N):
+    """A router's dx: few blocks of the summed extent, many tokens; rows at the ends and in between checked one by one."""
+    import paper_2609_36959_b200 as cb
+    _, w, _, _, dy = _inputs(T, K, N, 3)
+    whole, gx = _guarded(T, K, BF16)
+    for _ in range(2):
+        gx.fill_(5.0)
+        cb.linear_backward(dy, None, w, _workspace(T, K, N), grad_x=gx)
+    torch.cuda.synchronize()
+    assert (whole[T] == 7).all() and cb.read_and_clear_device_error() == 0
+    for part in (slice(0, 20000), slice(30000, 50000), slice(T - 26000, T)):
+        ref = dy[part].double() @ w.double()
+        size = 2 * (N + 4) * U * (dy[part].double().abs() @ w.double().abs())
+        assert ((gx[part].double() - ref).abs() <= size + D.HALF[BF16] * (ref.abs() + size)).all()
+
+
 def test_linear_rows_keep_to_themselves():
     """A row of x with a NaN or an infinity reaches its own row of the result only; one of W its own column."""
     import paper_2609_36959_b200 as cb
