@@ -472,7 +472,9 @@ int cobalt_rms_norm_backward(const void* grad_y, const void* grad_sum, const voi
  * x [T, K] and w [N, K] bf16 (operand COBALT_BF16; the scales are not read), or e4m3 codes with one scale a row, fp32 [T] and
  * [N], as cobalt_pack_rows leaves them with group 0 (operand COBALT_E4M3).  bias bf16 [N] or NULL; residual [T, N] like
  * out, or NULL; out of out_type COBALT_BF16 or COBALT_F32.  pre, where a backward pass follows an activation: bf16 [T, N]
- * (pre_type COBALT_BF16), or COBALT_I8 codes [T, N] with pre_scales fp32 [T, ceil(N / 128)]; else NULL.  act:
+ * (pre_type COBALT_BF16), or COBALT_I8 codes [T, N] with pre_scales fp32 [T, ceil(N / 128)]; else NULL.  The backward
+ * call takes the slope at the value that was kept: in 8 bits, values below half a step are 0, where relu's slope is 0 (0.4 % of
+ * a normal distribution): keep bf16 for relu.  act:
  *   COBALT_ACT_NONE   COBALT_ACT_RELU   COBALT_ACT_SILU v / (1 + exp(-v))   COBALT_ACT_GELU v (1 + erf(v / sqrt 2)) / 2
  * Backward, for bf16 x and w, with grad_out [T, N] of grad_type (COBALT_BF16 or COBALT_F32):
  *   d = grad_out * act'(pre)     grad_x = d w     grad_w = d^T x     grad_bias = sum_t d     (bf16, overwritten)

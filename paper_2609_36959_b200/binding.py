@@ -715,38 +715,83 @@ def dropout_add_backward(grad_out: torch.Tensor, p: float, seed, grad_x: torch.T
 
 
 # ---- the dense part of a layer --------------------------------------------------------------
+# These calls are a few microseconds of GPU time for a token or two, so the checks query every tensor once.
 
 _CODES = {torch.float8_e4m3fn: E4M3, torch.int8: I8}
+_get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _packed(packed, T: int, H: int, what: str):
+def _current_device() -> int:
+    try:
+        return _get_device()
+    except RuntimeError:                         # no driver: no tensor is there either
+        return -2
+
+
+def _here(t: Optional[torch.Tensor], device: int, dtype: torch.dtype, shape, what: str) -> Optional[int]:
+    """The pointer of a contiguous tensor of this type and shape on this device."""
+    if t is None:
+        return None
+    if t.get_device() == device and t.dtype is dtype and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    if not t.is_cuda:
+        raise TypeError(f"{what} must be a CUDA tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise CobaltError(ERR_INVALID_ARG, f"{what} (size {tuple(t.shape)}, not {tuple(shape)})")
+    if not t.is_contiguous():
+        raise TypeError(f"{what} must be contiguous")
+    raise CobaltError(ERR_INVALID_ARG, f"{what} (on device {t.get_device()}, the current one is {device})")
+
+
+def _workspace(t: torch.Tensor, device: int) -> int:
+    if t.get_device() != device or not t.is_contiguous():
+        raise TypeError("workspace must be a contiguous tensor on the current device")
+    return t.data_ptr()
+
+
+def _stream_on(device: int) -> int:
+    return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+
+
+def _packed(packed, device: int, T: int, H: int, what: str):
     """(codes pointer, scales pointer, code, group) of rows in 8 bits: codes float8_e4m3fn or int8 [T, H], scales float32 with
     one value a row ([T] or [T, 1]) or one for each 128 columns ([T, ceil(H / 128)])."""
     q, scales = packed
     code = _CODES.get(q.dtype)
     if code is None:
         raise TypeError(f"{what} must be float8_e4m3fn or int8, got {q.dtype}")
-    groups = scales.numel() // T if T > 0 else (scales.shape[1] if scales.dim() == 2 else 1)
-    if tuple(q.shape) != (T, H) or scales.numel() != T * groups or groups not in (1, -(-H // PACK_GROUP)):
-        raise CobaltError(ERR_INVALID_ARG, f"{what} (sizes)")
-    return _ptr(q, None, what), _ptr(scales, torch.float32, f"{what} scales"), code, 0 if groups == 1 else PACK_GROUP
+    groups = -(-H // PACK_GROUP)
+    size = scales.shape
+    if len(size) == 2 and size[1] == groups:
+        group = PACK_GROUP if groups > 1 else 0
+    elif len(size) == 1 or (len(size) == 2 and size[1] == 1):
+        group = 0
+    else:
+        raise CobaltError(ERR_INVALID_ARG, f"{what} scales (size {tuple(size)})")
+    if size[0] != T:
+        raise CobaltError(ERR_INVALID_ARG, f"{what} scales (size {tuple(size)})")
+    return _here(q, device, q.dtype, (T, H), what), _here(scales, device, torch.float32, size, what), code, group
 
 
 def pack_rows(x: torch.Tensor, q: torch.Tensor, scales: torch.Tensor) -> None:
     """Rows of x [T, H] (bfloat16 or float32) in 8 bits: q float8_e4m3fn or int8 [T, H], scales float32, one a row ([T] or
     [T, 1]) or one for each 128 columns ([T, ceil(H / 128)]).  A group's largest absolute value becomes the largest code."""
-    T, H = x.shape
-    q_ptr, scales_ptr, code, group = _packed((q, scales), T, H, "q")
-    _check(_lib.cobalt_pack_rows(_ptr(x, None, "x"), T, H, _dtype_code(x, "x"), code, group, q_ptr, scales_ptr, _stream()),
-           "cobalt_pack_rows")
+    shape, device = x.shape, _current_device()
+    T, H = shape
+    q_ptr, scales_ptr, code, group = _packed((q, scales), device, T, H, "q")
+    _check(_lib.cobalt_pack_rows(_here(x, device, x.dtype, shape, "x"), T, H, _dtype_code(x, "x"), code, group, q_ptr, scales_ptr,
+                                 _stream_on(device)), "cobalt_pack_rows")
 
 
 def unpack_rows(q: torch.Tensor, scales: torch.Tensor, out: torch.Tensor) -> None:
     """out [T, H] (bfloat16 or float32) = the values of rows that pack_rows (or rms_norm, or linear) left in 8 bits."""
-    T, H = out.shape
-    q_ptr, scales_ptr, code, group = _packed((q, scales), T, H, "q")
-    _check(_lib.cobalt_unpack_rows(q_ptr, scales_ptr, T, H, code, group, _dtype_code(out, "out"), _ptr(out, None, "out"), _stream()),
-           "cobalt_unpack_rows")
+    shape, device = out.shape, _current_device()
+    T, H = shape
+    q_ptr, scales_ptr, code, group = _packed((q, scales), device, T, H, "q")
+    _check(_lib.cobalt_unpack_rows(q_ptr, scales_ptr, T, H, code, group, _dtype_code(out, "out"),
+                                   _here(out, device, out.dtype, shape, "out"), _stream_on(device)), "cobalt_unpack_rows")
 
 
 def rms_norm(x: torch.Tensor, gamma: torch.Tensor, eps: float, *, residual: Optional[torch.Tensor] = None,
@@ -755,17 +800,13 @@ def rms_norm(x: torch.Tensor, gamma: torch.Tensor, eps: float, *, residual: Opti
     """y = s * rstd * gamma over the rows of s = x + residual [T, H] (bfloat16 or float32, s in the same type; gamma float32
     [H]).  Written where given: the sum, y, packed = (q, scales) with y in 8 bits as in pack_rows, and rstd float32 [T] for
     rms_norm_backward."""
-    T, H = x.shape
-    code = _dtype_code(x, "x")
-    for t in (residual, sum_out, y):
-        if t is not None and t.shape != x.shape:
-            raise CobaltError(ERR_INVALID_ARG, "rms_norm (sizes)")
-    if gamma.numel() != H or (rstd is not None and rstd.numel() != T):
-        raise CobaltError(ERR_INVALID_ARG, "rms_norm (sizes)")
-    q_ptr, scales_ptr, q_code, group = (None, None, 0, 0) if packed is None else _packed(packed, T, H, "packed")
-    _check(_lib.cobalt_rms_norm(_ptr(x, None, "x"), _ptr(residual, x.dtype, "residual"), _ptr(gamma, torch.float32, "gamma"), T, H, code,
-                                eps, _ptr(sum_out, x.dtype, "sum_out"), _ptr(y, x.dtype, "y"), q_ptr, scales_ptr, q_code, group,
-                                _ptr(rstd, torch.float32, "rstd"), _stream()), "cobalt_rms_norm")
+    shape, dtype, device = x.shape, x.dtype, _current_device()
+    T, H = shape
+    q_ptr, scales_ptr, q_code, group = (None, None, 0, 0) if packed is None else _packed(packed, device, T, H, "packed")
+    _check(_lib.cobalt_rms_norm(_here(x, device, dtype, shape, "x"), _here(residual, device, dtype, shape, "residual"),
+                                _here(gamma, device, torch.float32, (H,), "gamma"), T, H, _dtype_code(x, "x"), eps,
+                                _here(sum_out, device, dtype, shape, "sum_out"), _here(y, device, dtype, shape, "y"), q_ptr, scales_ptr,
+                                q_code, group, _here(rstd, device, torch.float32, (T,), "rstd"), _stream_on(device)), "cobalt_rms_norm")
 
 
 def rms_norm_workspace_bytes(T: int, H: int) -> int:
@@ -776,21 +817,20 @@ def rms_norm_backward(grad_y: torch.Tensor, rows, gamma: torch.Tensor, rstd: tor
                       grad_gamma: torch.Tensor, workspace: torch.Tensor, *, grad_sum: Optional[torch.Tensor] = None) -> None:
     """Gradients of rms_norm: grad_x [T, H] (of x and of residual alike) and grad_gamma float32 [H].  rows is the sum that was
     normalised, or (q, scales) as pack_rows left it; grad_sum is the gradient that reaches the sum past the norm."""
-    T, H = grad_y.shape
+    shape, dtype, device = grad_y.shape, grad_y.dtype, _current_device()
+    T, H = shape
     code = _dtype_code(grad_y, "grad_y")
-    if (grad_x.shape != grad_y.shape or (grad_sum is not None and grad_sum.shape != grad_y.shape) or gamma.numel() != H or
-            rstd.numel() != T or grad_gamma.numel() != H):
-        raise CobaltError(ERR_INVALID_ARG, "rms_norm_backward (sizes)")
     if isinstance(rows, tuple):
-        rows_ptr, scales_ptr, rows_type, group = _packed(rows, T, H, "rows")
+        rows_ptr, scales_ptr, rows_type, group = _packed(rows, device, T, H, "rows")
     else:
-        if rows.shape != grad_y.shape:
-            raise CobaltError(ERR_INVALID_ARG, "rms_norm_backward (sizes)")
-        rows_ptr, scales_ptr, rows_type, group = _ptr(rows, grad_y.dtype, "rows"), None, code, 0
-    _check(_lib.cobalt_rms_norm_backward(_ptr(grad_y, None, "grad_y"), _ptr(grad_sum, grad_y.dtype, "grad_sum"), rows_ptr, scales_ptr,
-                                         rows_type, group, _ptr(gamma, torch.float32, "gamma"), _ptr(rstd, torch.float32, "rstd"), T, H,
-                                         code, _ptr(grad_x, grad_y.dtype, "grad_x"), _ptr(grad_gamma, torch.float32, "grad_gamma"),
-                                         _ptr(workspace), _ws_bytes(workspace), _stream()), "cobalt_rms_norm_backward")
+        rows_ptr, scales_ptr, rows_type, group = _here(rows, device, dtype, shape, "rows"), None, code, 0
+    _check(_lib.cobalt_rms_norm_backward(_here(grad_y, device, dtype, shape, "grad_y"), _here(grad_sum, device, dtype, shape, "grad_sum"),
+                                         rows_ptr, scales_ptr, rows_type, group, _here(gamma, device, torch.float32, (H,), "gamma"),
+                                         _here(rstd, device, torch.float32, (T,), "rstd"), T, H, code,
+                                         _here(grad_x, device, dtype, shape, "grad_x"),
+                                         _here(grad_gamma, device, torch.float32, (H,), "grad_gamma"), _workspace(workspace, device),
+                                         _ws_bytes(workspace),
+                                         _stream_on(device)), "cobalt_rms_norm_backward")
 
 
 def linear_workspace_bytes(T: int, K: int, N: int) -> int:
@@ -805,17 +845,15 @@ def _activation(act: str) -> int:
     return code
 
 
-def _pre(pre, T: int, N: int, what: str):
+def _pre(pre, device: int, T: int, N: int, what: str):
     if pre is None:
         return None, None, BF16
     if isinstance(pre, tuple):
-        q_ptr, scales_ptr, code, group = _packed(pre, T, N, "pre")
+        q_ptr, scales_ptr, code, group = _packed(pre, device, T, N, "pre")
         if code != I8 or (group == 0 and N > PACK_GROUP):
             raise CobaltError(ERR_INVALID_ARG, f"{what} (pre in 8 bits is int8 with a scale for each 128 columns)")
         return q_ptr, scales_ptr, I8
-    if tuple(pre.shape) != (T, N):
-        raise CobaltError(ERR_INVALID_ARG, f"{what} (pre size)")
-    return _ptr(pre, torch.bfloat16, "pre"), None, BF16
+    return _here(pre, device, torch.bfloat16, (T, N), "pre"), None, BF16
 
 
 def linear(x, w, out: torch.Tensor, workspace: torch.Tensor, *, bias: Optional[torch.Tensor] = None,
@@ -825,23 +863,25 @@ def linear(x, w, out: torch.Tensor, workspace: torch.Tensor, *, bias: Optional[t
     x [T, K] and w [N, K] are both bfloat16, or both (q, scales) in float8_e4m3fn with one scale a row, as pack_rows and
     rms_norm leave them.  bias bfloat16 [N]; residual like out.  act: none, relu, silu or gelu.  pre, where a backward pass
     follows an activation: bfloat16 [T, N], or (int8 [T, N], float32 [T, ceil(N / 128)]) to keep it in 8 bits."""
-    x8, w8 = isinstance(x, tuple), isinstance(w, tuple)
-    if x8 != w8:
+    shape, device = out.shape, _current_device()
+    T, N = shape
+    if isinstance(x, tuple) != isinstance(w, tuple):
         raise TypeError("x and w must both be bfloat16, or both (q, scales)")
-    (T, K), (N, K_w) = (x[0] if x8 else x).shape, (w[0] if w8 else w).shape
-    if K_w != K or tuple(out.shape) != (T, N) or (bias is not None and bias.numel() != N) or (residual is not None and residual.shape != out.shape):
-        raise CobaltError(ERR_INVALID_ARG, "linear (sizes)")
-    if x8:
-        x_ptr, x_scales, code, group = _packed(x, T, K, "x")
-        w_ptr, w_scales, w_code, w_group = _packed(w, N, K, "w")
+    if isinstance(x, tuple):
+        K = x[0].shape[1]
+        x_ptr, x_scales, code, group = _packed(x, device, T, K, "x")
+        w_ptr, w_scales, w_code, w_group = _packed(w, device, N, K, "w")
         if (code, group, w_code, w_group) != (E4M3, 0, E4M3, 0):
             raise CobaltError(ERR_INVALID_ARG, "linear (8-bit operands are float8_e4m3fn with one scale a row)")
     else:
-        x_ptr, x_scales, w_ptr, w_scales, code = _ptr(x, torch.bfloat16, "x"), None, _ptr(w, torch.bfloat16, "w"), None, BF16
-    pre_ptr, pre_scales, pre_type = _pre(pre, T, N, "linear")
-    _check(_lib.cobalt_linear(x_ptr, x_scales, w_ptr, w_scales, _ptr(bias, torch.bfloat16, "bias"), _ptr(residual, out.dtype, "residual"),
-                              T, K, N, code, _activation(act), _dtype_code(out, "out"), pre_ptr, pre_scales, pre_type,
-                              _ptr(out, None, "out"), _ptr(workspace), _ws_bytes(workspace), _stream()), "cobalt_linear")
+        K = x.shape[1]
+        x_ptr, x_scales, code = _here(x, device, torch.bfloat16, (T, K), "x"), None, BF16
+        w_ptr, w_scales = _here(w, device, torch.bfloat16, (N, K), "w"), None
+    pre_ptr, pre_scales, pre_type = _pre(pre, device, T, N, "linear")
+    _check(_lib.cobalt_linear(x_ptr, x_scales, w_ptr, w_scales, _here(bias, device, torch.bfloat16, (N,), "bias"),
+                              _here(residual, device, out.dtype, shape, "residual"), T, K, N, code, _activation(act), _dtype_code(out, "out"),
+                              pre_ptr, pre_scales, pre_type, _here(out, device, out.dtype, shape, "out"), _workspace(workspace, device),
+                              _ws_bytes(workspace), _stream_on(device)), "cobalt_linear")
 
 
 def linear_backward(grad_out: torch.Tensor, x: Optional[torch.Tensor], w: Optional[torch.Tensor], workspace: torch.Tensor, *,
@@ -850,19 +890,17 @@ def linear_backward(grad_out: torch.Tensor, x: Optional[torch.Tensor], w: Option
     """Gradients of linear for bfloat16 x and w, from grad_out [T, N] (bfloat16 or float32) and the pre of the forward call:
     grad_x [T, K], grad_w [N, K], grad_bias [N], bfloat16, each of which may be left out (x is read for grad_w, w for grad_x).
     grad_pre [T, N] bfloat16 is scratch, needed with an activation or a float32 grad_out; it may be a bfloat16 grad_out."""
-    T, N = grad_out.shape
-    sizes = {t.shape[1] for t in (x, w, grad_x, grad_w) if t is not None}
-    K = sizes.pop() if len(sizes) == 1 else 8
-    for t, shape in ((x, (T, K)), (w, (N, K)), (grad_x, (T, K)), (grad_w, (N, K)), (grad_pre, (T, N)), (grad_bias, (N,))):
-        if sizes or (t is not None and tuple(t.shape) != shape):
-            raise CobaltError(ERR_INVALID_ARG, "linear_backward (sizes)")
-    pre_ptr, pre_scales, pre_type = _pre(pre, T, N, "linear_backward")
+    shape, device = grad_out.shape, _current_device()
+    T, N = shape
+    K = next((t.shape[1] for t in (x, w, grad_x, grad_w) if t is not None), 8)
+    pre_ptr, pre_scales, pre_type = _pre(pre, device, T, N, "linear_backward")
     bf16 = torch.bfloat16
-    _check(_lib.cobalt_linear_backward(_ptr(grad_out, None, "grad_out"), _ptr(x, bf16, "x"), _ptr(w, bf16, "w"), pre_ptr, pre_scales,
-                                       pre_type, T, K, N, _activation(act), _dtype_code(grad_out, "grad_out"),
-                                       _ptr(grad_pre, bf16, "grad_pre"), _ptr(grad_x, bf16, "grad_x"), _ptr(grad_w, bf16, "grad_w"),
-                                       _ptr(grad_bias, bf16, "grad_bias"), _ptr(workspace), _ws_bytes(workspace), _stream()),
-           "cobalt_linear_backward")
+    _check(_lib.cobalt_linear_backward(_here(grad_out, device, grad_out.dtype, shape, "grad_out"), _here(x, device, bf16, (T, K), "x"),
+                                       _here(w, device, bf16, (N, K), "w"),
+                                       pre_ptr, pre_scales, pre_type, T, K, N, _activation(act), _dtype_code(grad_out, "grad_out"),
+                                       _here(grad_pre, device, bf16, shape, "grad_pre"), _here(grad_x, device, bf16, (T, K), "grad_x"),
+                                       _here(grad_w, device, bf16, (N, K), "grad_w"), _here(grad_bias, device, bf16, (N,), "grad_bias"), _workspace(workspace, device),
+                                       _ws_bytes(workspace), _stream_on(device)), "cobalt_linear_backward")
 
 
 def read_and_clear_device_error() -> int:

@@ -509,7 +509,7 @@ int cobalt_rms_norm(const void* x, const void* residual, const float* gamma, int
 {
     int rc = check_rms(T, H, dtype);
     if (rc != COBALT_OK) return rc;
-    if (!(eps >= 0.0f) || (q && !check_code(q_code, q_group)) || (!residual && sum)) return COBALT_ERR_INVALID_ARG;
+    if (!(eps >= 0.0f) || (q && !check_code(q_code, q_group)) || (!residual && sum) || (sum && sum == y)) return COBALT_ERR_INVALID_ARG;
     if (T == 0) return COBALT_OK;
     if (!x || !gamma || (!y && !q) || (q && !q_scales)) return COBALT_ERR_INVALID_ARG;
     if (!aligned16(x) || !aligned16(residual) || !aligned16(gamma) || !aligned16(sum) || !aligned16(y) || !aligned16(q) ||
