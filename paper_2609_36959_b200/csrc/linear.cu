@@ -96,11 +96,12 @@ constexpr float kLog2E = 1.44269504088896341f;
 
 __device__ __forceinline__ float fast_sigmoid(float v) { return fast_inverse(1.0f + fast_exp2(-kLog2E * v)); }
 
-// The activations, of whole arrays: the switch stands outside the loops (inside, it took as long as the rest of the epilogue).
-// gelu's normal distribution function comes from the rational approximations of Abramowitz and Stegun's Handbook for erf of a = |v| / sqrt 2:
-//   7.1.28 (to 3e-7, no exponential)   erf a = 1 - (1 + a1 a + ... + a6 a^6)^-16
+// The activations, of whole arrays: the switch stands outside the loops (inside, it took as long as the rest of the epilogue), and the
+// arithmetic is on pairs, since the epilogue is bound by instructions.  gelu's normal distribution function comes from the rational
+// approximations of Abramowitz and Stegun's Handbook for erf of a = |v| / sqrt 2:
+//   7.1.28 (to 3e-7, no exponential)   erf a = 1 - (1 + a1 a + ... + a6 a^6)^-16        gelu = max(v, 0) - |v| / 2 (1 + ...)^-16
 //   7.1.26 (to 1.5e-7)                 erf a = 1 - (b1 t + ... + b5 t^5) exp(-a^2), t = 1 / (1 + 0.3275911 a)
-// both without branches; the epilogue is bound by instructions, and erff with its two branches takes three times as many.
+// both without branches.  (The coefficients here are those of |v|: a_k 2^(-k / 2).)
 template <int N>
 __device__ __forceinline__ void apply_act(int act, float (&v)[N])
 {
@@ -111,21 +112,25 @@ __device__ __forceinline__ void apply_act(int act, float (&v)[N])
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] *= fast_sigmoid(v[i]);
     } else if (act == COBALT_ACT_GELU) {
+        constexpr int kStep = N > 1 ? 2 : 1;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float a = fabsf(v[i]) * 0.70710678118654752f;
-            float p = fmaf(a, 0.0000430638f, 0.0002765672f);
-            p = fmaf(a, p, 0.0001520143f);
-            p = fmaf(a, p, 0.0092705272f);
-            p = fmaf(a, p, 0.0422820123f);
-            p = fmaf(a, p, 0.0705230784f);
-            p = fmaf(a, p, 1.0f);
-            p *= p;
-            p *= p;
-            p *= p;
-            p *= p;
-            const float tail = 0.5f * fast_inverse(p);                              // beyond |v|, on one side
-            v[i] *= v[i] > 0.0f ? 1.0f - tail : tail;
+        for (int i = 0; i < N; i += kStep) {
+            // (|v| held finite: infinity times 0 below)
+            const Pair a = pair(fminf(fabsf(v[i]), 1e4f), fminf(fabsf(v[i + kStep - 1]), 1e4f)), h = a * pair(-0.5f);
+            Pair p = fma2(a, pair(5.382975000e-06f), pair(4.889063564e-05f));
+            p = fma2(a, p, pair(3.800357500e-05f));
+            p = fma2(a, p, pair(3.277626324e-03f));
+            p = fma2(a, p, pair(2.114100615e-02f));
+            p = fma2(a, p, pair(4.986734697e-02f));
+            p = fma2(a, p, pair(1.0f));
+            p = p * p;
+            p = p * p;
+            p = p * p;
+            p = p * p;
+            const Pair r = fma2(h, pair(fast_inverse(p.v.x), fast_inverse(p.v.y)),
+                                pair(v[i] < 0.0f ? 0.0f : v[i], v[i + kStep - 1] < 0.0f ? 0.0f : v[i + kStep - 1]));
+            v[i] = r.v.x;
+            v[i + kStep - 1] = r.v.y;
         }
     }
 }
@@ -589,8 +594,15 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
                                 e[i] = __uint_as_float(r[hl][4 * (i >> 1) + 2 * o + (i & 1)]);
-                                if (kProduct == kForwardE4M3) e[i] *= sx[i] * scale[2 * hl + o];
-                                if (kElementwise) e[i] += bias[2 * hl + o];
+                            }
+                            if (kElementwise) {
+#pragma unroll
+                                for (int i = 0; i < 8; i += 2) {
+                                    Pair u = pair(e[i], e[i + 1]);
+                                    if (kProduct == kForwardE4M3) u = fma2(u, pair(sx[i], sx[i + 1]) * pair(scale[2 * hl + o]), pair(bias[2 * hl + o]));
+                                    else u = u + pair(bias[2 * hl + o]);
+                                    e[i] = u.v.x, e[i + 1] = u.v.y;
+                                }
                             }
                             if (kElementwise) apply_act(p.finish.act, e);
                             const uint32_t at = 64 * quarter + 32 * hl + 16 * o;         // bytes into the 128 values

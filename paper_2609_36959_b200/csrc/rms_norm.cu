@@ -73,19 +73,20 @@ struct RmsForward {
     float* rstd;                             // or null
 };
 
-// A row's codes and scales.  y is itself a rounded value: a code at a border may go either way.
+// A row's codes and scales; most: of y / rstd.  y is itself a rounded value: a code at a border may go either way.
 template <typename Code, int N, int VPT>
-__device__ __forceinline__ void store_packed(const RmsForward& p, int64_t row, int first, int step, const float (&y)[VPT][N], const uint32_t (&most)[VPT],
-                                             uint32_t row_most)
+__device__ __forceinline__ void store_packed(const RmsForward& p, int64_t row, int first, int step, float rstd, const float (&y)[VPT][N],
+                                             const uint32_t (&most)[VPT], uint32_t row_most)
 {
-    GroupScale g = GroupScale::of<Code>(row_most);
+    auto scale_of = [rstd](uint32_t bits) { return GroupScale::of<Code>(abs_bits(__uint_as_float(bits) * rstd)); };
+    GroupScale g = scale_of(row_most);
     if (p.group == 0 && first == 0) p.scales[row] = g.scale;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
         const int at = first + i * step;
         if (at >= p.H / N) continue;
         if (p.group != 0) {
-            g = GroupScale::of<Code>(most[i]);
+            g = scale_of(most[i]);
             if (at % (kPackGroup / N) == 0) p.scales[row * ((p.H + kPackGroup - 1) / kPackGroup) + at / (kPackGroup / N)] = g.scale;
         }
         uint32_t w[N / 4];
@@ -141,13 +142,30 @@ rms_norm_kernel(const RmsForward p)
             if (p.sum && at < n_vec) st_stream16(static_cast<T*>(p.sum) + at_row + at * N, v[i]);
         }
     }
-    float squares[1] = {0.0f};
+    float squares[1] = {0.0f}, sg[kPacked ? VPT : 1][N];
+    uint32_t most[kPacked ? VPT : 1], row_most = 0;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
         float f[N];
         Vec16<T>::unpack(v[i], f);
 #pragma unroll
         for (int k = 0; k < N; ++k) squares[0] = fmaf(f[k], f[k], squares[0]);
+        if constexpr (kPacked) {             // the largest |s gamma| too: times rstd it is the largest |y|, and one barrier serves both
+            const int at = first + i * step;
+            float g[N] = {};
+            if (at < n_vec) load_gamma<N>(p.gamma + at * N, p.wide, g);
+            most[i] = 0;
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                sg[i][k] = f[k] * g[k];
+                if (at < n_vec) most[i] = abs_max(most[i], sg[i][k]);
+            }
+            row_most = max(row_most, most[i]);
+        }
+    }
+    if (kPacked && p.group == 0) {
+        row_most = __reduce_max_sync(0xFFFFFFFFu, row_most);
+        if (kCta && lane == 0) scratch_max[warp] = row_most;
     }
     row_sums<kCta, 1>(squares, scratch);
     const float rstd = rsqrtf(squares[0] / static_cast<float>(p.H) + p.eps);
@@ -166,43 +184,23 @@ rms_norm_kernel(const RmsForward p)
             st_stream16(static_cast<T*>(p.y) + at_row + at * N, Vec16<T>::pack(f));
         }
     } else {
-        // y in registers between a group's largest value and its codes
-        float y[VPT][N];
-        uint32_t most[VPT], row_most = 0;
-#pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            const int at = first + i * step;
-            most[i] = 0;
-#pragma unroll
-            for (int k = 0; k < N; ++k) y[i][k] = 0.0f;
-            if (at < n_vec) {
-                float g[N];
-                load_gamma<N>(p.gamma + at * N, p.wide, g);
-                Vec16<T>::unpack(v[i], y[i]);
-#pragma unroll
-                for (int k = 0; k < N; ++k) {
-                    y[i][k] = y[i][k] * rstd * g[k];
-                    most[i] = abs_max(most[i], y[i][k]);
-                }
-                if (p.y) st_stream16(static_cast<T*>(p.y) + at_row + at * N, Vec16<T>::pack(y[i]));
-            }
-            row_most = max(row_most, most[i]);
-        }
         if (p.group == 0) {
-            row_most = __reduce_max_sync(0xFFFFFFFFu, row_most);
-            if (kCta) {
-                if (lane == 0) scratch_max[warp] = row_most;
-                __syncthreads();
-                row_most = __reduce_max_sync(0xFFFFFFFFu, lane < (blockDim.x >> 5) ? scratch_max[lane] : 0u);
-            }
-        } else {                         // 128 columns: neighbouring lanes, all of them here
+            if (kCta) row_most = __reduce_max_sync(0xFFFFFFFFu, lane < (blockDim.x >> 5) ? scratch_max[lane] : 0u);
+        } else {                             // 128 columns: neighbouring lanes, all of them here
 #pragma unroll
             for (int i = 0; i < VPT; ++i)
 #pragma unroll
                 for (int off = 1; off < kPackGroup / N; off <<= 1) most[i] = max(most[i], __shfl_xor_sync(0xFFFFFFFFu, most[i], off));
         }
-        if (p.code == COBALT_E4M3) store_packed<CodeE4M3, N, VPT>(p, row, first, step, y, most, row_most);
-        else store_packed<CodeI8, N, VPT>(p, row, first, step, y, most, row_most);
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            const int at = first + i * step;
+#pragma unroll
+            for (int k = 0; k < N; ++k) sg[i][k] *= rstd;
+            if (p.y && at < n_vec) st_stream16(static_cast<T*>(p.y) + at_row + at * N, Vec16<T>::pack(sg[i]));
+        }
+        if (p.code == COBALT_E4M3) store_packed<CodeE4M3, N, VPT>(p, row, first, step, rstd, sg, most, row_most);
+        else store_packed<CodeI8, N, VPT>(p, row, first, step, rstd, sg, most, row_most);
     }
 }
 
@@ -432,13 +430,13 @@ static RmsShape rms_shape(int n_vec, int vpt)
 
 constexpr int kMaxSms = 256;                 // the workspace query knows no device: sized for this many
 
-// CTAs (= partial sums) of the backward kernels: about 1024 threads an SM, and eight rows each where there are that many.
+// CTAs (= partial sums) of the backward kernels: about 1024 threads an SM, and four rows each where there are that many.
 static int64_t rms_parts(int64_t T, const RmsShape& s, int sms)
 {
     const int64_t rows = s.cta ? 1 : s.threads / 32;
     int64_t ctas = (T + rows - 1) / rows, resident = 1024 / s.threads;
     resident = resident < 1 ? 1 : resident > 8 ? 8 : resident;
-    int64_t most = resident * sms, by_rows = (ctas + 7) / 8;
+    int64_t most = resident * sms, by_rows = (ctas + 3) / 4;
     if (by_rows < sms) by_rows = sms;
     if (most > by_rows) most = by_rows;
     if (ctas > most) ctas = most;
