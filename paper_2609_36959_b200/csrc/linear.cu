@@ -768,8 +768,10 @@ linear_few_rows_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict_
 }
 
 // d = dout act'(pre) in bf16 (where the products need it) and its column sums: a CTA has 128 features and a slice of the
-// tokens, 32 at a time; the sums of its sixteen token rows are added in order and written to partial [gridDim.y][N].
-constexpr int kGradPreAhead = 2;         // tokens that a thread has in flight
+// tokens, 16 at a time; the sums of its sixteen token rows are added in order and written to partial [gridDim.y][N].
+// Tokens that a thread has in flight, and CTAs an SM: more CTAs of one token each (8192 x 2816 with silu and 8-bit pre 52 us with a small
+// product behind it, two tokens and four CTAs 56).
+constexpr int kGradPreAhead = 1, kGradPreCtas = 6;
 
 struct GradPreArgs {
     const void* grad_out;
@@ -781,7 +783,7 @@ struct GradPreArgs {
     float* partial;                      // or null
 };
 
-__global__ void __launch_bounds__(256, 4)
+__global__ void __launch_bounds__(256, kGradPreCtas)
 linear_grad_pre_kernel(const GradPreArgs p)
 {
     constexpr int kAhead = kGradPreAhead;
@@ -830,8 +832,8 @@ linear_grad_pre_kernel(const GradPreArgs p)
                     float v[8];
                     if (p.pre_scales) {
                         float x[4], y[4];
-                        CodeI8::decode4(v16[a].x, x);
-                        CodeI8::decode4(v16[a].y, y);
+                        CodeI8::decode4_fp16(v16[a].x, x);
+                        CodeI8::decode4_fp16(v16[a].y, y);
 #pragma unroll
                         for (int k = 0; k < 4; ++k) v[k] = x[k] * scale[a], v[4 + k] = y[k] * scale[a];
                     } else {
@@ -930,11 +932,11 @@ static size_t part_bytes(int64_t I, int64_t J)
 
 static int64_t deep_blocks(int64_t k, int deep) { return (k + deep - 1) / deep; }
 
-// Slices of the tokens in the pass over the output's gradient: about six CTAs an SM, of as equal a number of steps as can be.
+// Slices of the tokens in the pass over the output's gradient: a CTA for every place on an SM, of as equal a number of steps as can be.
 static int bias_parts(int64_t T, int N)
 {
     const int64_t groups = (N + 127) / 128, steps = (T + 16 * kGradPreAhead - 1) / (16 * kGradPreAhead);
-    int64_t parts = (6 * 2 * kPlanPairs + groups - 1) / groups;
+    int64_t parts = (kGradPreCtas * 2 * kPlanPairs + groups - 1) / groups;
     if (parts > steps) parts = steps;
     if (parts < 1) parts = 1;
     const int64_t each = (steps + parts - 1) / parts;

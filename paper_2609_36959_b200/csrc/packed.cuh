@@ -52,6 +52,19 @@ struct CodeI8 {
 #pragma unroll
         for (int i = 0; i < 4; ++i) f[i] = static_cast<float>(static_cast<int8_t>(w >> (8 * i)));
     }
+    // The same without the conversion unit, for callers that have it busy with exponentials: code + 128 as the last byte of an fp16
+    // number from 1024 on.
+    static __device__ __forceinline__ void decode4_fp16(uint32_t w, float (&f)[4])
+    {
+        const uint32_t b = w ^ 0x80808080u, pairs[2] = {__byte_perm(b, 0x64646464u, 0x4140), __byte_perm(b, 0x64646464u, 0x4342)};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const __half2 h = __hadd2(*reinterpret_cast<const __half2*>(&pairs[i]), __half2half2(__ushort_as_half(0xE480)));      // - 1152
+            const float2 v = __half22float2(h);
+            f[2 * i] = v.x;
+            f[2 * i + 1] = v.y;
+        }
+    }
     static __device__ __forceinline__ uint32_t encode_exact(double u) { return static_cast<uint32_t>(__double2int_rn(u)) & 0xFFu; }
 };
 
