@@ -444,7 +444,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
         // ---- epilogue: two groups of four warps, each a quarter of the tensor memory lanes a warp, take 32 columns in turn ----------
         const int quarter = warp & 3, group = (warp - 2) >> 2, tid = (threadIdx.x - 64) & 127;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(32 * quarter) << 16);
-        int turn = 0;
+        int turn = 0, stored = 0;                // accumulators, and (kPlain) staging buffers of this group, used so far
         // one verdict for the eight warps: none is left alone at the barriers below
         auto accumulator = [&]() {
             ok = named_barrier_and(1, 256, barrier_wait(acc_full + 8 * (turn & 1), (turn >> 1) & 1));
@@ -582,7 +582,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int c = 64 * q + 32 * group;
-                    const uint32_t buf = staging + (2 * group + (q & 1)) * kBuffer16;
+                    const uint32_t buf = staging + (2 * group + (stored & 1)) * kBuffer16;
                     tmem_wait(r[0]);
                     tmem_wait(r[1]);
                     if (c >= columns) break;
@@ -617,6 +617,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                     fence_async_shared();
                     if (tid == 0) store_groups_read();       // the other buffer, which is written next
                     named_barrier(2 + group, 128);
+                    ++stored;                                // (a tile may have an odd number of chunks)
                     if (tid == 0 && i_cta < p.I) {
                         tma_store_2d(&map_out, buf, i_cta, w.j0 + c);
                         if (i_cta + 64 < p.I) tma_store_2d(&map_out, buf + kBox16, i_cta + 64, w.j0 + c);

@@ -135,15 +135,16 @@ __device__ __noinline__ uint32_t code_of_quotient(float v, float most)
 // The codes by the definition, for values of type T.
 //
 // A quotient of bf16 values, L m 2^e / n with m and n of eight bits, often lies on a border between codes (one value in a thousand is
-// half of its group's largest); if not, it is at least 2^-16 of itself away (a border has at most eight bits: |2 L m 2^i - b n| >= 1).
+// half of its group's largest); if not, it is at least 2^-17 of itself away (|2 L m 2^i - b n| >= 1 for a border of b, of eight bits).
 // So the product with `factor`, rounded to 18 bits (by a splitting product, after Dekker), is on the border where the quotient is, and on
 // its side of it elsewhere.  Quotients of fp32 values come as near as 2^-33: the few whose product is in doubt are done again.  So is
-// all of a group so small that `factor` overflows.
+// all of a group so small that `factor` overflows, or (fp32) so large that the reciprocal in it has lost bits.
 template <typename T, typename Code, int N>
 __device__ __forceinline__ void encode_exactly(const float (&x)[N], const GroupScale& g, uint32_t (&w)[N / 4])
 {
     constexpr bool kI8 = Code::kLargest == CodeI8::kLargest;
-    bool doubt = g.factor > 1e30f;
+    const bool all = g.factor > 1e30f || (sizeof(T) == 4 && g.most > 8e37f);
+    bool doubt = all;
     if constexpr (sizeof(T) == 2) {
         const uint32_t mask = g.factor > 0.0f ? 0xFFFFFFFFu : 0u;
         const Pair by = pair(g.factor), split = pair(65.0f), minus = pair(-1.0f);
@@ -184,7 +185,7 @@ __device__ __forceinline__ void encode_exactly(const float (&x)[N], const GroupS
     if (doubt && g.factor > 0.0f) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            if (g.factor > 1e30f || (kI8 ? near_border_i8(x[i], g.factor) : near_border_e4m3(x[i] * g.factor))) {
+            if (all || (kI8 ? near_border_i8(x[i], g.factor) : near_border_e4m3(x[i] * g.factor))) {
                 const int shift = 8 * (i % 4);
                 w[i / 4] = (w[i / 4] & ~(0xFFu << shift)) | (code_of_quotient<Code>(x[i], g.most) << shift);
             }

@@ -189,7 +189,7 @@ class MoELayer:
 
     def restore(self, checkpoint: LayerCheckpoint) -> None:
         """Computes again what backward needs, with the routing as it was and the rows as they were kept.  backward then gives the
-        gradients at those rows; the checkpoint is read by it and must stay as it is."""
+        gradients at those rows; the checkpoint is read by it and must stay as it is.  step.src_rank is the checkpoint's afterwards."""
         s, c = self.step, checkpoint
         if tuple(c.rows[0].shape) != (self.T, self.H) or c.logits.shape != self.logits.shape or c.topk_ids.shape != s.topk_ids.shape:
             raise cb.CobaltError(cb.ERR_INVALID_ARG, "MoELayer.restore (sizes)")

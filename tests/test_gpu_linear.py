@@ -155,6 +155,20 @@ def test_linear_gradient_of_many_rows_from_a_few_features(T, K, N):
         assert ((gx[part].double() - ref).abs() <= size + D.HALF[BF16] * (ref.abs() + size)).all()
 
 
+@pytest.mark.parametrize("T,K,N", [(1457, 8192, 264), (449, 16384, 520), (2400, 6400, 136)])
+def test_linear_tiles_with_an_odd_number_of_chunks(T, K, N):
+    """Last tiles of 177, 193 and 96 rows: a group of warps stores an odd number of chunks, and the pair's next tile follows at once."""
+    import paper_2609_36959_b200 as cb
+    _, w, _, _, dy = _inputs(T, K, N, 3)
+    ref = dy.double() @ w.double()
+    size = 2 * (N + 4) * U * (dy.double().abs() @ w.double().abs()) + D.HALF[BF16] * ref.abs() * 1.001
+    gx, ws = torch.empty((T, K), dtype=BF16, device="cuda"), _workspace(T, K, N)
+    for _ in range(10):
+        gx.fill_(5.0)
+        cb.linear_backward(dy, None, w, ws, grad_x=gx)
+        assert ((gx.double() - ref).abs() <= size).all()
+
+
 def test_linear_rows_keep_to_themselves():
     """A row of x with a NaN or an infinity reaches its own row of the result only; one of W its own column."""
     import paper_2609_36959_b200 as cb

@@ -149,6 +149,21 @@ def test_dense_block_in_8_bits():
             m.backward(x)
 
 
+def test_layer_without_tokens():
+    import paper_2609_36959_b200 as cb
+    w = W.make_custom(0, 8, 2, 64, 2, 2, 3, seed=3, C=2)
+    m, x, r, dy = _layer(w, 40, 136, norm="rms", router="linear")
+    for t in (m.grad_w_shared_up, m.grad_b_shared_down, m.grad_w_router, m.grad_gamma):
+        t.fill_(3.0)
+    out = m.forward(x, 1, residual=r)
+    m.restore(m.save())
+    assert out.shape == m.backward(dy).shape == (0, 64)
+    torch.cuda.synchronize()
+    assert cb.read_and_clear_device_error() == 0
+    for t in (m.grad_w_shared_up, m.grad_b_shared_down, m.grad_w_router, m.grad_gamma):
+        assert (t == 0).all()
+
+
 def test_layer_refusals():
     import paper_2609_36959_b200 as cb
     w = W.make_custom(8, 8, 2, 64, 2, 2, 3, seed=3, C=2)

@@ -84,6 +84,7 @@ def test_pack_extremes(code, group):
     x[6] *= 1e37
     x[7] = 0
     x[8] = -0.0
+    x[10] *= 6e37                                                     # a reciprocal below the normal range
     x[9] *= 2.0 ** -60
     x[9, 0] = 1.0                                                     # everything else in its group far below a step
     _check(x, code, group, _pack(x, code, group))
