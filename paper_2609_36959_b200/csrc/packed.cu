@@ -5,6 +5,7 @@
 //           With one scale a row a warp or a CTA holds the row in registers between its largest value and the codes.
 //   unpack  the same walk without the reduction.
 //
+// Bound by HBM: 32768 x 7168 bf16 with a scale for 128 columns 132 us (5.3 TB/s), with one a row 118 us, read back 109 us (6.5 TB/s).
 // Rows whose width is no multiple of such a piece, or pointers off a 32-byte boundary, take eight columns a piece.
 #include "packed.cuh"
 
