@@ -482,7 +482,8 @@ int cobalt_rms_norm_backward(const void* grad_y, const void* grad_sum, const voi
  * be grad_out where that is bf16); d is rounded to bf16 once.  pre is not read without an activation.  The residual's gradient is
  * grad_out itself.  Each of the three results may be NULL, but not all.  Products and sums are fp32.
  * K and N multiples of 8 (e4m3: K of 16), at most COBALT_LINEAR_MAX_WIDTH; T <= 2^31 - 2^21; T = 0 is allowed (gradients
- * of w and bias are then 0).  out may be residual.  Results do not vary from run to run. */
+ * of w and bias are then 0).  out may be residual.  A workspace of the size for T serves any smaller T, both calls, and
+ * grad_bias alone whatever K.  Results do not vary from run to run. */
 #define COBALT_ACT_NONE 0
 #define COBALT_ACT_RELU 1
 #define COBALT_ACT_SILU 2

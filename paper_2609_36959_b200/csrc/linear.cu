@@ -929,11 +929,11 @@ static LinearPlan linear_plan(int64_t I, int64_t J, int64_t blocks)
     return best;
 }
 
-// At least what the plan's parts take.
+// At least what the plan's parts take, for J of j or fewer: k is split where there are fewer than 2 kPlanPairs tiles.
 static size_t part_bytes(int64_t I, int64_t J)
 {
-    const int64_t tiles = ((I + kTileM - 1) / kTileM) * ((J + kTileN - 1) / kTileN);
-    if (tiles >= 2 * kPlanPairs) return 0;
+    const int64_t most_j = (2 * kPlanPairs - 1) / ((I + kTileM - 1) / kTileM) * kTileN;
+    if (J > most_j) J = most_j;
     const int64_t by_splits = kMostSplits * I * J, by_tiles = static_cast<int64_t>(kMostParts) * kTileM * kTileN;
     return static_cast<size_t>(by_splits < by_tiles ? by_splits : by_tiles) * sizeof(float);
 }
@@ -959,10 +959,19 @@ static int check_linear(int64_t T, int32_t K, int32_t N, int deep_unit)
     return COBALT_OK;
 }
 
+// The sums of the bias's gradient, for T tokens or fewer.
+static size_t bias_bytes(int64_t T, int32_t N)
+{
+    const int64_t groups = (N + 127) / 128, steps = (T + 16 * kGradPreAhead - 1) / (16 * kGradPreAhead);
+    const int64_t most = (kGradPreCtas * 2 * kPlanPairs + groups - 1) / groups;
+    return static_cast<size_t>(steps < most ? steps : most) * N * sizeof(float);
+}
+
+// Never less than for fewer tokens.
 static size_t linear_workspace(int64_t T, int32_t K, int32_t N)
 {
     if (T == 0) return 256;
-    size_t most = static_cast<size_t>(bias_parts(T, N)) * N * sizeof(float);
+    size_t most = bias_bytes(T, N);
     const size_t all[3] = {part_bytes(N, T), part_bytes(K, T), part_bytes(K, N)};
     for (size_t b : all) most = b > most ? b : most;
     return round_up(most > 0 ? most : 1, 256);
@@ -1103,7 +1112,8 @@ int cobalt_linear_backward(const void* grad_out, const void* x, const void* w, c
     if (!aligned16(grad_out) || !aligned16(x) || !aligned16(w) || !aligned16(pre) || !aligned16(pre_scales) || !aligned16(grad_pre) ||
         !aligned16(grad_x) || !aligned16(grad_w) || !aligned16(grad_bias) || !aligned16(workspace))
         return COBALT_ERR_INVALID_ARG;
-    if (!workspace || workspace_bytes < linear_workspace(T, K, N)) return COBALT_ERR_WORKSPACE_TOO_SMALL;
+    // (for the bias alone K is not known to a caller without x and w)
+    if (!workspace || workspace_bytes < (products ? linear_workspace(T, K, N) : bias_bytes(T, N))) return COBALT_ERR_WORKSPACE_TOO_SMALL;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (T == 0) {                                // no rows: the weights' gradients are 0
         if (grad_w) COBALT_CUDA_TRY(cudaMemsetAsync(grad_w, 0, static_cast<size_t>(N) * K * sizeof(bf16), s));

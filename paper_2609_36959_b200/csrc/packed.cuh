@@ -74,7 +74,7 @@ __device__ __forceinline__ uint32_t abs_max(uint32_t most, float v) { return max
 
 // What a group's codes and scale follow from.
 struct GroupScale {
-    float most, factor, scale;               // factor: L / most to 2^-22, 0 where every code is 0
+    float most, factor, scale;               // factor: L / most to 2^-22, 0 where every code is 0, infinity below 2^-119
     template <typename Code>
     static __device__ __forceinline__ GroupScale of(uint32_t most_bits)
     {
@@ -107,10 +107,21 @@ __device__ __forceinline__ bool near_border_e4m3(float t)
 }
 
 // The codes of N values, four a word, from their products with `factor`, whichever way a value at a border goes.  (A group without a
-// factor may hold infinities; its codes are cleared at the end.)
+// factor may hold infinities; its codes are cleared at the end.)  Of groups so small that the factor would be past the range, 2^100 times
+// the values are coded.
 template <typename Code, int N>
-__device__ __forceinline__ void encode_fast(const float (&x)[N], const GroupScale& g, uint32_t (&w)[N / 4])
+__device__ __forceinline__ void encode_fast(const float (&values)[N], const GroupScale& group, uint32_t (&w)[N / 4])
 {
+    GroupScale g = group;
+    float x[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = values[i];
+    if (g.factor > 1e30f) {
+        constexpr float kLift = 1.267650600e+30f;
+        g = GroupScale::of<Code>(abs_bits(g.most * kLift));
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] *= kLift;
+    }
     const uint32_t mask = g.factor > 0.0f ? 0xFFFFFFFFu : 0u;
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) {

@@ -125,6 +125,15 @@ def test_workspace_covers_the_plan_everywhere(cb):
         assert call == cb.ERR_WORKSPACE_TOO_SMALL and size >= 256
 
 
+def test_a_workspace_for_many_tokens_serves_fewer(cb):
+    sizes = [1, 2, 5, 64, 300, 801, 4099, 9473, 75776, 131072, 1 << 20]
+    for K, N in ((8, 8), (4096, 2816), (7168, 256), (65536, 65536), (200, 1000), (40000, 8)):
+        for query in (lambda t: cb.linear_workspace_bytes(t, K, N), lambda t: cb.rms_norm_workspace_bytes(t, min(K, 16384))):
+            got = [query(t) for t in sizes + list(range(1, 4000, 17))]
+            by_size = [b for _, b in sorted(zip(sizes + list(range(1, 4000, 17)), got))]
+            assert by_size == sorted(by_size)
+
+
 def test_binding_refuses_wrong_shapes_and_host_tensors(cb):
     z, f8 = torch.zeros, torch.float8_e4m3fn
     with pytest.raises(TypeError):

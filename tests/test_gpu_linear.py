@@ -233,3 +233,32 @@ def test_linear_captured_with_two_streams():
         step(x, w, bias, residual, dy, b)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b[k]) for a, k in zip(got, ("out", "gx", "gw", "gb")))
+
+
+def test_linear_smallest_pre_activations_in_8_bits():
+    """Pre-activations so small that 127 / most is past the range, zeros among them: the bias alone, as x is 0, so that pre is exact.  The
+    scale, below 2^-126, is good to 2^-150."""
+    import paper_2609_36959_b200 as cb
+    T, K, N = 40, 64, 264
+    g = torch.Generator(device="cuda").manual_seed(1)
+    bias = (torch.randint(-9, 10, (N,), generator=g, device="cuda").double() * 2.0 ** -129).to(BF16)
+    pre = torch.full((T, N), 7, dtype=torch.int8, device="cuda"), torch.full((T, 3), 7.0, device="cuda")
+    out = torch.empty((T, N), dtype=BF16, device="cuda")
+    cb.linear(torch.zeros((T, K), dtype=BF16, device="cuda"), torch.ones((N, K), dtype=BF16, device="cuda"), out, _workspace(T, K, N), bias=bias,
+              act="silu", pre=pre)
+    ref = bias.double().expand(T, N)
+    step = D.values(torch.ones_like(ref), pre[1], 128)
+    assert ((D.values(pre[0], pre[1], 128) - ref).abs() <= 0.5 * step * (1 + 64 * U) + 127 * 2.0 ** -150).all()
+
+
+def test_linear_bias_gradient_alone_takes_the_workspace_of_the_whole_call():
+    """Neither x nor w is given then, so that the call does not know the rows' width; and a workspace for many tokens serves fewer."""
+    import paper_2609_36959_b200 as cb
+    T, K, N = 8192, 4096, 2816
+    ws = _workspace(T, K, N)
+    for t in (T, 801, 300, 1):
+        dy = torch.randn((t, N), generator=torch.Generator(device="cuda").manual_seed(t), device="cuda").to(BF16)
+        got = torch.empty(N, dtype=BF16, device="cuda")
+        cb.linear_backward(dy, None, None, ws, grad_bias=got)
+        ref = dy.double().sum(0)
+        assert ((got.double() - ref).abs() <= t * U * dy.double().abs().sum(0) + D.HALF[BF16] * ref.abs() * 1.001).all()

@@ -166,3 +166,21 @@ def test_rms_norm_no_rows():
     cb.rms_norm_backward(x, x, torch.ones(64, device="cuda"), rstd, x, dg, ws)
     torch.cuda.synchronize()
     assert (dg == 0).all()
+
+
+@pytest.mark.parametrize("code", [torch.int8, torch.float8_e4m3fn], ids=["i8", "e4m3"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_rms_norm_in_8_bits_of_the_smallest_values(dtype, code):
+    """Rows so small that L / most is past the range, zeros among them.  x is a multiple of 2^-133 and gamma 1, so that s gamma is exact;
+    y is good to 26 u, a code's product to 4 u more, and the scale, below 2^-126, to 2^-150: 448 2^-150 of a value."""
+    import paper_2609_36959_b200 as cb
+    for H, group in ((264, 128), (264, 0), (4096, 128), (4096, 0)):
+        g = torch.Generator(device="cuda").manual_seed(H)
+        x = (torch.randint(-9, 10, (5, H), generator=g, device="cuda").double() * 2.0 ** -133).to(dtype)
+        x[0, 1:] = 0
+        q, scales = torch.empty(x.shape, dtype=code, device="cuda"), torch.empty((5, len(D.groups_of(H, group))), device="cuda")
+        cb.rms_norm(x, torch.ones(H, device="cuda"), 1e-5, packed=(q, scales))
+        ref, _ = D.rms_forward(x, torch.ones(H, device="cuda"), 1e-5)
+        got, step = D.values(q, scales, group), D.values(torch.ones_like(ref), scales, group)
+        half = 0.5 * step if code == torch.int8 else torch.maximum(2.0 ** -4 * ref.abs(), 2.0 ** -10 * step)
+        assert ((got - ref).abs() <= half * (1 + 64 * U) + 64 * U * ref.abs() + 448 * 2.0 ** -150).all()
