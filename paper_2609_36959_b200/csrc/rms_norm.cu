@@ -23,22 +23,16 @@ namespace cobalt {
 constexpr int kRmsMaxH = 16384;
 constexpr int kRmsWarpVecs = 128;            // 16-byte vectors of a row up to which one warp takes it
 
-// Each v's sum over the CTA (kCta; `scratch` is not still read after an earlier call) or the warp, for every thread.
-template <bool kCta, int R>
-__device__ __forceinline__ void row_sums(float (&v)[R], float (&scratch)[R][32])
+// The sum over the CTA (kCta; `scratch` is not still read after an earlier call) or the warp, for every thread.
+template <bool kCta>
+__device__ __forceinline__ float row_sum(float v, float (&scratch)[32])
 {
-#pragma unroll
-    for (int r = 0; r < R; ++r) v[r] = warp_sum(v[r]);
-    if (kCta) {
-        const int lane = threadIdx.x & 31;
-        if (lane == 0) {
-#pragma unroll
-            for (int r = 0; r < R; ++r) scratch[r][threadIdx.x >> 5] = v[r];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int r = 0; r < R; ++r) v[r] = warp_sum(lane < (blockDim.x >> 5) ? scratch[r][lane] : 0.0f);
-    }
+    v = warp_sum(v);
+    if (!kCta) return v;
+    const int lane = threadIdx.x & 31;
+    if (lane == 0) scratch[threadIdx.x >> 5] = v;
+    __syncthreads();
+    return warp_sum(lane < (blockDim.x >> 5) ? scratch[lane] : 0.0f);
 }
 
 // N neighbouring values of gamma.  `wide` (a 32-byte boundary): one load of 32 bytes a lane for bf16 rows; two of 16 touch every line
@@ -111,7 +105,7 @@ __global__ void __launch_bounds__(kRmsThreads<T, VPT, kCta>, !kCta ? 4 : VPT == 
 rms_norm_kernel(const RmsForward p)
 {
     constexpr int N = Vec16<T>::kElems;
-    __shared__ float scratch[1][32];
+    __shared__ float scratch[32];
     __shared__ uint32_t scratch_max[32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_vec = p.H / N;
     const int first = kCta ? threadIdx.x : lane, step = kCta ? blockDim.x : 32;
@@ -146,14 +140,14 @@ rms_norm_kernel(const RmsForward p)
             if (p.sum && at < n_vec) st_stream16(static_cast<T*>(p.sum) + at_row + at * N, v[i]);
         }
     }
-    float squares[1] = {0.0f}, sg[kPacked ? VPT : 1][N];
+    float squares = 0.0f, sg[kPacked ? VPT : 1][N];
     uint32_t most[kPacked ? VPT : 1], row_most = 0;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
         float f[N];
         Vec16<T>::unpack(v[i], f);
 #pragma unroll
-        for (int k = 0; k < N; ++k) squares[0] = fmaf(f[k], f[k], squares[0]);
+        for (int k = 0; k < N; ++k) squares = fmaf(f[k], f[k], squares);
         if constexpr (kPacked) {             // the largest |s gamma| too: times rstd it is the largest |y|, and one barrier serves both
             const int at = first + i * step;
             float g[N] = {};
@@ -171,8 +165,8 @@ rms_norm_kernel(const RmsForward p)
         row_most = __reduce_max_sync(0xFFFFFFFFu, row_most);
         if (kCta && lane == 0) scratch_max[warp] = row_most;
     }
-    row_sums<kCta, 1>(squares, scratch);
-    const float rstd = rsqrtf(squares[0] / static_cast<float>(p.H) + p.eps);
+    squares = row_sum<kCta>(squares, scratch);
+    const float rstd = rsqrtf(squares / static_cast<float>(p.H) + p.eps);
     if (p.rstd && first == 0) p.rstd[row] = rstd;
 
     if constexpr (!kPacked) {
@@ -272,14 +266,47 @@ struct SavedRows<T, void> {
     }
 };
 
-// Persistent CTAs; a thread has the same columns of every row, whose gradients of gamma stay in its registers.  R rows at a time share
-// the wait for their loads and a barrier.
-template <typename T, typename Code, int VPT, bool kCta, bool kSum, int R>
+// What a thread has of a row.
+template <typename T, typename Code, int VPT, bool kSum>
+struct BackwardRow {
+    static constexpr int N = Vec16<T>::kElems;
+    uint4 dy[VPT], ds[kSum ? VPT : 1];
+    SavedRows<T, Code> s[VPT];
+    float rstd;
+    __device__ __forceinline__ void load(const RmsBackward& p, int64_t row, int first, int step, int n_vec)
+    {
+        const bool here = row < p.rows;
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            const int at = first + i * step;
+            dy[i] = make_uint4(0, 0, 0, 0);
+            s[i].clear();
+            if (here && at < n_vec) {
+                dy[i] = ld_once16(static_cast<const T*>(p.grad_y) + row * p.H + at * N);
+                s[i].load(p, row, at);
+            }
+        }
+        rstd = here ? __ldg(p.rstd + row) : 0.0f;
+    }
+    __device__ __forceinline__ void load_sum(const RmsBackward& p, int64_t row, int first, int step, int n_vec)
+    {
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            const int at = first + i * step;
+            ds[kSum ? i : 0] = make_uint4(0, 0, 0, 0);
+            if (row < p.rows && at < n_vec) ds[kSum ? i : 0] = ld_once16(static_cast<const T*>(p.grad_sum) + row * p.H + at * N);
+        }
+    }
+};
+
+// Persistent CTAs; a thread has the same columns of every row, whose gradients of gamma stay in its registers.  kAhead: the next
+// row's loads (the second gradient's own at the row's start: it is needed last) are under way while one is computed.
+template <typename T, typename Code, int VPT, bool kCta, bool kSum, bool kAhead>
 __global__ void __launch_bounds__(kRmsThreads<T, VPT, kCta>, kCta ? (VPT == 2 ? 2 : 1) : 2)
 rms_norm_backward_kernel(const RmsBackward p)
 {
     constexpr int N = Vec16<T>::kElems;
-    __shared__ float scratch[2][R][32];
+    __shared__ float scratch[2][32];
     extern __shared__ float warp_sums[];     // [H], one warp a row only
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_vec = p.H / N;
     const int first = kCta ? threadIdx.x : lane, step = kCta ? blockDim.x : 32;
@@ -292,70 +319,47 @@ rms_norm_backward_kernel(const RmsBackward p)
     for (int i = 0; i < VPT; ++i)
 #pragma unroll
         for (int k = 0; k < N / 2; ++k) acc[i][k] = pair(0.0f);
-    for (int turn = 0; row < p.rows; row += R * rows_step, turn ^= 1) {
-        uint4 dy[R][VPT], ds[R][VPT];
-        SavedRows<T, Code> s[R][VPT];
-        float rstd[R], mean[R];
+    BackwardRow<T, Code, VPT, kSum> in, ahead;
+    if (kAhead) ahead.load(p, row, first, step, n_vec);
+    for (int turn = 0; row < p.rows; row += rows_step, turn ^= 1) {
+        if (kAhead) in = ahead;
+        else in.load(p, row, first, step, n_vec);
+        if (kSum) in.load_sum(p, row, first, step, n_vec);
+        if (kAhead) ahead.load(p, row + rows_step, first, step, n_vec);
+        Pair dot = pair(0.0f);
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int64_t own = row + r * rows_step;
-            const bool here = own < p.rows;
+        for (int i = 0; i < VPT; ++i) {
+            const int at = first + i * step;
+            if (at >= n_vec) continue;
+            float gm[N];
+            Pair z[N / 2], d[N / 2];
+            load_gamma<N>(p.gamma + at * N, p.wide, gm);
+            in.s[i].values(in.rstd, z);
+            unpack_pairs<T>(in.dy[i], d);
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) {
-                const int at = first + i * step;
-                dy[r][i] = ds[r][i] = make_uint4(0, 0, 0, 0);
-                s[r][i].clear();
-                if (here && at < n_vec) {
-                    dy[r][i] = ld_once16(static_cast<const T*>(p.grad_y) + own * p.H + at * N);
-                    s[r][i].load(p, own, at);
-                    if (kSum) ds[r][i] = ld_once16(static_cast<const T*>(p.grad_sum) + own * p.H + at * N);
-                }
+            for (int k = 0; k < N / 2; ++k) {
+                const Pair dz = d[k] * z[k];
+                acc[i][k] = acc[i][k] + dz;
+                dot = fma2(dz, pair(gm[2 * k], gm[2 * k + 1]), dot);
             }
-            rstd[r] = here ? __ldg(p.rstd + own) : 0.0f;
         }
+        const float minus_mean = -row_sum<kCta>(dot.v.x + dot.v.y, scratch[turn]) * inv_h;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            Pair dot = pair(0.0f);
+        for (int i = 0; i < VPT; ++i) {
+            const int at = first + i * step;
+            if (at >= n_vec) continue;
+            float gm[N];
+            Pair z[N / 2], d[N / 2], e[N / 2];
+            load_gamma<N>(p.gamma + at * N, p.wide, gm);
+            in.s[i].values(in.rstd, z);
+            unpack_pairs<T>(in.dy[i], d);
+            if (kSum) unpack_pairs<T>(in.ds[kSum ? i : 0], e);
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) {
-                const int at = first + i * step;
-                if (at >= n_vec) continue;
-                float gm[N];
-                Pair z[N / 2], d[N / 2];
-                load_gamma<N>(p.gamma + at * N, p.wide, gm);
-                s[r][i].values(rstd[r], z);
-                unpack_pairs<T>(dy[r][i], d);
-#pragma unroll
-                for (int k = 0; k < N / 2; ++k) {
-                    const Pair dz = d[k] * z[k];
-                    acc[i][k] = acc[i][k] + dz;
-                    dot = fma2(dz, pair(gm[2 * k], gm[2 * k + 1]), dot);
-                }
+            for (int k = 0; k < N / 2; ++k) {
+                const Pair v = fma2(pair(minus_mean), z[k], d[k] * pair(gm[2 * k], gm[2 * k + 1]));
+                d[k] = kSum ? fma2(pair(in.rstd), v, e[k]) : pair(in.rstd) * v;
             }
-            mean[r] = dot.v.x + dot.v.y;
-        }
-        row_sums<kCta, R>(mean, scratch[turn]);
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int64_t own = row + r * rows_step;
-            const float minus_mean = -mean[r] * inv_h;
-#pragma unroll
-            for (int i = 0; i < VPT; ++i) {
-                const int at = first + i * step;
-                if (at >= n_vec || own >= p.rows) continue;
-                float gm[N];
-                Pair z[N / 2], d[N / 2], e[N / 2];
-                load_gamma<N>(p.gamma + at * N, p.wide, gm);
-                s[r][i].values(rstd[r], z);
-                unpack_pairs<T>(dy[r][i], d);
-                if (kSum) unpack_pairs<T>(ds[r][i], e);
-#pragma unroll
-                for (int k = 0; k < N / 2; ++k) {
-                    const Pair v = fma2(pair(minus_mean), z[k], d[k] * pair(gm[2 * k], gm[2 * k + 1]));
-                    d[k] = kSum ? fma2(pair(rstd[r]), v, e[k]) : pair(rstd[r]) * v;
-                }
-                st_stream16(static_cast<T*>(p.grad_x) + own * p.H + at * N, pack_pairs<T>(d));
-            }
+            st_stream16(static_cast<T*>(p.grad_x) + row * p.H + at * N, pack_pairs<T>(d));
         }
     }
     float* out = p.partial + static_cast<int64_t>(blockIdx.x) * p.H;
@@ -478,16 +482,20 @@ static int launch_backward(const RmsBackward& p, int sms, int* parts, cudaStream
 {
     const RmsShape shape = rms_shape(p.H / Vec16<T>::kElems, 2);
     *parts = static_cast<int>(rms_parts(p.rows, shape, sms < kMaxSms ? sms : kMaxSms));
-    // two rows at a time where their registers fit (rows as they are, no second gradient: 235 us against 260 at 32768 x 7168 bf16)
-    constexpr int kRows = !kSum && std::is_void<Code>::value ? 2 : 1;
+    // The next row's loads ahead (32768 x 7168 bf16, us, with / without): rows as they are 224 / 260 without a second gradient, 312 / 304 with
+    // one (registers spill); rows in 8 bits 262 / 304 with one; 222 / 267 without, but 160 / 142 at 32768 x 4096 and 197 / 186 at 5120, where
+    // three or more CTAs an SM cover for one another.
+    constexpr bool kPlain = std::is_void<Code>::value, kAhead = !(kPlain && kSum);
     const size_t smem = shape.cta ? 0 : sizeof(float) * p.H;
     if (shape.cta) {
-        if (shape.vpt == 2) rms_norm_backward_kernel<T, Code, 2, true, kSum, kRows><<<*parts, shape.threads, smem, s>>>(p);
-        else rms_norm_backward_kernel<T, Code, 4, true, kSum, 1><<<*parts, shape.threads, smem, s>>>(p);
+        if (shape.vpt == 4) rms_norm_backward_kernel<T, Code, 4, true, kSum, false><<<*parts, shape.threads, smem, s>>>(p);
+        else if (kAhead && (kPlain || kSum || 1024 / shape.threads < 3))
+            rms_norm_backward_kernel<T, Code, 2, true, kSum, kAhead><<<*parts, shape.threads, smem, s>>>(p);
+        else rms_norm_backward_kernel<T, Code, 2, true, kSum, false><<<*parts, shape.threads, smem, s>>>(p);
     } else {
-        if (shape.vpt == 1) rms_norm_backward_kernel<T, Code, 1, false, kSum, 1><<<*parts, shape.threads, smem, s>>>(p);
-        else if (shape.vpt == 2) rms_norm_backward_kernel<T, Code, 2, false, kSum, 1><<<*parts, shape.threads, smem, s>>>(p);
-        else rms_norm_backward_kernel<T, Code, 4, false, kSum, 1><<<*parts, shape.threads, smem, s>>>(p);
+        if (shape.vpt == 1) rms_norm_backward_kernel<T, Code, 1, false, kSum, false><<<*parts, shape.threads, smem, s>>>(p);
+        else if (shape.vpt == 2) rms_norm_backward_kernel<T, Code, 2, false, kSum, false><<<*parts, shape.threads, smem, s>>>(p);
+        else rms_norm_backward_kernel<T, Code, 4, false, kSum, false><<<*parts, shape.threads, smem, s>>>(p);
     }
     return COBALT_OK;
 }
