@@ -11,8 +11,9 @@
 // way on an SM; with 8-bit rows the largest |s gamma| is found beside the sum of squares.  Bound by HBM: 32768 x 7168 bf16 with
 // residual 276 us (6.8 TB/s), with e4m3 rows 258 us (6.4 TB/s).  Backward: persistent CTAs, because the gradients of gamma of a thread's
 // columns stay in its registers (one partial sum a CTA and column, added in order by a second kernel).  Those registers leave 28 warps
-// an SM; with ds, 8 bytes a value, that is enough (304 us, 6.2 TB/s), from int8 rows, 5 bytes, latency and instructions show (261 us,
-// 4.5 TB/s).  A ring of bulk copies ahead of the rows was slower (355 and 351 us), since it does not shorten what a row takes.
+// an SM, so the next row's loads are under way while one is computed: with ds, 8 bytes a value, 303 us (6.2 TB/s, without loads ahead: two
+// rows' worth spills), from int8 rows, 5 bytes, 221 us (5.3 TB/s; 267 without loads ahead), with ds 261 us (6.3 TB/s).  A ring of bulk
+// copies ahead of the rows was slower (355 and 351 us): reading it back costs instructions, which the row's two passes are short of.
 #include <type_traits>
 
 #include "packed.cuh"
@@ -301,8 +302,8 @@ struct BackwardRow {
 
 // Persistent CTAs; a thread has the same columns of every row, whose gradients of gamma stay in its registers.  kAhead: the next
 // row's loads (the second gradient's own at the row's start: it is needed last) are under way while one is computed.
-template <typename T, typename Code, int VPT, bool kCta, bool kSum, bool kAhead>
-__global__ void __launch_bounds__(kRmsThreads<T, VPT, kCta>, kCta ? (VPT == 2 ? 2 : 1) : 2)
+template <typename T, typename Code, int VPT, bool kCta, bool kSum, bool kAhead, int kThreads>
+__global__ void __launch_bounds__(kThreads, !kCta && VPT == 1 ? 4 : kThreads <= 448 ? 2 : 1)
 rms_norm_backward_kernel(const RmsBackward p)
 {
     constexpr int N = Vec16<T>::kElems;
@@ -416,35 +417,41 @@ rms_norm_reduce_kernel(const float* partial, int parts, int H, float* __restrict
 struct RmsShape {
     int vpt, threads;
     bool cta;
+    int resident;                            // CTAs of the backward kernels that fit on an SM
 };
 
 // Up to this many rows the forward pass takes two vectors a thread: more threads for a row, which is all the latency there is.
 constexpr int64_t kFewRows = 148;
 
-// A warp a row up to 128 vectors; above, a CTA a row with `vpt` vectors a thread.
-static RmsShape rms_shape(int n_vec, int vpt)
+// A warp a row up to 128 vectors; above, a CTA a row with `vpt` vectors a thread, four of rows of more than `most`.  elems: values of a
+// vector.
+static RmsShape rms_shape(int H, int elems, int vpt, int most)
 {
+    const int n_vec = H / elems;
     RmsShape s = {};
     s.cta = n_vec > kRmsWarpVecs;
     if (!s.cta) {
         s.threads = 256;
         s.vpt = n_vec <= 32 ? 1 : n_vec <= 64 ? 2 : 4;
     } else {
-        s.vpt = n_vec <= 896 ? vpt : 4;
+        s.vpt = n_vec <= most ? vpt : 4;
         s.threads = ((n_vec + s.vpt - 1) / s.vpt + 31) / 32 * 32;
     }
+    // by the registers that the launch bounds leave a thread: a CTA too many would wait for a whole one (32768 x 4096 bf16 with a second
+    // gradient, where three fit: 181 us, with four 234)
+    const int registers = s.cta ? (s.threads <= 448 && s.vpt == 2 ? 72 : 64) : s.vpt == 1 ? 64 : 128;
+    s.resident = 65536 / (registers * s.threads);
+    if (s.resident > 8) s.resident = 8;
     return s;
 }
 
 constexpr int kMaxSms = 256;                 // the workspace query knows no device: sized for this many
 
-// CTAs (= partial sums) of the backward kernels: about 1024 threads an SM, and four rows each where there are that many.
+// CTAs (= partial sums) of the backward kernels: as many as fit, and four rows each where there are that many.
 static int64_t rms_parts(int64_t T, const RmsShape& s, int sms)
 {
     const int64_t rows = s.cta ? 1 : s.threads / 32;
-    int64_t ctas = (T + rows - 1) / rows, resident = 1024 / s.threads;
-    resident = resident < 1 ? 1 : resident > 8 ? 8 : resident;
-    int64_t most = resident * sms, by_rows = (ctas + 3) / 4;
+    int64_t ctas = (T + rows - 1) / rows, most = static_cast<int64_t>(s.resident) * sms, by_rows = (ctas + 3) / 4;
     if (by_rows < sms) by_rows = sms;
     if (most > by_rows) most = by_rows;
     if (ctas > most) ctas = most;
@@ -463,7 +470,7 @@ static bool check_code(int32_t code, int32_t group) { return (code == COBALT_E4M
 template <typename T, bool kPacked>
 static void launch_forward(const RmsForward& p, cudaStream_t s)
 {
-    const RmsShape shape = rms_shape(p.H / Vec16<T>::kElems, p.rows <= kFewRows ? 2 : 4);
+    const RmsShape shape = rms_shape(p.H, Vec16<T>::kElems, p.rows <= kFewRows ? 2 : 4, 896);
     const int64_t per_cta = shape.cta ? 1 : shape.threads / 32, ctas = (p.rows + per_cta - 1) / per_cta;
     const unsigned grid = static_cast<unsigned>(ctas);
     if (shape.cta) {
@@ -480,22 +487,20 @@ static void launch_forward(const RmsForward& p, cudaStream_t s)
 template <typename T, typename Code, bool kSum>
 static int launch_backward(const RmsBackward& p, int sms, int* parts, cudaStream_t s)
 {
-    const RmsShape shape = rms_shape(p.H / Vec16<T>::kElems, 2);
+    const RmsShape shape = rms_shape(p.H, Vec16<T>::kElems, 2, 2048);
     *parts = static_cast<int>(rms_parts(p.rows, shape, sms < kMaxSms ? sms : kMaxSms));
-    // The next row's loads ahead (32768 x 7168 bf16, us, with / without): rows as they are 224 / 260 without a second gradient, 312 / 304 with
-    // one (registers spill); rows in 8 bits 262 / 304 with one; 222 / 267 without, but 160 / 142 at 32768 x 4096 and 197 / 186 at 5120, where
-    // three or more CTAs an SM cover for one another.
-    constexpr bool kPlain = std::is_void<Code>::value, kAhead = !(kPlain && kSum);
+    // The next row's loads ahead, but where their registers spill (32768 x 7168 bf16, us, with / without: rows as they are 224 / 260 without a
+    // second gradient, 312 / 304 with one; rows in 8 bits 221 / 267 and 261 / 304; 32768 x 8192: 281 / 287, 337 / 338, 250 / 324, 375 / 331).
+    constexpr bool kPlain = std::is_void<Code>::value;
     const size_t smem = shape.cta ? 0 : sizeof(float) * p.H;
     if (shape.cta) {
-        if (shape.vpt == 4) rms_norm_backward_kernel<T, Code, 4, true, kSum, false><<<*parts, shape.threads, smem, s>>>(p);
-        else if (kAhead && (kPlain || kSum || 1024 / shape.threads < 3))
-            rms_norm_backward_kernel<T, Code, 2, true, kSum, kAhead><<<*parts, shape.threads, smem, s>>>(p);
-        else rms_norm_backward_kernel<T, Code, 2, true, kSum, false><<<*parts, shape.threads, smem, s>>>(p);
+        if (sizeof(T) == 4 && shape.vpt == 4) rms_norm_backward_kernel<float, Code, 4, true, kSum, false, 1024><<<*parts, shape.threads, smem, s>>>(p);
+        else if (shape.threads <= 448) rms_norm_backward_kernel<T, Code, 2, true, kSum, !(kPlain && kSum), 448><<<*parts, shape.threads, smem, s>>>(p);
+        else rms_norm_backward_kernel<T, Code, 2, true, kSum, !kSum, 1024><<<*parts, shape.threads, smem, s>>>(p);
     } else {
-        if (shape.vpt == 1) rms_norm_backward_kernel<T, Code, 1, false, kSum, false><<<*parts, shape.threads, smem, s>>>(p);
-        else if (shape.vpt == 2) rms_norm_backward_kernel<T, Code, 2, false, kSum, false><<<*parts, shape.threads, smem, s>>>(p);
-        else rms_norm_backward_kernel<T, Code, 4, false, kSum, false><<<*parts, shape.threads, smem, s>>>(p);
+        if (shape.vpt == 1) rms_norm_backward_kernel<T, Code, 1, false, kSum, false, 256><<<*parts, shape.threads, smem, s>>>(p);
+        else if (shape.vpt == 2) rms_norm_backward_kernel<T, Code, 2, false, kSum, false, 256><<<*parts, shape.threads, smem, s>>>(p);
+        else rms_norm_backward_kernel<T, Code, 4, false, kSum, false, 256><<<*parts, shape.threads, smem, s>>>(p);
     }
     return COBALT_OK;
 }
@@ -538,7 +543,7 @@ size_t cobalt_rms_norm_workspace_bytes(int64_t T, int32_t H)
     if (check_rms(T, H, COBALT_F32) != COBALT_OK) return 0;
     int64_t parts = 0;
     for (int elems = 4; elems <= 8; elems += 4) {        // whichever type needs more
-        const int64_t p = rms_parts(T, rms_shape(H / elems, 2), kMaxSms);
+        const int64_t p = rms_parts(T, rms_shape(H, elems, 2, 2048), kMaxSms);
         parts = p > parts ? p : parts;
     }
     return round_up(static_cast<size_t>(parts) * H * sizeof(float), 256);
