@@ -681,6 +681,9 @@ linear_join_kernel(const __grid_constant__ LinearArgs p)
 
 constexpr int kFewThreads = 256;
 
+// CTAs an SM that fit, by the registers of the kernel's launch bounds.
+constexpr int few_resident(int rows) { return rows < 4 ? 4 : 3; }
+
 // Sixteen bytes of an operand's row as fp32: eight bf16 values or sixteen e4m3 ones.
 template <bool kE4M3>
 struct OperandVec {
@@ -707,7 +710,7 @@ struct OperandVec {
 // rows from L1, and add their sums in order.  Persistent CTAs; the next feature's first vectors are under way while one is summed up.
 // Every vector index is clamped to the row, so that no address lies outside it.
 template <bool kE4M3, int R>
-__global__ void __launch_bounds__(kFewThreads, R < 4 ? 4 : 3)
+__global__ void __launch_bounds__(kFewThreads, few_resident(R))
 linear_few_rows_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict__ w, int T, int K, int N, int share, void* out, const Finish f)
 {
     constexpr int kAhead = 4, kElems = OperandVec<kE4M3>::kElems;        // vectors of W that a lane has in flight
@@ -1036,8 +1039,6 @@ static int launch_product(const void* a, const void* b, int64_t I, int64_t J, in
 // 2048, two tokens 9.2 / 11.0, three 16.8 / 11.2; 2048 to 1408, four tokens 4.1 / 7.2; 4096 to 8192, two tokens 18.6 / 15.9.
 static bool few_rows(int64_t T, int32_t K, int32_t N) { return T == 1 || (T <= 4 && T * K * N <= (1ll << 25)); }
 
-constexpr int kFewResident = 4;          // CTAs an SM
-
 template <bool kE4M3>
 static int launch_few_rows(const void* x, const void* w, int T, int K, int N, void* out, const Finish& f, cudaStream_t s)
 {
@@ -1047,7 +1048,7 @@ static int launch_few_rows(const void* x, const void* w, int T, int K, int N, vo
     while (share < 8 && N * share < 4096 && vecs >= 256 * share) share *= 2;
     int sms = 0;
     COBALT_TRY(sm_count(&sms));
-    const int tasks = (N + 8 / share - 1) / (8 / share), most = kFewResident * sms;
+    const int tasks = (N + 8 / share - 1) / (8 / share), most = few_resident(T > 2 ? 4 : T) * sms;
     const dim3 grid(static_cast<unsigned>(tasks < most ? tasks : most)), block(kFewThreads);
     const uint8_t *a = static_cast<const uint8_t*>(x), *b = static_cast<const uint8_t*>(w);
     if (T == 1) return launch_after(linear_few_rows_kernel<kE4M3, 1>, grid, block, 0, s, a, b, T, K, N, share, out, f);
