@@ -262,3 +262,17 @@ def test_linear_bias_gradient_alone_takes_the_workspace_of_the_whole_call():
         cb.linear_backward(dy, None, None, ws, grad_bias=got)
         ref = dy.double().sum(0)
         assert ((got.double() - ref).abs() <= t * U * dy.double().abs().sum(0) + D.HALF[BF16] * ref.abs() * 1.001).all()
+
+
+@pytest.mark.parametrize("K,N", [(16384, 264), (14080, 24), (13056, 520), (16, 8), (4096, 5000)])
+def test_linear_one_token_from_8_bit_rows(K, N):
+    """Widths on both sides of what fits in shared memory, and features that no CTA number divides.  bf16 results: half a step."""
+    import paper_2609_36959_b200 as cb
+    x, w, bias, residual, _ = _inputs(1, K, N, K + N)
+    x8, w8 = _rows8(x), _rows8(w)
+    out = torch.full((2, N), 7.0, dtype=BF16, device="cuda")
+    cb.linear(x8, w8, out[:1], _workspace(1, K, N), bias=bias, residual=residual)
+    xv, wv = D.values(*x8, 0), D.values(*w8, 0)
+    ref = xv @ wv.t() + bias.double() + residual.double()
+    tol = 2 * (K + 4) * U * (xv.abs() @ wv.abs().t() + bias.double().abs() + residual.double().abs()) + D.HALF[BF16] * ref.abs() * 1.001
+    assert ((out[:1].double() - ref).abs() <= tol).all() and (out[1] == 7).all()
