@@ -684,34 +684,44 @@ constexpr int kFewThreads = 256;
 // CTAs an SM that fit, by the registers of the kernel's launch bounds.
 constexpr int few_resident(int rows) { return rows < 4 ? 4 : 3; }
 
-// Sixteen bytes of an operand's row as fp32: eight bf16 values or sixteen e4m3 ones.
+// Sixteen bytes of an operand's row as pairs of 16-bit floats: eight bf16 values, or sixteen e4m3 ones, which are exact in fp16.
 template <bool kE4M3>
 struct OperandVec {
     static constexpr int kElems = kE4M3 ? 16 : 8;
-    float f[kElems];
+    uint32_t h[kElems / 2];
+    __device__ __forceinline__ OperandVec() {}
     __device__ __forceinline__ explicit OperandVec(const uint4& v)
     {
-        if constexpr (kE4M3) {
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float e[4];
-                CodeE4M3::decode4(w[i], e);
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (kE4M3) h[2 * i] = CodeE4M3::half2_bits(w[i]), h[2 * i + 1] = CodeE4M3::half2_bits(w[i] >> 16);
+            else h[i] = w[i];
+        }
+    }
+    // sum[0] and sum[1]: of the even and of the odd columns' products, which are exact in fp32
+    __device__ __forceinline__ void dot(const OperandVec& b, float (&sum)[2]) const
+    {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) f[4 * i + k] = e[k];
-            }
-        } else {
-            Vec16<bf16>::unpack(v, f);
+        for (int i = 0; i < kElems / 2; ++i) {
+            if constexpr (kE4M3)
+                asm("{\n\t.reg .b16 a, b, c, d;\n\tmov.b32 {a, b}, %2;\n\tmov.b32 {c, d}, %3;\n\t"
+                    "fma.rn.f32.f16 %0, a, c, %0;\n\tfma.rn.f32.f16 %1, b, d, %1;\n\t}"
+                    : "+f"(sum[0]), "+f"(sum[1]) : "r"(h[i]), "r"(b.h[i]));
+            else
+                asm("{\n\t.reg .b16 a, b, c, d;\n\tmov.b32 {a, b}, %2;\n\tmov.b32 {c, d}, %3;\n\t"
+                    "fma.rn.f32.bf16 %0, a, c, %0;\n\tfma.rn.f32.bf16 %1, b, d, %1;\n\t}"
+                    : "+f"(sum[0]), "+f"(sum[1]) : "r"(h[i]), "r"(b.h[i]));
         }
     }
 };
 
 // Up to R tokens on the fp32 units: `share` warps (1, 2, 4 or 8 of a CTA's eight) take one feature, its row of W once and the tokens'
 // rows from L1, and add their sums in order.  Persistent CTAs; the next feature's first vectors are under way while one is summed up.
-// Every vector index is clamped to the row, so that no address lies outside it.  kStaged: the token's e4m3 values are decoded once a
-// CTA, to fp32 in shared memory (sixteen bytes of every quarter of a vector together: neighbouring lanes read neighbouring ones), since
-// decoding bounds that form (7168 to 16384 26.5 us, 30.6 with every feature's own decoding; four tokens 9.4 and 7.6 at 2048 to 4096: not
-// for them).
+// Every vector index is clamped to the row, so that no address lies outside it.  The products of 16-bit floats are added to fp32 sums by one
+// instruction (one token, 7168 to 2048 bf16 6.8 us; with the values converted to fp32 first 8.3).  kStaged: the tokens' e4m3 values are
+// decoded once a CTA, to fp16 in shared memory (sixteen bytes of either half of a vector together: neighbouring lanes read neighbouring
+// ones), since decoding bounds that form (7168 to 16384 23.9 us, 30.6 with every feature's own decoding, four tokens of 512 9.7 and 10.6).
 template <bool kE4M3, int R, bool kStaged>
 __global__ void __launch_bounds__(kFewThreads, few_resident(R))
 linear_few_rows_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict__ w, int T, int K, int N, int share, void* out, const Finish f)
@@ -729,18 +739,18 @@ linear_few_rows_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict_
         for (int i = 0; i < kAhead; ++i) next[i] = ld_stream16(row + 16 * static_cast<int64_t>(min(base + 32 * i + lane, vecs - 1)));
     };
     load(blockIdx.x, start);
-    extern __shared__ float4 staged[];           // [4][vecs]
+    extern __shared__ uint4 staged[];            // [R][2][vecs]
     if constexpr (kStaged) {
-        for (int v = threadIdx.x; v < vecs; v += kFewThreads) {
-            const OperandVec<kE4M3> b(__ldg(reinterpret_cast<const uint4*>(x) + v));
+        for (int v = threadIdx.x; v < R * vecs; v += kFewThreads) {
+            const int r = v / vecs, at = v - r * vecs;
+            const OperandVec<kE4M3> b(__ldg(reinterpret_cast<const uint4*>(x) + static_cast<int64_t>(min(r, T - 1)) * vecs + at));
 #pragma unroll
-            for (int c = 0; c < 4; ++c) staged[c * vecs + v] = make_float4(b.f[4 * c], b.f[4 * c + 1], b.f[4 * c + 2], b.f[4 * c + 3]);
+            for (int c = 0; c < 2; ++c) staged[(2 * r + c) * vecs + at] = make_uint4(b.h[4 * c], b.h[4 * c + 1], b.h[4 * c + 2], b.h[4 * c + 3]);
         }
         __syncthreads();
     }
     for (int task = blockIdx.x, turn = 0; task < tasks; task += gridDim.x, turn ^= 1) {
-        float sum[R] = {};
-        Pair both = pair(0.0f);                  // kStaged: sums of even and of odd columns
+        float sum[R][2] = {};
         int base = start;
         do {
             uint4 now[kAhead];
@@ -754,30 +764,30 @@ linear_few_rows_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict_
                 const int v = base + 32 * i + lane;
                 if (v >= vecs) continue;
                 const OperandVec<kE4M3> a(now[i]);
-                if constexpr (kStaged) {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const float4 b = staged[c * vecs + v];
-                        both = fma2(pair(a.f[4 * c], a.f[4 * c + 1]), pair(b.x, b.y), both);
-                        both = fma2(pair(a.f[4 * c + 2], a.f[4 * c + 3]), pair(b.z, b.w), both);
-                    }
-                    continue;
-                }
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
-                    const int token = R == 1 ? 0 : min(r, T - 1);
-                    const OperandVec<kE4M3> b(__ldg(reinterpret_cast<const uint4*>(x + (static_cast<int64_t>(token) * vecs + v) * 16)));
+                    if constexpr (kStaged) {
+                        OperandVec<kE4M3> b;
 #pragma unroll
-                    for (int k = 0; k < kElems; ++k) sum[r] = fmaf(a.f[k], b.f[k], sum[r]);
+                        for (int c = 0; c < 2; ++c) {
+                            const uint4 u = staged[(2 * r + c) * vecs + v];
+                            b.h[4 * c] = u.x, b.h[4 * c + 1] = u.y, b.h[4 * c + 2] = u.z, b.h[4 * c + 3] = u.w;
+                        }
+                        a.dot(b, sum[r]);
+                    } else {
+                        const int token = R == 1 ? 0 : min(r, T - 1);
+                        a.dot(OperandVec<kE4M3>(__ldg(reinterpret_cast<const uint4*>(x + (static_cast<int64_t>(token) * vecs + v) * 16))), sum[r]);
+                    }
                 }
             }
             base += stride;
         } while (base < vecs);
+        float total[R];
 #pragma unroll
-        for (int r = 0; r < R; ++r) sum[r] = warp_sum(kStaged ? both.v.x + both.v.y : sum[r]);
+        for (int r = 0; r < R; ++r) total[r] = warp_sum(sum[r][0] + sum[r][1]);
         if (lane == 0) {
 #pragma unroll
-            for (int r = 0; r < R; ++r) sums[turn][warp][r] = sum[r];
+            for (int r = 0; r < R; ++r) sums[turn][warp][r] = total[r];
         }
         __syncthreads();
         // one thread a result
@@ -1057,9 +1067,9 @@ static int launch_product(const void* a, const void* b, int64_t I, int64_t J, in
     return launch_after(linear_join_kernel<kProduct>, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, s, p);
 }
 
-// Calls that the fp32 units take: one token, and up to four while the products are few.  Measured (us, this form / tiles, bf16): 7168 to
-// 2048, two tokens 9.2 / 11.0, three 16.8 / 11.2; 2048 to 1408, four tokens 4.1 / 7.2; 4096 to 8192, two tokens 18.6 / 15.9.
-static bool few_rows(int64_t T, int32_t K, int32_t N) { return T == 1 || (T <= 4 && T * K * N <= (1ll << 25)); }
+// Calls that the fp32 units take: one token, and two to four while the products are few.  Measured (us, this form / tiles, bf16): two
+// tokens, 7168 to 2048 9.0 / 10.8, 4096 to 8192 16.8 / 15.7; four, 2048 to 1408 3.8 / 6.4, 2048 to 4096 9.2 / 8.2.
+static bool few_rows(int64_t T, int32_t K, int32_t N) { return T == 1 || (T <= 4 && T * K * N <= (T == 2 ? 1ll << 25 : 1ll << 24)); }
 
 template <bool kE4M3>
 static int launch_few_rows(const void* x, const void* w, int T, int K, int N, void* out, const Finish& f, cudaStream_t s)
@@ -1075,11 +1085,13 @@ static int launch_few_rows(const void* x, const void* w, int T, int K, int N, vo
     const uint8_t *a = static_cast<const uint8_t*>(x), *b = static_cast<const uint8_t*>(w);
     auto launch = [&](auto kernel, size_t smem) { return launch_after(kernel, grid, block, smem, s, a, b, T, K, N, share, out, f); };
     if constexpr (kE4M3) {
-        // staged where the shared memory of an SM has room for it four times
-        const size_t smem = static_cast<size_t>(K) * sizeof(float);
-        if (T == 1 && smem <= 55 * 1024) {
-            COBALT_TRY(ensure_kernel_attributes(reinterpret_cast<const void*>(&linear_few_rows_kernel<true, 1, true>), smem, false));
-            return launch(linear_few_rows_kernel<true, 1, true>, smem);
+        // staged where the shared memory of an SM has room for it in all its CTAs
+        const int rows = T > 2 ? 4 : T;
+        const size_t smem = static_cast<size_t>(rows) * K * 2;
+        if (smem <= static_cast<size_t>(220 / few_resident(rows)) * 1024) {
+            auto kernel = rows == 1 ? linear_few_rows_kernel<true, 1, true> : rows == 2 ? linear_few_rows_kernel<true, 2, true> : linear_few_rows_kernel<true, 4, true>;
+            COBALT_TRY(ensure_kernel_attributes(reinterpret_cast<const void*>(kernel), smem, false));
+            return launch(kernel, smem);
         }
     }
     return T == 1 ? launch(linear_few_rows_kernel<kE4M3, 1, false>, 0)

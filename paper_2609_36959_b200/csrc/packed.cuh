@@ -25,11 +25,17 @@ struct CodeE4M3 {
         return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
     }
     static __device__ __forceinline__ uint32_t encode4(const float (&t)[4]) { return encode2(t[0], t[1]) | (encode2(t[2], t[3]) << 16); }
+    // The values of the low two bytes as a pair of fp16 numbers.
+    static __device__ __forceinline__ uint32_t half2_bits(uint32_t w)
+    {
+        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w), __NV_E4M3);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
     static __device__ __forceinline__ void decode4(uint32_t w, float (&f)[4])
     {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w >> (16 * i)), __NV_E4M3);
+            const uint32_t h = half2_bits(w >> (16 * i));
             const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h));
             f[2 * i] = v.x;
             f[2 * i + 1] = v.y;
