@@ -184,3 +184,23 @@ def test_rms_norm_in_8_bits_of_the_smallest_values(dtype, code):
         got, step = D.values(q, scales, group), D.values(torch.ones_like(ref), scales, group)
         half = 0.5 * step if code == torch.int8 else torch.maximum(2.0 ** -4 * ref.abs(), 2.0 ** -10 * step)
         assert ((got - ref).abs() <= half * (1 + 64 * U) + 64 * U * ref.abs() + 448 * 2.0 ** -150).all()
+
+
+@pytest.mark.parametrize("second", [False, True])
+@pytest.mark.parametrize("rows", ["plain", "i8", "e4m3"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,H", [(1300, 5120), (700, 8192), (450, 16384)])
+def test_rms_norm_gradients_of_several_long_rows_a_cta(T, H, dtype, rows, second):
+    """Every CTA has more than one row, so that the next one's loads are under way; and the result takes the gradient's place."""
+    import paper_2609_36959_b200 as cb
+    x, _, dy, ds, gamma = _inputs(T, H, dtype, T + H)
+    s, kept = x.double(), x
+    if rows != "plain":
+        kept = torch.empty((T, H), dtype=torch.int8 if rows == "i8" else torch.float8_e4m3fn, device="cuda"), torch.empty((T, H // 128), device="cuda")
+        cb.pack_rows(x, *kept)
+        s = D.values(*kept, 128)
+    rstd = (1.0 / torch.sqrt((s * s).mean(1) + 1e-5)).float()
+    ws = torch.full((cb.rms_norm_workspace_bytes(T, H),), 0xAB, dtype=torch.uint8, device="cuda")
+    dx, dg = dy.clone(), torch.empty(H, device="cuda")
+    cb.rms_norm_backward(dx, kept, gamma, rstd, dx, dg, ws, grad_sum=ds if second else None)
+    _check_backward(dy, s, gamma, rstd, ds if second else None, dx, dg, dtype)
