@@ -5,7 +5,7 @@
 //           With one scale a row a warp or a CTA holds the row in registers between its largest value and the codes.
 //   unpack  the same walk without the reduction.
 //
-// Bound by HBM: 32768 x 7168 bf16 with a scale for 128 columns 132 us (5.3 TB/s), with one a row 118 us, read back 109 us (6.5 TB/s).
+// Bound by HBM: 32768 x 7168 bf16 with a scale for 128 columns 114 us (6.2 TB/s), with one a row 118 us, read back 109 us (6.5 TB/s).
 // Rows whose width is no multiple of such a piece, or pointers off a 32-byte boundary, take eight columns a piece.
 #include "packed.cuh"
 
@@ -103,9 +103,14 @@ struct Piece {
     }
 };
 
+// CTAs an SM: four spill a few registers and are faster all the same (32768 x 7168 bf16 114 us, three 118, without a bound two and 134), but
+// for e4m3 codes of fp32 (16384 x 4096 66 us with three, 75 with four, 79 without).
+template <typename T, typename Code>
+constexpr int kPackCtas = sizeof(T) == 4 && Code::kLargest == CodeE4M3::kLargest ? 3 : 4;
+
 // One scale for each 128 columns.  per_row counts the last group's missing columns too: its lanes take part in the shuffles.
 template <typename T, typename Code, int C>
-__global__ void __launch_bounds__(kPackThreads)
+__global__ void __launch_bounds__(kPackThreads, kPackCtas<T, Code>)
 pack_groups_kernel(const T* __restrict__ x, int64_t rows, int H, uint8_t* __restrict__ q, float* __restrict__ scales)
 {
     constexpr int kLanes = kPackGroup / C, N = Vec16<T>::kElems;
