@@ -420,8 +420,10 @@ struct RmsShape {
     int resident;                            // CTAs of the backward kernels that fit on an SM
 };
 
-// Up to this many rows the forward pass takes two vectors a thread: more threads for a row, which is all the latency there is.
-constexpr int64_t kFewRows = 148;
+// Vectors up to which the forward pass takes two a thread instead of four: more threads for a row where its latency counts, and narrow rows
+// keep more of them under way.  Two / four, us: 500 x 2048 bf16 with residual 3.5 / 4.0, to e4m3 rows 3.9 / 4.5; 4999 x 2048 14.6 / 14.8 and
+// 16.2 / 17.0; 1000 x 7168 11.4 / 11.9 and 14.2 / 13.8; 32768 x 7168 273 / 275 and 312 / 258; 65536 x 2048 161 / 161 and 152 / 146.
+static bool few_vectors(int64_t rows, int n_vec) { return rows * n_vec <= (n_vec <= 256 ? 1 << 21 : 1 << 19); }
 
 // A warp a row up to 128 vectors; above, a CTA a row with `vpt` vectors a thread, four of rows of more than `most`.  elems: values of a
 // vector.
@@ -470,7 +472,7 @@ static bool check_code(int32_t code, int32_t group) { return (code == COBALT_E4M
 template <typename T, bool kPacked>
 static void launch_forward(const RmsForward& p, cudaStream_t s)
 {
-    const RmsShape shape = rms_shape(p.H, Vec16<T>::kElems, p.rows <= kFewRows ? 2 : 4, 896);
+    const RmsShape shape = rms_shape(p.H, Vec16<T>::kElems, few_vectors(p.rows, p.H / Vec16<T>::kElems) ? 2 : 4, 896);
     const int64_t per_cta = shape.cta ? 1 : shape.threads / 32, ctas = (p.rows + per_cta - 1) / per_cta;
     const unsigned grid = static_cast<unsigned>(ctas);
     if (shape.cta) {
