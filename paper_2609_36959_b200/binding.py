@@ -834,7 +834,7 @@ def rms_norm_backward(grad_y: torch.Tensor, rows, gamma: torch.Tensor, rstd: tor
 
 
 def linear_workspace_bytes(T: int, K: int, N: int) -> int:
-    """For linear and linear_backward on x [T, K] and w [N, K]."""
+    """For linear and linear_backward on x [T, K] and w [N, K]; what T tokens need serves fewer."""
     return _lib.cobalt_linear_workspace_bytes(T, K, N)
 
 
