@@ -204,3 +204,23 @@ def test_rms_norm_gradients_of_several_long_rows_a_cta(T, H, dtype, rows, second
     dx, dg = dy.clone(), torch.empty(H, device="cuda")
     cb.rms_norm_backward(dx, kept, gamma, rstd, dx, dg, ws, grad_sum=ds if second else None)
     _check_backward(dy, s, gamma, rstd, ds if second else None, dx, dg, dtype)
+
+
+@pytest.mark.parametrize("group", [0, 128])
+@pytest.mark.parametrize("code", [torch.int8, torch.float8_e4m3fn], ids=["i8", "e4m3"])
+def test_rms_norm_in_8_bits_of_infinities_and_nan(code, group):
+    """A NaN makes its row's values NaN.  An infinity makes rstd 0: its own group's values are NaN, the row's other groups 0."""
+    import paper_2609_36959_b200 as cb
+    x, _, _, _, gamma = _inputs(4, 512, torch.bfloat16, 9)
+    x[1, 200], x[2, 300] = float("nan"), float("inf")
+    x[3] = 0
+    q, scales = torch.full((4, 512), 7, dtype=torch.uint8, device="cuda").view(code), torch.zeros((4, len(D.groups_of(512, group))), device="cuda")
+    y = torch.empty_like(x)
+    cb.rms_norm(x, gamma, 1e-5, y=y, packed=(q, scales))
+    v = D.values(q, scales, group)
+    assert torch.isnan(v[1]).all() and torch.isnan(y[1]).all() and (q[1].view(torch.uint8) == 0).all()
+    bad = torch.isnan(v[2])
+    want = torch.zeros_like(bad)
+    want[256:384] = True
+    assert bad.all() if group == 0 else torch.equal(bad, want) and (v[2][~want] == 0).all()
+    assert torch.isnan(y[2, 300]) and (v[3] == 0).all() and torch.isfinite(v[0]).all()
