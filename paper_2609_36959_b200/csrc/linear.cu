@@ -17,7 +17,7 @@
 //   - Where k is short (four blocks) and i long, a router's dx, a pair keeps its j's operand in shared memory for all tiles of i and only
 //     the other one streams: half of what went through L2, which bounded that product (11 TB/s).
 //   - Epilogue: bias, scales and activation are applied to the accumulators as they are read, and bf16 results leave through shared
-//     memory by tensor-map stores.  With a residual, a saved pre-activation or fp32 results the accumulators pass through shared memory in
+//     memory by tensor-map stores.  With a residual, a saved pre-activation or kLong the accumulators pass through shared memory in
 //     fp32 instead, 32 columns of j at a time, so that a thread has eight neighbouring i of one j: everything moves in 16-byte vectors, and
 //     the 128 i that share a scale when pre is kept in 8 bits are sixteen neighbouring lanes.
 //   - One token, or a few and a small W: the fp32 units, W's rows streamed by warps.
@@ -54,14 +54,18 @@ constexpr int kPitch32 = 528, kBuffer32 = 16 * kPitch32;
 constexpr int kStaging = 4 * (kBuffer16 > kBuffer32 ? kBuffer16 : kBuffer32);
 constexpr int kLinearSmem = kRing * kSlotBytes + kStaging + 256;
 constexpr int kLinearThreads = 320;
-constexpr int kLongBlocks = 8;           // blocks of k (512 values) that the tensor cores add up before fp32 registers take over
+// Blocks of k that the tensor cores add up before fp32 registers take over (kLong): 512 bf16 values or 1024 e4m3 ones of an fp32 result,
+// 8192 tokens of the weights' gradient.
+constexpr int kResultBlocks = 8, kTokenBlocks = 128;
 constexpr int kBand = 8;                 // tiles of j that run together for every tile of i
 
 enum Product { kForward, kForwardE4M3, kGradRows, kGradWeights };
 
-// kPlain: bf16 results of bias, scales and activation alone.  kFull: any.  kLong: fp32 results; the tensor cores cut every addition (a sum
-// of 7168 products is 6.9e-6 too small, in proportion to their number), so 512 values are added there and the sums of those, rounded,
-// in registers (4.7e-7).
+// kPlain: bf16 results of bias, scales and activation alone.  kFull: any.  kLong: long sums.  The tensor cores cut every addition, 16 bf16
+// products each: a sum of 7168 of either sign is 7.9e-6 off, a sum of 8192 of one sign 3.0e-5 too small, of 131072 7.7e-4 and of a million
+// 6.6e-3, more than half a step of bf16.  So a part is added there and the sums of the parts, rounded, in registers: for fp32 results 512
+// values at a time (4.8e-7), for the weights' gradient, where a split has more than 8192 tokens, 8192 at a time (2.3 ms at 131072 tokens,
+// 4096 x 2560, as in one go).  bf16 results of sums over K or N, at most 65536 values, are added in one go: a tenth of a half step.
 enum Form { kPlain, kFull, kLong };
 
 // The elementwise part of the forward call.
@@ -106,8 +110,8 @@ __device__ __forceinline__ float fast_sigmoid(float v) { return fast_inverse(1.0
 // The tail T(a) of the normal distribution, 1 - Phi(a), for a >= 0: exp(-a^2 / 2) t Q(t) with t = 1 / (1 + 0.305 a), the form of 7.1.26 in
 // Abramowitz and Stegun's Handbook.  Q, of degree 7, was fitted to the least relative error (weighted least squares, the weights times the
 // error until it is level, after Lawson): 9.7e-8 for a up to 14.5, beyond which the exponential is 0.  The error has to be relative: the tail
-// is all there is of gelu below 0.  (A rational power good to 3e-7 absolutely was 0.6 us of 18 faster at 4999 x 2048 to 1408, and 1 % off
-// at -4.)  Rounding adds 1.5 a^2 + 22 units of 2^-24.
+// is all there is of gelu below 0.  (A rational power good to 3e-7 absolutely was 0.6 us of 18 faster at 4999 x 2048 to 1408, and 0.4 % off
+// at -4, 5 % at -5.)  Rounding adds 1.5 a^2 + 22 units of 2^-24.
 __device__ __forceinline__ Pair normal_tail(const Pair& a)
 {
     const Pair arg = a * a * pair(-0.5f * kLog2E), d = fma2(a, pair(0.305f), pair(1.0f));
@@ -306,6 +310,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
 {
     constexpr bool kAMn = kProduct == kGradRows || kProduct == kGradWeights, kBMn = kProduct == kGradWeights;
     constexpr int kStepK = kProduct == kForwardE4M3 ? kDeepBytes : kDeep;                // values of k in a block
+    constexpr int kLongBlocks = kProduct == kGradWeights ? kTokenBlocks : kResultBlocks;
     extern __shared__ __align__(1024) uint8_t smem[];                    // the swizzle counts from 1024-byte boundaries
     const uint32_t base = smem_u32(smem), staging = base + kRing * kSlotBytes, bars = staging + kStaging;
     constexpr int kSlots = kStay ? kStayRing : kRing, kStride = kStay ? kHalfBytes : kSlotBytes;
@@ -1196,7 +1201,9 @@ int cobalt_linear_backward(const void* grad_out, const void* x, const void* w, c
     }
     if (grad_w) {
         p.out = grad_w;
-        COBALT_TRY((launch_product<kGradWeights, kPlain>(x, d, K, N, T, p, workspace, s)));
+        const bool long_sum = linear_plan(K, N, deep_blocks(T, kDeep)).per_split > kTokenBlocks;
+        COBALT_TRY((long_sum ? launch_product<kGradWeights, kLong>(x, d, K, N, T, p, workspace, s)
+                             : launch_product<kGradWeights, kPlain>(x, d, K, N, T, p, workspace, s)));
     }
     return COBALT_OK;
 }
