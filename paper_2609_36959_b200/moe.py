@@ -119,8 +119,7 @@ class MoELayer:
             self.grad_n_dense = new(T, H)
         self.workspace = torch.empty((ws,), dtype=torch.uint8, device=dev)
         self.x = None                                   # input of the last forward call
-        self.rows8 = None                               # the same in 8 bits, after restore()
-        self.x_restored = None                          # and their values, allocated by the first restore()
+        self.x_restored = None                          # restored rows, allocated by the first restore()
 
     def _experts(self, send: torch.Tensor, expert_out: torch.Tensor) -> None:
         cb.expert_ffn(send, self.step.dest_offsets, self.slot_expert, self.w_gate_up, self.w_down, self.act, expert_out,
@@ -160,7 +159,7 @@ class MoELayer:
         first: the layer's input is their sum, x alone is not kept.  Otherwise x is kept by reference and read again by
         backward; it may be the output buffer itself if no backward call follows."""
         s = self.step
-        self.x, self.seed, self.rows8 = self._norm(x, residual), seed, None
+        self.x, self.seed = self._norm(x, residual), seed
         x = self.x
         if self.router == "plain":
             torch.mm(s.x, self.w_router.t(), out=self.logits)
@@ -188,15 +187,16 @@ class MoELayer:
         return LayerCheckpoint(rows, self.logits.clone(), s.topk_ids.clone(), s.gate_w.clone(), s.src_rank.clone(), seed)
 
     def restore(self, checkpoint: LayerCheckpoint) -> None:
-        """Computes again what backward needs, with the routing as it was and the rows as they were kept.  backward then gives the
-        gradients at those rows; the checkpoint is read by it and must stay as it is.  step.src_rank is the checkpoint's afterwards."""
+        """Computes again what backward needs, with the routing as it was and the rows as they were kept, rounded to bfloat16.  backward
+        then gives the gradients at those rows; of the checkpoint it reads a seed on the device only.  step.src_rank is the checkpoint's
+        afterwards."""
         s, c = self.step, checkpoint
         if tuple(c.rows[0].shape) != (self.T, self.H) or c.logits.shape != self.logits.shape or c.topk_ids.shape != s.topk_ids.shape:
             raise cb.CobaltError(cb.ERR_INVALID_ARG, "MoELayer.restore (sizes)")
         if self.x_restored is None:
             self.x_restored = torch.empty((self.T, self.H), dtype=torch.bfloat16, device=s.device)
         cb.unpack_rows(*c.rows, self.x_restored)
-        self.x, self.seed, self.rows8 = self._norm(self.x_restored, None), c.seed, c.rows
+        self.x, self.seed = self._norm(self.x_restored, None), c.seed
         self.logits.copy_(c.logits)
         s.topk_ids.copy_(c.topk_ids)
         s.gate_w.copy_(c.gate_w)
@@ -235,8 +235,7 @@ class MoELayer:
                                grad_bias=self.grad_b_shared_up)
             self.grad_n.add_(self.grad_n_dense)
         if self.norm == "rms":                          # the gradient down the residual stream joins in the same pass
-            cb.rms_norm_backward(self.grad_n, self.x if self.rows8 is None else self.rows8, self.gamma, self.rstd, self.grad_x,
-                                 self.grad_gamma, self.workspace, grad_sum=grad_out)
+            cb.rms_norm_backward(self.grad_n, self.x, self.gamma, self.rstd, self.grad_x, self.grad_gamma, self.workspace, grad_sum=grad_out)
             return self.grad_x
         cb.layer_norm_backward(self.grad_n, self.x, self.gamma, self.mean, self.rstd, self.grad_n, self.grad_gamma,
                                self.grad_beta, self.workspace)
