@@ -11,8 +11,11 @@ Plumbing only, as in `router`: torch allocates the buffers once, multiplies by t
 unless router="linear") and adds gradients; everything else is one C-ABI call each, enqueued on the current torch stream.
 
 What a layer needs for its backward pass is 2 T H + 4 P H + 6 P F bytes and more.  `save()` leaves T H bytes of it (the layer's
-input rows in 8 bits) and the small arrays of the routing; `restore()` computes the rest again, so that layers may share one
-object's buffers.
+input rows in 8 bits) and the small arrays of the routing; `restore()` computes the rest again, so that layers of the same sizes
+and options may share one object's buffers.  The parameters are attributes that the calls read when they are made, and none is
+part of a checkpoint: before each layer's forward and restore calls the user assigns that layer's tensors (gamma, beta, w_*, b_*;
+pack_shared() for the 8-bit block), and after its backward call takes the gradients out of grad_* (the next backward call
+overwrites them).
 """
 from __future__ import annotations
 
@@ -28,7 +31,7 @@ from .router import RouteStep
 @dataclass
 class LayerCheckpoint:
     """What `MoELayer.restore` starts from: the layer's input rows in 8 bits (with the residual added, if there was one) and the
-    routing's small arrays."""
+    routing's small arrays.  Not the parameters: those of the layer have to be in the object again."""
 
     rows: Tuple[torch.Tensor, torch.Tensor]        # int8 [T, H], float32 [T, ceil(H / 128)]
     logits: torch.Tensor
