@@ -1,13 +1,11 @@
 // Status codes, the device error word and the expert-layout handle.
 #include <stdlib.h>
 
-#include <map>
-#include <mutex>
 #include <new>
-#include <utility>
 #include <vector>
 
 #include "common.cuh"
+#include "kernel_grants.h"
 
 namespace cobalt {
 
@@ -41,28 +39,16 @@ int device_error_word(uint32_t** out)
 
 int ensure_kernel_attributes(const void* kernel, size_t bytes, bool non_portable_cluster)
 {
-    static std::mutex lock;
-    static std::map<std::pair<const void*, int>, size_t> granted;   // (kernel, device) -> bytes + 1 once set up
+    static KernelGrants grants;
     int dev = 0;
     COBALT_CUDA_TRY(cudaGetDevice(&dev));
-    const auto key = std::make_pair(kernel, dev);
-    try {                                                           // the map may run out of host memory
-        {
-            std::lock_guard<std::mutex> guard(lock);
-            auto it = granted.find(key);
-            if (it != granted.end() && it->second > bytes) return COBALT_OK;
-        }
+    return grants.ensure(kernel, dev, bytes, [&]() -> int {
         if (bytes > 48 * 1024)
             COBALT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)));
         if (non_portable_cluster)
             COBALT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-        std::lock_guard<std::mutex> guard(lock);
-        size_t& have = granted[key];
-        if (have < bytes + 1) have = bytes + 1;
-    } catch (...) {
-        return COBALT_ERR_HOST_ALLOC;
-    }
-    return COBALT_OK;
+        return COBALT_OK;
+    });
 }
 
 int sm_count(int* out)
