@@ -456,7 +456,8 @@ int cobalt_unpack_rows(const void* q, const float* scales, int64_t T, int32_t H,
  * s as rows_type `dtype` (row_scales and group are then not read), or s in 8 bits (rows_type COBALT_I8 or COBALT_E4M3) as
  * cobalt_pack_rows leaves it.  gamma, grad_gamma fp32 [H]; rstd fp32 [T].  H a multiple of 8, at most 16384; T < 2^31;
  * T = 0 is allowed (grad_gamma is then 0).  eps >= 0; a row of zeros with eps = 0 gives NaN.  sum and y may each be x or
- * residual (not both the same buffer), grad_x may be grad_y or grad_sum.  Results do not vary from run to run. */
+ * residual (not both the same buffer), grad_x may be grad_y or grad_sum.  q_scales, row_scales and the backward call's rstd may lie on any 4-byte boundary (rows
+ * from any token on).  Results do not vary from run to run. */
 int cobalt_rms_norm(const void* x, const void* residual, const float* gamma, int64_t T, int32_t H,
                     int32_t dtype, float eps, void* sum, void* y, void* q, float* q_scales, int32_t q_code,
                     int32_t q_group, float* rstd, cobalt_stream_t stream);
@@ -470,7 +471,7 @@ int cobalt_rms_norm_backward(const void* grad_y, const void* grad_sum, const voi
 /* ---- linear: a product with bias, activation and residual ------------------------------------------------
  *   pre = x w^T + bias     out = act(pre) + residual
  * x [T, K] and w [N, K] bf16 (operand COBALT_BF16; the scales are not read), or e4m3 codes with one scale a row, fp32 [T] and
- * [N], as cobalt_pack_rows leaves them with group 0 (operand COBALT_E4M3).  bias bf16 [N] or NULL; residual [T, N] like
+ * [N], as cobalt_pack_rows leaves them with group 0 (operand COBALT_E4M3; x_scales on any 4-byte boundary).  bias bf16 [N] or NULL; residual [T, N] like
  * out, or NULL; out of out_type COBALT_BF16 or COBALT_F32.  pre, where a backward pass follows an activation: bf16 [T, N]
  * (pre_type COBALT_BF16), or COBALT_I8 codes [T, N] with pre_scales fp32 [T, ceil(N / 128)]; else NULL.  The backward
  * call takes the slope at the value that was kept: in 8 bits, values below half a step are 0, where relu's slope is 0 (0.4 % of

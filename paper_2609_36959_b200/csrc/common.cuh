@@ -41,6 +41,7 @@ int ensure_kernel_attributes(const void* kernel, size_t bytes, bool non_portable
 constexpr int kRowsItemBytes = 32768;
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 

@@ -1134,7 +1134,7 @@ int cobalt_linear(const void* x, const float* x_scales, const void* w, const flo
     COBALT_TRY(check_linear(T, K, N, e4m3 ? 16 : 8));
     if (T == 0) return COBALT_OK;
     if (!x || !w || !out || (e4m3 && (!x_scales || !w_scales)) || (pre8 && !pre_scales)) return COBALT_ERR_INVALID_ARG;
-    if (!aligned16(x) || !aligned16(x_scales) || !aligned16(w) || !aligned16(w_scales) || !aligned16(bias) || !aligned16(residual) ||
+    if (!aligned16(x) || !aligned4(x_scales) || !aligned16(w) || !aligned16(w_scales) || !aligned16(bias) || !aligned16(residual) ||
         !aligned16(pre) || !aligned16(pre_scales) || !aligned16(out) || !aligned16(workspace))
         return COBALT_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < linear_workspace(T, K, N)) return COBALT_ERR_WORKSPACE_TOO_SMALL;

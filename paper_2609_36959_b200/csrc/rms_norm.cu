@@ -541,7 +541,7 @@ int cobalt_rms_norm(const void* x, const void* residual, const float* gamma, int
     if (T == 0) return COBALT_OK;
     if (!x || !gamma || (!y && !q) || (q && !q_scales)) return COBALT_ERR_INVALID_ARG;
     if (!aligned16(x) || !aligned16(residual) || !aligned16(gamma) || !aligned16(sum) || !aligned16(y) || !aligned16(q) ||
-        !aligned16(q_scales) || !aligned16(rstd))
+        !aligned4(q_scales) || !aligned16(rstd))
         return COBALT_ERR_INVALID_ARG;
     const RmsForward p = {x, residual, gamma, on_32_bytes(gamma), T, H, eps, sum, y, static_cast<uint8_t*>(q), q_scales, q_code, q_group, rstd};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -571,7 +571,7 @@ int cobalt_rms_norm_backward(const void* grad_y, const void* grad_sum, const voi
     const bool packed = rows_type != dtype;
     if (packed && !check_code(rows_type, group)) return COBALT_ERR_INVALID_ARG;
     if (!gamma || !grad_gamma || (T > 0 && (!grad_y || !rows || !rstd || !grad_x || (packed && !row_scales)))) return COBALT_ERR_INVALID_ARG;
-    if (!aligned16(grad_y) || !aligned16(grad_sum) || !aligned16(rows) || !aligned16(row_scales) || !aligned16(gamma) || !aligned16(rstd) ||
+    if (!aligned16(grad_y) || !aligned16(grad_sum) || !aligned16(rows) || !aligned4(row_scales) || !aligned16(gamma) || !aligned4(rstd) ||
         !aligned16(grad_x) || !aligned16(grad_gamma) || !aligned16(workspace))
         return COBALT_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < cobalt_rms_norm_workspace_bytes(T, H)) return COBALT_ERR_WORKSPACE_TOO_SMALL;
