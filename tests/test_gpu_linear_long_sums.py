@@ -42,14 +42,17 @@ def test_weight_gradient_of_many_tokens_is_not_too_small():
     assert cb.read_and_clear_device_error() == 0
 
 
-@pytest.mark.parametrize("T,K,N", [(20003, 264, 136), (8200, 1032, 72), (70001, 8, 8)])
+@pytest.mark.parametrize("T,K,N", [(20003, 264, 136), (8200, 1032, 72), (70001, 8, 8), (300001, 264, 136), (1 << 20, 24, 8), (9000, 4104, 2824)])
 def test_weight_gradient_of_long_splits(T, K, N):
-    """Few tiles, long parts of k: every element against 64 bits. A part adds at most 8192 values at a time."""
+    """Sizes that fill no tile, every element against 64 bits: k split into parts below and above 8192 tokens, and (the last) not split.  A part
+    adds at most 8192 values at a time."""
     import paper_2609_36959_b200 as cb
     x, dy = _positive(T, K, 3), _positive(T, N, 4)
     whole = torch.full((N + 1, K), 7.0, dtype=BF16, device="cuda")
     cb.linear_backward(dy, x, None, torch.empty(cb.linear_workspace_bytes(T, K, N), dtype=torch.uint8, device="cuda"), grad_w=whole[:N])
-    ref = dy.double().t() @ x.double()
+    ref = torch.zeros((N, K), dtype=D.F64, device="cuda")
+    for a in range(0, T, 1 << 16):
+        ref += dy[a:a + (1 << 16)].double().t() @ x[a:a + (1 << 16)].double()
     assert ((whole[:N].double() - ref).abs() <= (D.HALF[BF16] * 1.001 + 6.2e-5) * ref).all() and (whole[N] == 7).all()
     assert cb.read_and_clear_device_error() == 0
 
