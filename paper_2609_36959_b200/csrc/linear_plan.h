@@ -27,7 +27,7 @@ inline int64_t deep_blocks(int64_t k, int deep) { return (k + deep - 1) / deep; 
 // n and the number of splits with the least estimated cycles: waves of tiles, a block of k taking 2n cycles on the tensor cores (at least
 // what its loads take), a fixed part for filling and emptying a tile, and the parts' way through L2 where k is split.  The last three
 // numbers are fitted to 40 products of 8 to 4096 by 256 to 8192 with k of 1024 to 8192, every n and up to 16 splits each: the chosen pair
-// takes 1.3 % more than the best one on average and 8 % at most (300 x 7168 to 4096: 23 us, 28 without a split).
+// takes 1.3 % more than the best one on average and 9 % at most (300 x 7168 to 4096: 23 us, 28 without a split).
 inline LinearPlan linear_plan(int64_t I, int64_t J, int64_t blocks)
 {
     static const int kSplits[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32};
